@@ -56,7 +56,7 @@ typedef enum moc_status {
     MOC_OK = 0,
     MOC_ERR_NULL = -1,      /* a required pointer is NULL */
     MOC_ERR_SHAPE = -2,     /* N, C, B, H <= 0; d not in {64,128}; topk out of range; N*topk overflow; 2^31 work items of captions */
-    MOC_ERR_OFFSETS = -3,   /* chunk_offsets not strictly increasing from 0 to N */
+    MOC_ERR_OFFSETS = -3,   /* chunk_offsets not strictly increasing from 0 to N; q_offsets decreasing */
     MOC_ERR_TEXT_SPAN = -4, /* a text span is empty, out of range, overlapping, unsorted or not chunk-aligned */
     MOC_ERR_WINDOW = -5,    /* equal window ids not contiguous, or a window spans two shots */
     MOC_ERR_DTYPE = -6,     /* dtype is neither MOC_BF16 nor MOC_F32 */
@@ -308,6 +308,118 @@ int moc_attn_bwd_after_fwd(const moc_meta *meta, int32_t B, int32_t H, int32_t d
                            const float *lse, const void *d_o, const int32_t *sel, int32_t topk,
                            float softmax_scale, void *dq, void *dk, void *dv, void *workspace,
                            size_t workspace_bytes, void *stream);
+
+/*
+ * Around the layer: a transformer block normalises the queries and keys of
+ * every head, turns them by their positions in time, height and width, and
+ * attends the states of a text or image encoder. The calls below take what the
+ * block's projections write and leave what moc_route and moc_attn_* read, and
+ * the other way round in the backward pass.
+ *
+ * moc_rows: a [B, heads, N, d] tensor in any order of memory. Element
+ * (b, h, n, e) lies at data + b*stride_b + h*stride_h + n*stride_n + e; strides
+ * count elements, the d features of a row are contiguous. data has to be
+ * 16-byte aligned and the strides multiples of 16 bytes (MOC_ERR_ALIGN). A slice
+ * of a fused projection [B, N, 3H, d] is such a tensor, and so is a head-major one.
+ *
+ * moc_rope_plan: how tokens are turned. The d features of a head are d/2 pairs:
+ * (2j, 2j+1), or with halves != 0 (j, j + d/2). The first axis_pairs[0] pairs belong
+ * to axis 0 of the positions, the next axis_pairs[1] to axis 1, and so on; pairs
+ * behind the last axis stay as they are. Pair (x, y) of a token becomes
+ * (x cos a - y sin a, x sin a + y cos a) with a = position on the pair's axis *
+ * freq[pair]. Angles are formed in double precision, so far positions turn as
+ * exactly as near ones.
+ *   positions  DEVICE [N][n_axes] int32, shared by the samples (4-byte aligned)
+ *   freq       DEVICE [sum of axis_pairs] double, radians per unit of position (8-byte aligned)
+ */
+typedef struct moc_rows {
+    void *data;
+    int64_t stride_b, stride_h, stride_n;
+} moc_rows;
+
+#define MOC_MAX_AXES 4
+typedef struct moc_rope_plan {
+    const int32_t *positions;
+    const double *freq;
+    int32_t n_axes;                     /* 1 .. MOC_MAX_AXES */
+    int32_t axis_pairs[MOC_MAX_AXES];   /* >= 0, together at most d/2 */
+    int32_t halves;
+} moc_rope_plan;
+
+/*
+ * Norms of queries and keys with the rotation, in one pass: with x a row of d
+ * features of one head, r = 1/sqrt(mean(x^2) + eps),
+ *   y = weight * x * r,   out = rotation of y (rope NULL: y itself).
+ *   q, k, v       DEVICE in, HOST structs: q has H heads, k and v have Hk. Any of the three
+ *                 may be NULL and is left out then, but not all. v is copied: neither
+ *                 normalised nor turned.
+ *   q_weight, k_weight  DEVICE [d] float or NULL (ones); eps finite and >= 0.
+ *   q_out, k_out, v_out DEVICE out, contiguous [B, heads, N, d], NULL where the input is NULL.
+ * Rows are in float, sums too; results are rounded once, to `dtype`. N here is free of any
+ * layout (an encoder's states have their own); B * heads * N < 2^31. Outputs must not
+ * overlap inputs.
+ *
+ * moc_qk_norm_rope_bwd: gradients of the same call. d_q_out, d_k_out, d_v_out (DEVICE in,
+ * contiguous like the outputs) -> dq, dk, dv (DEVICE out, moc_rows: token-major, or slices of
+ * the gradient of a fused projection) and dq_weight, dk_weight (DEVICE out [d] float, the
+ * sums over samples, heads and tokens; NULL where not wanted). q and k are the
+ * forward's inputs; the norms are formed again from them. For v give d_v_out and dv, or
+ * NULL for both. workspace: moc_qk_norm_rope_workspace_bytes bytes. Sums have a fixed
+ * order: same input, same bits.
+ */
+int moc_qk_norm_rope(int32_t B, int32_t N, int32_t H, int32_t Hk, int32_t d, int dtype, const moc_rows *q,
+                     const moc_rows *k, const moc_rows *v, const float *q_weight, const float *k_weight, float eps,
+                     const moc_rope_plan *rope, void *q_out, void *k_out, void *v_out, void *stream);
+int moc_qk_norm_rope_workspace_bytes(int32_t B, int32_t N, int32_t H, int32_t Hk, int32_t d, int dtype, size_t *bytes);
+int moc_qk_norm_rope_bwd(int32_t B, int32_t N, int32_t H, int32_t Hk, int32_t d, int dtype, const moc_rows *q,
+                         const moc_rows *k, const float *q_weight, const float *k_weight, float eps,
+                         const moc_rope_plan *rope, const void *d_q_out, const void *d_k_out, const void *d_v_out,
+                         const moc_rows *dq, const moc_rows *dk, const moc_rows *dv, float *dq_weight, float *dk_weight,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The rotation alone: out = rotation of x by the plan, or with inverse != 0 by the
+ * negative angles, which is also the gradient of the rotation. x and out are moc_rows
+ * of H heads; they may be the same tensor (same data and strides), but not overlap otherwise.
+ */
+int moc_rope(int32_t B, int32_t N, int32_t H, int32_t d, int dtype, const moc_rows *x, const moc_rope_plan *rope,
+             int32_t inverse, const moc_rows *out, void *stream);
+
+/*
+ * Cross attention to an encoder's states of another length:
+ *   o_i = softmax(q_i K_R^T * softmax_scale) V_R,  lse_i = log sum_t exp(logit_it).
+ *   q          DEVICE in [B,H,N,d];  k, v DEVICE in [B,Hk,M,d]; Hk divides H, query head h
+ *              reads key head h / (H / Hk).
+ *   S, q_offsets  the stream is cut into S segments (shots): segment s is the queries
+ *              [q_offsets[s], q_offsets[s+1]). HOST [S+1], never decreasing, from 0 to N; a segment may be
+ *              empty. NULL: one segment (S must be 1). 1 <= S <= MOC_MAX_CROSS_SEGMENTS.
+ *   kv_ranges  DEVICE [B][S][2] int32 or NULL: the queries of segment s in sample b attend the
+ *              states [first, end) of their sample, clipped to [0, M]. Valid lengths of a
+ *              padded batch are ranges (0, length), captions of shots one range a shot; ranges may
+ *              overlap. NULL: all M states. Where a range is empty (end <= first) o = 0,
+ *              lse = -infinity and no gradient arises. States outside every range are never
+ *              used, whatever they hold; their dk and dv are 0.
+ *   o DEVICE out [B,H,N,d];  lse DEVICE out [B,H,N] float.
+ * MOC_BF16: products on bf16 matrix cores, softmax and sums in float, probabilities and dS rounded to
+ * bf16 for the second products. MOC_F32: everything in float, the products on float matrix cores (unlike
+ * moc_attn_*). softmax_scale finite and > 0. B * H <= 65535, N, M < 2^26, B * H * N and B * Hk * M < 2^31.
+ *
+ * moc_cross_attn_bwd: dq [B,H,N,d], dk, dv [B,Hk,M,d] (fully overwritten; dk and dv are summed over the
+ * query heads of a key head) from the forward's o and lse and d_o [B,H,N,d]. Every sum has a fixed order: same
+ * input, same bits. workspace: moc_cross_attn_workspace_bytes(..., with_bwd) bytes, which
+ * serve both calls; nothing is kept in it between calls. No call allocates or waits, so they
+ * can be captured into a HIP graph.
+ */
+#define MOC_MAX_CROSS_SEGMENTS 128
+int moc_cross_attn_workspace_bytes(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t d, int32_t S, int dtype,
+                                   int with_bwd, size_t *bytes);
+int moc_cross_attn_fwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t d, int dtype, const void *q,
+                       const void *k, const void *v, int32_t S, const int32_t *q_offsets, const int32_t *kv_ranges,
+                       float softmax_scale, void *o, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+int moc_cross_attn_bwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t d, int dtype, const void *q,
+                       const void *k, const void *v, const void *o, const float *lse, const void *d_o, int32_t S,
+                       const int32_t *q_offsets, const int32_t *kv_ranges, float softmax_scale, void *dq, void *dk,
+                       void *dv, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Per-kernel timing (measurement aid, not part of the layer). While enabled,

@@ -26,6 +26,8 @@ SYMBOLS = ["moc_status_string", "moc_last_error", "moc_chunk_meta", "moc_meta_de
            "moc_route_workspace_bytes", "moc_route", "moc_route_static", "moc_route_fused", "moc_route_fused_status", "moc_route_perturbed", "moc_outer_workspace_bytes", "moc_outer_route",
            "moc_outer_segments", "moc_reduce_layout", "moc_gather_rows", "moc_attn_workspace_bytes", "moc_attn_fwd",
            "moc_attn_bwd", "moc_attn_bwd_after_fwd",
+           "moc_qk_norm_rope", "moc_qk_norm_rope_workspace_bytes", "moc_qk_norm_rope_bwd", "moc_rope",
+           "moc_cross_attn_workspace_bytes", "moc_cross_attn_fwd", "moc_cross_attn_bwd",
            "moc_prof_enable", "moc_prof_read", "moc_probe"]
 
 
@@ -74,6 +76,16 @@ def lib():
     l.moc_outer_route.argtypes = [i32, i32, C.c_int, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp, C.POINTER(i32),
                                   vp, sz, vp]
     l.moc_gather_rows.argtypes = [i32, i32, i32, vp, i32, vp, vp, vp, sz, vp]
+    l.moc_qk_norm_rope.argtypes = [i32, i32, i32, i32, i32, C.c_int, vp, vp, vp, vp, vp, C.c_float, vp, vp, vp, vp, vp]
+    l.moc_qk_norm_rope_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, C.c_int, C.POINTER(sz)]
+    l.moc_qk_norm_rope_bwd.argtypes = [i32, i32, i32, i32, i32, C.c_int, vp, vp, vp, vp, C.c_float, vp, vp, vp, vp,
+                                       vp, vp, vp, vp, vp, vp, sz, vp]
+    l.moc_rope.argtypes = [i32, i32, i32, i32, C.c_int, vp, vp, i32, vp, vp]
+    l.moc_cross_attn_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, i32, C.c_int, C.c_int, C.POINTER(sz)]
+    l.moc_cross_attn_fwd.argtypes = [i32, i32, i32, i32, i32, i32, C.c_int, vp, vp, vp, i32, vp, vp, C.c_float, vp, vp,
+                                     vp, sz, vp]
+    l.moc_cross_attn_bwd.argtypes = [i32, i32, i32, i32, i32, i32, C.c_int, vp, vp, vp, vp, vp, vp, i32, vp, vp,
+                                     C.c_float, vp, vp, vp, vp, sz, vp]
     l.moc_probe.argtypes = [i32, vp, sz, i32, vp, C.POINTER(C.c_float), C.POINTER(C.c_double)]
     l.moc_prof_enable.argtypes = [C.c_int]
     l.moc_prof_read.argtypes = [i32, C.c_char_p, sz, C.POINTER(i32), C.POINTER(C.c_float)]
@@ -381,3 +393,253 @@ def reduce_layout(offsets, shot, window, text_spans, seg_offsets, kept):
                                    C.byref(oC), C.byref(oT), ranges.ctypes.data), "moc_reduce_layout")
     return (o_off[:oC.value + 1].copy(), o_shot[:oC.value].copy(), o_win[:oC.value].copy(),
             o_spans[:oT.value].copy(), ranges[:len(kp)].copy())
+
+
+# ---- around the layer: head norms with rotation, cross attention ----------------------------------------------------
+
+MOC_MAX_AXES = 4
+MOC_MAX_CROSS_SEGMENTS = 128
+
+
+class _Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_h", C.c_int64), ("stride_n", C.c_int64)]
+
+
+class _RopePlan(C.Structure):
+    _fields_ = [("positions", C.c_void_p), ("freq", C.c_void_p), ("n_axes", C.c_int32),
+                ("axis_pairs", C.c_int32 * MOC_MAX_AXES), ("halves", C.c_int32)]
+
+
+class RopePlan:
+    """How tokens are turned (moc_rope_plan); owns the positions [N, axes] int32 and the frequencies on the device."""
+
+    def __init__(self, positions: torch.Tensor, axis_pairs, freq: torch.Tensor, halves: bool):
+        self.positions, self.freq, self.axis_pairs, self.halves = positions, freq, list(axis_pairs), bool(halves)
+        self.N = positions.shape[0]
+        self.struct = _RopePlan(positions.data_ptr(), freq.data_ptr(), positions.shape[1],
+                                (C.c_int32 * MOC_MAX_AXES)(*self.axis_pairs), int(self.halves))
+
+
+def rope_plan(positions: torch.Tensor, axis_pairs, freq=None, base: float = 10000.0, halves: bool = False) -> RopePlan:
+    """positions [N, axes] int32 (device); axis_pairs: pairs of features each axis turns; freq: angle of every pair per
+    unit of position (default: pair i of an axis of n pairs turns by base ** (-i / n)); halves: pairs are (j, j + d/2)
+    instead of (2j, 2j + 1)."""
+    if positions.dtype != torch.int32 or positions.dim() != 2 or not positions.is_contiguous():
+        raise ValueError("positions must be a contiguous int32 tensor [N, axes]")
+    axis_pairs = [int(n) for n in axis_pairs]
+    if len(axis_pairs) != positions.shape[1] or not 1 <= len(axis_pairs) <= MOC_MAX_AXES or min(axis_pairs) < 0:
+        raise ValueError(f"axis_pairs must name the pairs of each of 1 to {MOC_MAX_AXES} axes")
+    if freq is None:
+        freq = np.concatenate([float(base) ** (-np.arange(n) / max(n, 1)) for n in axis_pairs])
+    if not torch.is_tensor(freq):
+        freq = torch.from_numpy(np.ascontiguousarray(freq, dtype=np.float64))
+    freq = freq.to(device=positions.device, dtype=torch.float64).contiguous()
+    if freq.numel() != sum(axis_pairs):
+        raise ValueError("freq must hold a value for every pair of axis_pairs")
+    return RopePlan(positions, axis_pairs, freq, halves)
+
+
+def _same_device(first: torch.Tensor, *others):
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError("tensors must be on one device")
+    return torch.cuda.device(first.device)
+
+
+def _rows(t: Optional[torch.Tensor], token_major: bool):
+    """moc_rows of a [B, N, heads, d] (token_major) or [B, heads, N, d] tensor; None stays None."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dim() != 4 or t.stride(3) != 1:
+        raise ValueError("tensors must be 4-dimensional CUDA tensors with contiguous features")
+    n, h = (1, 2) if token_major else (2, 1)
+    return _Rows(t.data_ptr(), t.stride(0), t.stride(h), t.stride(n))
+
+
+def _ref(s):
+    return None if s is None else C.byref(s)
+
+
+def _same_dtype(first: torch.Tensor, *others):
+    for t in others:
+        if t is not None and t.dtype != first.dtype:
+            raise TypeError("tensors must have one dtype")
+    return _dtype_code(first)
+
+
+def _weight(w: Optional[torch.Tensor], d: int):
+    if w is not None and not (w.is_cuda and w.is_contiguous() and w.dtype == torch.float32 and w.numel() == d):
+        raise ValueError("weights must be contiguous float32 CUDA tensors of d values")
+    return w
+
+
+def _token_shape(q, k, v):
+    """B, N, H, Hk, d of token-major projections, any of which may be None."""
+    some = [t for t in (q, k, v) if t is not None]
+    if not some:
+        raise ValueError("q, k and v are all None")
+    B, N, _, d = some[0].shape
+    Hk = (k if k is not None else v).shape[2] if k is not None or v is not None else 1
+    for t, heads in ((q, None), (k, Hk), (v, Hk)):
+        if t is not None and (t.shape[0], t.shape[1], t.shape[3]) != (B, N, d) or t is not None and heads not in (None, t.shape[2]):
+            raise ValueError("q, k and v must be [B, N, heads, d] of one B, N and d, k and v of as many heads")
+    return B, N, q.shape[2] if q is not None else Hk, Hk, d
+
+
+def _plan(rope: Optional[RopePlan], N: int, device):
+    if rope is None:
+        return None
+    if rope.N != N:
+        raise ValueError(f"tensor has N={N}, positions have N={rope.N}")
+    if rope.positions.device != device:
+        raise ValueError("tensors must be on one device")
+    return rope.struct
+
+
+def qk_norm_rope(q, k=None, v=None, q_weight=None, k_weight=None, rope: Optional[RopePlan] = None, eps: float = 1e-6, out=None):
+    """RMS norm of every head of q and k and the rotation by `rope` (None: not turned), from token-major projections
+    [B, N, heads, d] (any strides) to contiguous head-major [B, heads, N, d]; v is moved as it is. Any of q, k, v may be
+    None. -> (q, k, v), None where the input is None. `out`: the three tensors to fill."""
+    B, N, H, Hk, d = _token_shape(q, k, v)
+    some = q if q is not None else k if k is not None else v
+    dt = _same_dtype(some, q, k, v)
+    rq, rk, rv = (_rows(t, True) for t in (q, k, v))
+    with _same_device(some, q, k, v, q_weight, k_weight):
+        if out is None:
+            out = tuple(None if t is None else torch.empty(B, t.shape[2], N, d, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        else:
+            _need_like([(o, None if t is None else (B, t.shape[2], N, d)) for o, t in zip(out, (q, k, v))], some)
+        plan = _plan(rope, N, some.device)
+        _check(lib().moc_qk_norm_rope(B, N, H, Hk, d, dt, _ref(rq), _ref(rk), _ref(rv), _ptr(_weight(q_weight, d)),
+                                      _ptr(_weight(k_weight, d)), float(eps), _ref(plan), *(_ptr(t) for t in out), _stream()),
+               "moc_qk_norm_rope")
+    return tuple(out)
+
+
+def _need_like(pairs, like: torch.Tensor):
+    """Contiguous tensors of the shapes, of `like`'s dtype and device; None for None."""
+    for t, shape in pairs:
+        if (t is None) != (shape is None):
+            raise ValueError("a tensor is missing, or one was given that belongs to none")
+        if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != like.dtype or t.device != like.device
+                              or not t.is_contiguous()):
+            raise ValueError(f"need a contiguous {like.dtype} tensor {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+
+
+def qk_norm_rope_workspace(B: int, N: int, H: int, Hk: int, d: int, dtype: torch.dtype, device="cuda") -> torch.Tensor:
+    nbytes = C.c_size_t()
+    _check(lib().moc_qk_norm_rope_workspace_bytes(B, N, H, Hk, d, MOC_BF16 if dtype == torch.bfloat16 else MOC_F32,
+                                                  C.byref(nbytes)), "moc_qk_norm_rope_workspace_bytes")
+    return torch.empty(max(nbytes.value, 16), dtype=torch.uint8, device=device)
+
+
+def qk_norm_rope_bwd(q, k, d_q_out, d_k_out, d_v_out=None, q_weight=None, k_weight=None, rope: Optional[RopePlan] = None,
+                     eps: float = 1e-6, out=None, workspace: Optional[torch.Tensor] = None):
+    """Gradients of qk_norm_rope from those of its outputs (contiguous [B, heads, N, d]) and its inputs q and k
+    -> dq, dk, dv (token-major [B, N, heads, d]) and dq_weight, dk_weight ([d] float32); None where nothing was given.
+    `out` = (dq, dk, dv) tensors to fill, of any strides."""
+    d_v_tokens = None if d_v_out is None else d_v_out.transpose(1, 2)
+    B, N, H, Hk, d = _token_shape(q, k, d_v_tokens)
+    grads = (d_q_out, d_k_out, d_v_out)
+    some = next(t for t in (q, k, d_v_out) if t is not None)
+    dt = _same_dtype(some, q, k, *grads)
+    _need_like([(g, None if t is None else (B, t.shape[2], N, d)) for g, t in zip(grads, (q, k, d_v_tokens))], some)
+    with _same_device(some, q, k, *grads, q_weight, k_weight, workspace):
+        if out is None:
+            out = tuple(None if g is None else torch.empty(B, N, g.shape[1], d, dtype=g.dtype, device=g.device) for g in grads)
+        for o, g in zip(out, grads):
+            if (o is None) != (g is None) or (o is not None and (tuple(o.shape) != (B, N, g.shape[1], d) or o.dtype != g.dtype
+                                                                or o.device != g.device)):
+                raise ValueError("out must be the gradients [B, N, heads, d] of the inputs")
+        dqw = None if q is None else torch.empty(d, dtype=torch.float32, device=some.device)
+        dkw = None if k is None else torch.empty(d, dtype=torch.float32, device=some.device)
+        ws = workspace if workspace is not None else qk_norm_rope_workspace(B, N, H, Hk, d, some.dtype, some.device)
+        rows = [_rows(t, True) for t in (q, k, *out)]
+        plan = _plan(rope, N, some.device)
+        _check(lib().moc_qk_norm_rope_bwd(B, N, H, Hk, d, dt, _ref(rows[0]), _ref(rows[1]), _ptr(_weight(q_weight, d)),
+                                          _ptr(_weight(k_weight, d)), float(eps), _ref(plan), *(_ptr(g) for g in grads),
+                                          *(_ref(r) for r in rows[2:]), _ptr(dqw), _ptr(dkw), _ptr(ws), ws.numel(), _stream()),
+               "moc_qk_norm_rope_bwd")
+    return (*out, dqw, dkw)
+
+
+def apply_rope(x: torch.Tensor, rope: RopePlan, inverse: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rotation of x [B, heads, N, d] (any strides, contiguous features); inverse: by the negative angles, the gradient of
+    the rotation. `out` may be x itself (in place) or a tensor of any strides; without it the result is contiguous."""
+    rx = _rows(x, False)
+    B, H, N, d = x.shape
+    with _same_device(x, out):
+        if out is None:
+            out = torch.empty(B, H, N, d, dtype=x.dtype, device=x.device)
+        elif out.shape != x.shape or out.dtype != x.dtype:
+            raise ValueError("out must have the shape and dtype of x")
+        ro = _rows(out, False)
+        _check(lib().moc_rope(B, N, H, d, _dtype_code(x), _ref(rx), _ref(_plan(rope, N, x.device)), int(bool(inverse)),
+                              _ref(ro), _stream()), "moc_rope")
+    return out
+
+
+def _cross_shape(q, k, v, kv_ranges, q_offsets):
+    if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[3]:
+        raise ValueError("need q [B, H, N, d] and k, v [B, Hk, M, d]")
+    _need_contig(q, k, v, kv_ranges)
+    (B, H, N, d), (Hk, M) = q.shape, k.shape[1:3]
+    off = None if q_offsets is None else _i32(q_offsets)
+    S = 1 if off is None else off.shape[0] - 1
+    if kv_ranges is not None and (kv_ranges.dtype != torch.int32 or tuple(kv_ranges.shape) != (B, S, 2)):
+        raise ValueError(f"kv_ranges must be an int32 tensor {(B, S, 2)}")
+    return B, H, Hk, N, M, d, S, off
+
+
+def cross_attn_workspace(B: int, H: int, Hk: int, N: int, M: int, d: int, dtype: torch.dtype, with_bwd: bool,
+                         segments: int = 1, device="cuda") -> torch.Tensor:
+    nbytes = C.c_size_t()
+    _check(lib().moc_cross_attn_workspace_bytes(B, H, Hk, N, M, d, segments, MOC_BF16 if dtype == torch.bfloat16 else MOC_F32,
+                                                int(with_bwd), C.byref(nbytes)), "moc_cross_attn_workspace_bytes")
+    return torch.empty(max(nbytes.value, 16), dtype=torch.uint8, device=device)
+
+
+def cross_attn_fwd(q, k, v, kv_ranges: Optional[torch.Tensor] = None, q_offsets=None, scale: Optional[float] = None,
+                   workspace: Optional[torch.Tensor] = None, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
+    """Attention of q [B, H, N, d] to encoder states k, v [B, Hk, M, d] -> o [B, H, N, d], lse [B, H, N] fp32.
+    q_offsets [S+1] (host) cuts the queries into segments, kv_ranges [B, S, 2] int32 (device) says which states
+    [first, end) a segment of a sample attends; an empty range gives o = 0, lse = -inf."""
+    B, H, Hk, N, M, d, S, off = _cross_shape(q, k, v, kv_ranges, q_offsets)
+    dt = _same_dtype(q, k, v)
+    with _same_device(q, k, v, kv_ranges, workspace):
+        scale = float(d ** -0.5 if scale is None else scale)
+        ws = workspace if workspace is not None else cross_attn_workspace(B, H, Hk, N, M, d, q.dtype, False, S, q.device)
+        if out is None:
+            out = torch.empty_like(q), torch.empty(B, H, N, dtype=torch.float32, device=q.device)
+        else:
+            _need_like([(out[0], q.shape)], q)
+            _need_lse(out[1], q)
+        _check(lib().moc_cross_attn_fwd(B, H, Hk, N, M, d, dt, _ptr(q), _ptr(k), _ptr(v), S,
+                                        None if off is None else off.ctypes.data, _ptr(kv_ranges), scale, _ptr(out[0]),
+                                        _ptr(out[1]), _ptr(ws), ws.numel(), _stream()), "moc_cross_attn_fwd")
+    return tuple(out)
+
+
+def _need_lse(lse, q):
+    if tuple(lse.shape) != tuple(q.shape[:3]) or lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous float32 tensor [B, H, N]")
+
+
+def cross_attn_bwd(q, k, v, o, lse, d_o, kv_ranges: Optional[torch.Tensor] = None, q_offsets=None, scale: Optional[float] = None,
+                   workspace: Optional[torch.Tensor] = None, out=None):
+    """-> dq [B, H, N, d], dk, dv [B, Hk, M, d] from the forward's o and lse and the gradient d_o of o."""
+    B, H, Hk, N, M, d, S, off = _cross_shape(q, k, v, kv_ranges, q_offsets)
+    dt = _same_dtype(q, k, v, o, d_o)
+    _need_like([(o, q.shape), (d_o, q.shape)], q)
+    _need_lse(lse, q)
+    with _same_device(q, k, v, kv_ranges, workspace):
+        scale = float(d ** -0.5 if scale is None else scale)
+        ws = workspace if workspace is not None else cross_attn_workspace(B, H, Hk, N, M, d, q.dtype, True, S, q.device)
+        if out is None:
+            out = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+        else:
+            _need_like([(out[0], q.shape), (out[1], k.shape), (out[2], v.shape)], q)
+        _check(lib().moc_cross_attn_bwd(B, H, Hk, N, M, d, dt, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o), S,
+                                        None if off is None else off.ctypes.data, _ptr(kv_ranges), scale,
+                                        *(_ptr(t) for t in out), _ptr(ws), ws.numel(), _stream()), "moc_cross_attn_bwd")
+    return tuple(out)

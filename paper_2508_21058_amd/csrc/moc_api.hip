@@ -12,6 +12,7 @@
 #include <unordered_set>
 #include <vector>
 
+#include "moc_block.h"
 #include "moc_internal.h"
 
 namespace {
@@ -896,6 +897,270 @@ int moc_attn_bwd_after_fwd(const moc_meta *meta, int32_t B, int32_t H, int32_t d
                            void *workspace, size_t workspace_bytes, void *stream) {
     return attn_bwd_impl(meta, B, H, d, dtype, q, k, v, o, lse, d_o, sel, topk, softmax_scale, dq, dk, dv, workspace,
                          workspace_bytes, stream, true);
+}
+
+namespace {
+
+int check_heads(int32_t B, int32_t N, int32_t H, int32_t d, int dtype) {
+    if (dtype != MOC_BF16 && dtype != MOC_F32) return fail(MOC_ERR_DTYPE, "dtype must be MOC_BF16 or MOC_F32");
+    if (B <= 0 || N <= 0 || H <= 0) return fail(MOC_ERR_SHAPE, "B, N and the heads must be positive");
+    if (d != 64 && d != 128) return fail(MOC_ERR_SHAPE, "d must be 64 or 128");
+    if ((long long)B * N >= (1LL << 31) || (long long)B * N * H >= (1LL << 31)) return fail(MOC_ERR_SHAPE, "B * heads * N must be < 2^31");
+    return MOC_OK;
+}
+
+// A strided tensor for the row kernels; strides of dimensions of one element do not matter.
+int check_rows(const moc_rows *r, int32_t B, int32_t N, int32_t H, int dtype, long long *sb, long long *sh, long long *sn) {
+    if (!r->data) return fail(MOC_ERR_NULL, "moc_rows without data");
+    const int per16 = dtype == MOC_F32 ? 4 : 8;
+    *sb = B > 1 ? r->stride_b : 0;
+    *sh = H > 1 ? r->stride_h : 0;
+    *sn = N > 1 ? r->stride_n : 0;
+    if (misaligned(r->data) || *sb % per16 != 0 || *sh % per16 != 0 || *sn % per16 != 0)
+        return fail(MOC_ERR_ALIGN, "rows must be 16-byte aligned: data and every stride");
+    return MOC_OK;
+}
+
+int check_rope(const moc_rope_plan *p, int32_t d, moc::RowArgs &a) {
+    if (!p->positions || !p->freq) return fail(MOC_ERR_NULL, "positions or freq is NULL");
+    if ((reinterpret_cast<uintptr_t>(p->positions) & 3u) || (reinterpret_cast<uintptr_t>(p->freq) & 7u))
+        return fail(MOC_ERR_ALIGN, "positions must be 4-byte and freq 8-byte aligned");
+    if (p->n_axes < 1 || p->n_axes > MOC_MAX_AXES) return fail(MOC_ERR_SHAPE, "need 1 <= n_axes <= MOC_MAX_AXES");
+    int at = 0;
+    for (int x = 0; x < p->n_axes; ++x) {
+        if (p->axis_pairs[x] < 0 || p->axis_pairs[x] > d / 2 - at) return fail(MOC_ERR_SHAPE, "axis_pairs must be >= 0 and at most d/2 together");
+        at += p->axis_pairs[x];
+        a.axis_end[x] = at;
+    }
+    a.positions = p->positions;
+    a.freq = p->freq;
+    a.n_axes = p->n_axes;
+    return MOC_OK;
+}
+
+// The output of the forward (and the gradient of it): contiguous [B, heads, N, d].
+void head_major(moc::HeadPart &p, void *out, int32_t N, int32_t d) {
+    p.out = out;
+    p.o_n = d;
+    p.o_h = (long long)N * d;
+    p.o_b = p.o_h * p.heads;
+}
+
+int check_cross(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t d, int32_t S, int dtype) {
+    if (dtype != MOC_BF16 && dtype != MOC_F32) return fail(MOC_ERR_DTYPE, "dtype must be MOC_BF16 or MOC_F32");
+    if (B <= 0 || H <= 0 || Hk <= 0 || N <= 0 || M <= 0) return fail(MOC_ERR_SHAPE, "B, H, Hk, N and M must be positive");
+    if (H % Hk != 0) return fail(MOC_ERR_SHAPE, "Hk must divide H");
+    if (d != 64 && d != 128) return fail(MOC_ERR_SHAPE, "d must be 64 or 128");
+    if (S < 1 || S > MOC_MAX_CROSS_SEGMENTS) return fail(MOC_ERR_SHAPE, "need 1 <= S <= MOC_MAX_CROSS_SEGMENTS");
+    if ((long long)B * H > 65535) return fail(MOC_ERR_SHAPE, "B * H must be <= 65535");
+    if (N >= (1 << 26) || M >= (1 << 26)) return fail(MOC_ERR_SHAPE, "N and M must be < 2^26");
+    if ((long long)B * H * N >= (1LL << 31) || (long long)B * Hk * M >= (1LL << 31))
+        return fail(MOC_ERR_SHAPE, "B * H * N and B * Hk * M must be < 2^31");
+    return MOC_OK;
+}
+
+// The parts of a call that both directions share.
+int cross_args(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t d, int32_t S, const int32_t *q_offsets,
+               const int32_t *kv_ranges, float scale, moc::CrossArgs &a) {
+    if (bad_scale(scale)) return fail(MOC_ERR_SHAPE, "softmax_scale must be finite and positive");
+    if (!q_offsets && S != 1) return fail(MOC_ERR_NULL, "q_offsets is NULL with S > 1");
+    if (q_offsets) {
+        if (q_offsets[0] != 0 || q_offsets[S] != N) return fail(MOC_ERR_OFFSETS, "q_offsets must run from 0 to N");
+        for (int s = 0; s < S; ++s)
+            if (q_offsets[s + 1] < q_offsets[s]) return fail(MOC_ERR_OFFSETS, "q_offsets must not decrease");
+    }
+    if (reinterpret_cast<uintptr_t>(kv_ranges) & 7u) return fail(MOC_ERR_ALIGN, "kv_ranges must be 8-byte aligned");
+    a.ranges = reinterpret_cast<const moc::CrossRange *>(kv_ranges);
+    a.rows = (long long)B * H * N;
+    a.M = M;
+    a.n_seg = S;
+    a.Hk = Hk;
+    a.BHk = B * Hk;
+    a.scale = scale;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    // One segment: the query heads of a key head lie behind each other and are walked as one long head.
+    a.copies = S == 1 ? 1 : H / Hk;
+    a.N = S == 1 ? N * (H / Hk) : N;
+    for (int s = 0; s <= S; ++s) a.q_off[s] = S == 1 ? s * a.N : q_offsets[s];
+    a.tiles = 0;
+    for (int s = 0; s < S; ++s) {
+        a.tile_at[s] = a.tiles;
+        a.tiles += (a.q_off[s + 1] - a.q_off[s] + 127) / 128;
+    }
+    a.tile_at[S] = a.tiles;
+    return MOC_OK;
+}
+
+}  // namespace
+
+int moc_qk_norm_rope(int32_t B, int32_t N, int32_t H, int32_t Hk, int32_t d, int dtype, const moc_rows *q, const moc_rows *k,
+                     const moc_rows *v, const float *q_weight, const float *k_weight, float eps, const moc_rope_plan *rope,
+                     void *q_out, void *k_out, void *v_out, void *stream) {
+    int rc = check_heads(B, N, H, d, dtype);
+    if (!rc) rc = check_heads(B, N, Hk, d, dtype);
+    if (rc) return rc;
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(MOC_ERR_SHAPE, "eps must be finite and >= 0");
+    if (!q && !k && !v) return fail(MOC_ERR_NULL, "q, k and v are all NULL");
+    const moc_rows *in[3] = {q, k, v};
+    void *out[3] = {q_out, k_out, v_out};
+    moc::RowArgs a{};
+    a.N = N;
+    a.n_tokens = B * N;
+    a.eps = eps;
+    a.sign = 1.f;
+    for (int p = 0; p < 3; ++p) {
+        if (!in[p] != !out[p]) return fail(MOC_ERR_NULL, "an input without its output, or an output without its input");
+        if (!in[p]) continue;
+        moc::HeadPart &hp = a.part[p];
+        hp.heads = p ? Hk : H;
+        rc = check_rows(in[p], B, N, hp.heads, dtype, &hp.x_b, &hp.x_h, &hp.x_n);
+        if (rc) return rc;
+        if (misaligned(out[p])) return fail(MOC_ERR_ALIGN, "device pointers must be 16-byte aligned");
+        hp.x = in[p]->data;
+        head_major(hp, out[p], N, d);
+        a.heads_total += hp.heads;
+    }
+    if (misaligned(q_weight) || misaligned(k_weight)) return fail(MOC_ERR_ALIGN, "device pointers must be 16-byte aligned");
+    a.part[0].weight = q_weight;
+    a.part[1].weight = k_weight;
+    if (rope && (rc = check_rope(rope, d, a))) return rc;
+    const hipError_t e = moc::launch_rows(a, B, d, dtype, true, rope && rope->halves, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? MOC_OK : hip_fail(e, "head norm kernel");
+}
+
+int moc_qk_norm_rope_workspace_bytes(int32_t B, int32_t N, int32_t H, int32_t Hk, int32_t d, int dtype, size_t *bytes) {
+    if (!bytes) return fail(MOC_ERR_NULL, "bytes is NULL");
+    int rc = check_heads(B, N, H, d, dtype);
+    if (!rc) rc = check_heads(B, N, Hk, d, dtype);
+    if (rc) return rc;
+    *bytes = moc::rows_partial_bytes(d);
+    return MOC_OK;
+}
+
+int moc_qk_norm_rope_bwd(int32_t B, int32_t N, int32_t H, int32_t Hk, int32_t d, int dtype, const moc_rows *q, const moc_rows *k,
+                         const float *q_weight, const float *k_weight, float eps, const moc_rope_plan *rope, const void *d_q_out,
+                         const void *d_k_out, const void *d_v_out, const moc_rows *dq, const moc_rows *dk, const moc_rows *dv,
+                         float *dq_weight, float *dk_weight, void *workspace, size_t workspace_bytes, void *stream) {
+    int rc = check_heads(B, N, H, d, dtype);
+    if (!rc) rc = check_heads(B, N, Hk, d, dtype);
+    if (rc) return rc;
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(MOC_ERR_SHAPE, "eps must be finite and >= 0");
+    if (!d_q_out && !d_k_out && !d_v_out) return fail(MOC_ERR_NULL, "no gradient was given");
+    const moc_rows *in[3] = {q, k, nullptr}, *out[3] = {dq, dk, dv};
+    const void *grad[3] = {d_q_out, d_k_out, d_v_out};
+    moc::RowArgs a{};
+    a.N = N;
+    a.n_tokens = B * N;
+    a.eps = eps;
+    a.sign = 1.f;
+    for (int p = 0; p < 3; ++p) {
+        if (!grad[p] != !out[p] || (p < 2 && !grad[p] != !in[p]))
+            return fail(MOC_ERR_NULL, "q, its output's gradient and dq go together, and so for k and v");
+        if (!grad[p]) continue;
+        moc::HeadPart &hp = a.part[p];
+        hp.heads = p ? Hk : H;
+        if (in[p]) {
+            rc = check_rows(in[p], B, N, hp.heads, dtype, &hp.x_b, &hp.x_h, &hp.x_n);
+            if (rc) return rc;
+            hp.x = in[p]->data;
+        }
+        rc = check_rows(out[p], B, N, hp.heads, dtype, &hp.o_b, &hp.o_h, &hp.o_n);
+        if (rc) return rc;
+        if (misaligned(grad[p])) return fail(MOC_ERR_ALIGN, "device pointers must be 16-byte aligned");
+        hp.g = grad[p];
+        hp.out = out[p]->data;
+        a.heads_total += hp.heads;
+    }
+    if ((dq_weight && !q) || (dk_weight && !k)) return fail(MOC_ERR_NULL, "a weight's gradient without its input");
+    if (misaligned(q_weight) || misaligned(k_weight) || misaligned(dq_weight) || misaligned(dk_weight))
+        return fail(MOC_ERR_ALIGN, "device pointers must be 16-byte aligned");
+    a.part[0].weight = q_weight;
+    a.part[1].weight = k_weight;
+    if (rope && (rc = check_rope(rope, d, a))) return rc;
+    if (!workspace || workspace_bytes < moc::rows_partial_bytes(d)) return fail(MOC_ERR_WORKSPACE, "head norm workspace too small");
+    if (misaligned(workspace)) return fail(MOC_ERR_ALIGN, "workspace must be 16-byte aligned");
+    a.partial = static_cast<float *>(workspace);
+    const hipError_t e = moc::launch_rows_bwd(a, B, d, dtype, rope && rope->halves, dq_weight, dk_weight, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? MOC_OK : hip_fail(e, "head norm backward kernels");
+}
+
+int moc_rope(int32_t B, int32_t N, int32_t H, int32_t d, int dtype, const moc_rows *x, const moc_rope_plan *rope, int32_t inverse,
+             const moc_rows *out, void *stream) {
+    int rc = check_heads(B, N, H, d, dtype);
+    if (rc) return rc;
+    if (!x || !out || !rope) return fail(MOC_ERR_NULL, "x, out or rope is NULL");
+    moc::RowArgs a{};
+    moc::HeadPart &hp = a.part[0];
+    rc = check_rows(x, B, N, H, dtype, &hp.x_b, &hp.x_h, &hp.x_n);
+    if (!rc) rc = check_rows(out, B, N, H, dtype, &hp.o_b, &hp.o_h, &hp.o_n);
+    if (!rc) rc = check_rope(rope, d, a);
+    if (rc) return rc;
+    hp.x = x->data;
+    hp.out = out->data;
+    hp.heads = a.heads_total = H;
+    a.N = N;
+    a.n_tokens = B * N;
+    a.sign = inverse ? -1.f : 1.f;
+    const hipError_t e = moc::launch_rows(a, B, d, dtype, false, rope->halves, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? MOC_OK : hip_fail(e, "rotation kernel");
+}
+
+int moc_cross_attn_workspace_bytes(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t d, int32_t S, int dtype, int with_bwd,
+                                   size_t *bytes) {
+    if (!bytes) return fail(MOC_ERR_NULL, "bytes is NULL");
+    const int rc = check_cross(B, H, Hk, N, M, d, S, dtype);
+    if (rc) return rc;
+    *bytes = moc::cross_plan(B, H, Hk, N, M, d, S, with_bwd != 0).total;
+    return MOC_OK;
+}
+
+int moc_cross_attn_fwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t d, int dtype, const void *q, const void *k,
+                       const void *v, int32_t S, const int32_t *q_offsets, const int32_t *kv_ranges, float softmax_scale, void *o,
+                       float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    int rc = check_cross(B, H, Hk, N, M, d, S, dtype);
+    if (rc) return rc;
+    if (!q || !k || !v || !o || !lse) return fail(MOC_ERR_NULL, "a tensor pointer is NULL");
+    if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(o) || misaligned(lse))
+        return fail(MOC_ERR_ALIGN, "device pointers must be 16-byte aligned");
+    moc::CrossArgs a{};
+    rc = cross_args(B, H, Hk, N, M, d, S, q_offsets, kv_ranges, softmax_scale, a);
+    if (rc) return rc;
+    const moc::CrossPlan p = moc::cross_plan(B, H, Hk, N, M, d, S, false);
+    if (p.total > 0 && (!workspace || workspace_bytes < p.total)) return fail(MOC_ERR_WORKSPACE, "cross attention workspace too small");
+    if (misaligned(workspace)) return fail(MOC_ERR_ALIGN, "workspace must be 16-byte aligned");
+    char *ws = static_cast<char *>(workspace);
+    a.q = q; a.k = k; a.v = v; a.o = o; a.lse = lse;
+    a.split = p.split_fwd;
+    a.part = reinterpret_cast<float *>(ws + p.part);
+    a.part_lse = reinterpret_cast<float *>(ws + p.part_lse);
+    const hipError_t e = moc::launch_cross_fwd(a, d, dtype, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? MOC_OK : hip_fail(e, "cross attention forward kernels");
+}
+
+int moc_cross_attn_bwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t d, int dtype, const void *q, const void *k,
+                       const void *v, const void *o, const float *lse, const void *d_o, int32_t S, const int32_t *q_offsets,
+                       const int32_t *kv_ranges, float softmax_scale, void *dq, void *dk, void *dv, void *workspace,
+                       size_t workspace_bytes, void *stream) {
+    int rc = check_cross(B, H, Hk, N, M, d, S, dtype);
+    if (rc) return rc;
+    if (!q || !k || !v || !o || !lse || !d_o || !dq || !dk || !dv) return fail(MOC_ERR_NULL, "a tensor pointer is NULL");
+    if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(o) || misaligned(lse) || misaligned(d_o) || misaligned(dq) ||
+        misaligned(dk) || misaligned(dv))
+        return fail(MOC_ERR_ALIGN, "device pointers must be 16-byte aligned");
+    moc::CrossArgs a{};
+    rc = cross_args(B, H, Hk, N, M, d, S, q_offsets, kv_ranges, softmax_scale, a);
+    if (rc) return rc;
+    const moc::CrossPlan p = moc::cross_plan(B, H, Hk, N, M, d, S, true);
+    if (!workspace || workspace_bytes < p.total) return fail(MOC_ERR_WORKSPACE, "cross attention workspace too small (with_bwd)");
+    if (misaligned(workspace)) return fail(MOC_ERR_ALIGN, "workspace must be 16-byte aligned");
+    char *ws = static_cast<char *>(workspace);
+    a.q = q; a.k = k; a.v = v; a.o_in = o; a.lse_in = lse; a.d_o = d_o;
+    a.dq = dq; a.dk = dk; a.dv = dv;
+    a.stats = reinterpret_cast<float *>(ws + p.stats);
+    a.part = reinterpret_cast<float *>(ws + p.part);
+    a.kpart = reinterpret_cast<float *>(ws + p.kpart);
+    const hipError_t e = moc::launch_cross_bwd(a, p, d, dtype, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? MOC_OK : hip_fail(e, "cross attention backward kernels");
 }
 
 }  // extern "C"

@@ -1,0 +1,149 @@
+// Tiles and work items shared by the cross attention kernels.
+#pragma once
+#include "moc_attn_common.h"
+#include "moc_block.h"
+
+namespace moc {
+
+constexpr int kCrossRows = 128;      // queries of a workgroup in the query-stationary passes: four waves of 32
+constexpr int kCrossKeys = 128;      // states of a workgroup in the key-stationary pass: four waves of 32
+
+// What the kernels need of a storage type: T = bf16 runs on 32x32x16 matrix instructions, T = float on 32x32x2 ones. A tile in
+// LDS is row-major without padding, its 16-byte groups XOR-swizzled by the row (SwTile for bf16).
+//   frag(tile, row0, s)      row operand: rows row0 .. row0 + 31, features of step s
+//   tfrag(tile, row0, b, s)  transposed operand: feature block b (32), rows of step s behind row0
+//   pack(acc, s)             a step of rows of an accumulator as the other operand of a product with tfrag
+//   mma                      the product of one step
+// KS: steps of a row's features. RS: steps of 32 rows.
+template <int D, typename T> struct Ops;
+template <int D> struct Ops<D, bf16_t> {
+    typedef bf16x8 Frag;
+    static constexpr int KS = D / 16, RS = 2, RB = D * 2;
+    LaneOffs<D> lo;
+    __device__ __forceinline__ void init(int lane) { lo.init(lane); }
+    __device__ __forceinline__ Frag frag(const char *tile, int row0, int s) const {
+        return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(tile + lo.row[s] + row0 * RB));
+    }
+    __device__ __forceinline__ Frag tfrag(const char *tile, int row0, int b, int s) const {
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const char *p = tile + (row0 + 16 * s) * RB;
+        s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + lo.tr[2 * b]));
+        s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + lo.tr[2 * b + 1]));
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        s16x8 r = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+        return __builtin_bit_cast(bf16x8, r);
+    }
+    static __device__ __forceinline__ Frag pack(const f32x16 &acc, int s) { return acc_to_frag(acc, s); }
+    static __device__ __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) { return mfma32(a, b, c); }
+    // the same operand of a row in memory
+    static __device__ __forceinline__ Frag row_frag(const bf16_t *row, int s, int half) { return Io<bf16_t>::load8(row + 16 * s + 8 * half); }
+    static __device__ __forceinline__ float dot(Frag a, Frag b) {
+        const u32x4 x = __builtin_bit_cast(u32x4, a), y = __builtin_bit_cast(u32x4, b);
+        float r = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r = fmaf(bf16_lo(x[i]), bf16_lo(y[i]), fmaf(bf16_hi(x[i]), bf16_hi(y[i]), r));
+        return r;
+    }
+    static __device__ __forceinline__ int swizzle(int row) { return SwTile<D>::sw(row); }
+};
+template <int D> struct Ops<D, float> {
+    typedef f32x4 Frag;
+    static constexpr int KS = D / 8, RS = 4, RB = D * 4;
+    int l32, half;
+    __device__ __forceinline__ void init(int lane) { l32 = lane & 31; half = lane >> 5; }
+    static __device__ __forceinline__ int swizzle(int row) { return row & 15; }
+    // step s: features 8 s + 4 half .. + 4, one for each of four matrix instructions
+    __device__ __forceinline__ Frag frag(const char *tile, int row0, int s) const {
+        return *reinterpret_cast<const f32x4 *>(tile + (row0 + l32) * RB + (((2 * s + half) ^ (l32 & 15)) << 4));
+    }
+    // rows 8 s + 4 half + e, the rows of accumulator registers 4 s + e
+    __device__ __forceinline__ Frag tfrag(const char *tile, int row0, int b, int s) const {
+        f32x4 r;
+        const int f = 32 * b + l32;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int row = row0 + 8 * s + 4 * half + e;
+            r[e] = *reinterpret_cast<const float *>(tile + row * RB + (((f >> 2) ^ (row & 15)) << 4) + (f & 3) * 4);
+        }
+        return r;
+    }
+    static __device__ __forceinline__ Frag pack(const f32x16 &acc, int s) { return f32x4{acc[4 * s], acc[4 * s + 1], acc[4 * s + 2], acc[4 * s + 3]}; }
+    static __device__ __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+    static __device__ __forceinline__ Frag row_frag(const float *row, int s, int half) { return *reinterpret_cast<const f32x4 *>(row + 8 * s + 4 * half); }
+    static __device__ __forceinline__ float dot(Frag a, Frag b) { return fmaf(a[0], b[0], fmaf(a[1], b[1], fmaf(a[2], b[2], a[3] * b[3]))); }
+};
+
+// A wave's share of the asynchronous copy of `valid` rows (the others repeat the last of them) to a tile of ROWS rows; the base is
+// in scalar registers that a vector instruction may just have written, hence the wait states in front of the load.
+__device__ __forceinline__ void cross_copy16(const void *base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1"
+                 :: "v"(off), "s"(uniform_ptr(base)), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
+}
+template <int D, typename T, int ROWS, int NW = 4>
+__device__ __forceinline__ void copy_tile(const T *first, int valid, char *tile, int wave, int lane) {
+    constexpr int RB = D * (int)sizeof(T), GR = RB / 16, RPI = 64 / GR, NI = ROWS / RPI;
+    static_assert(NI % NW == 0, "rows divide evenly among the waves");
+    const uint32_t at = lds_address(tile);
+#pragma unroll
+    for (int p = 0; p < NI / NW; ++p) {
+        const int n = wave + NW * p, row = n * RPI + lane / GR;
+        const uint32_t off = (uint32_t)min(row, valid - 1) * RB + (((lane % GR) ^ Ops<D, T>::swizzle(row)) << 4);
+        cross_copy16(first, off, at + n * 1024);
+    }
+}
+
+// Work item of the query-stationary passes: up to kCrossRows queries of one segment of one query head.
+struct CrossItem {
+    int bhk, count, first, end;      // key head of all samples, queries, range of states
+    long long row;                   // first query in [B * H * N]
+};
+__device__ __forceinline__ CrossRange cross_range(const CrossArgs &a, int b, int s) {
+    CrossRange r = {0, a.M};
+    if (a.ranges) {
+        r = a.ranges[(size_t)b * a.n_seg + s];
+        r.first = max(r.first, 0);
+        r.end = min(r.end, a.M);
+    }
+    return r;
+}
+__device__ __forceinline__ CrossItem cross_item(const CrossArgs &a, int logical) {
+    CrossItem it;
+    const int per_head = a.tiles * a.copies;
+    it.bhk = logical / per_head;
+    const int rest = logical - it.bhk * per_head, copy = rest / a.tiles, t = rest - copy * a.tiles;
+    int s = 0, hi = a.n_seg;                                   // the last segment with tile_at <= t
+    while (hi - s > 1) {
+        const int mid = (s + hi) >> 1;
+        if (a.tile_at[mid] <= t) s = mid; else hi = mid;
+    }
+    const int q = a.q_off[s] + (t - a.tile_at[s]) * kCrossRows;
+    it.count = min(kCrossRows, a.q_off[s + 1] - q);
+    it.row = ((long long)it.bhk * a.copies + copy) * a.N + q;
+    const CrossRange r = cross_range(a, it.bhk / a.Hk, s);
+    it.first = __builtin_amdgcn_readfirstlane(r.first);
+    it.end = __builtin_amdgcn_readfirstlane(r.end);
+    return it;
+}
+// The part of a range that split z of n takes, whole tiles of `tile` states.
+__device__ __forceinline__ void cross_slice(int &first, int &end, int z, int n, int tile) {
+    if (n == 1 || end <= first) return;
+    const int tiles = (end - first + tile - 1) / tile, f = first;
+    first = min(end, f + (int)((long long)tiles * z / n) * tile);
+    end = min(end, f + (int)((long long)tiles * (z + 1) / n) * tile);
+}
+
+// A wave's 32 x D transposed accumulator (lane: row l32, four-feature pieces) times `scale` to the float rows at `out`.
+template <int D> __device__ __forceinline__ void store_rows_f32(const f32x16 *acc, float scale, float *row, int half) {
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            Io<float>::store4(row + b * 32 + g * 8 + half * 4, acc[b][4 * g] * scale, acc[b][4 * g + 1] * scale, acc[b][4 * g + 2] * scale,
+                              acc[b][4 * g + 3] * scale);
+}
+
+}  // namespace moc

@@ -1,0 +1,315 @@
+// Cross attention backward.
+//   delta_i = dO_i . o_i,  P_it = exp(scale q_i.k_t - lse_i),  dS_it = P_it (dO_i.v_t - delta_i)
+//   dQ_i = scale sum_t dS_it k_t,  dV_t = sum_i P_it dO_i,  dK_t = scale sum_i dS_it q_i
+//
+// Two passes without atomics: dQ over the queries, as the forward goes (it forms delta on its way in and leaves the
+// statistics), then dK and dV over the states: a workgroup owns 128 states of a key head and streams the queries of every segment whose
+// range meets them, 32 at a time, of all the query heads that share the key head. The states are few and the queries many, so the
+// queries of a tile of states are split over workgroups, whose sums a last launch adds in a fixed order.
+#include "moc_cross.h"
+
+namespace moc {
+
+template <int D, typename T>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void cross_dq_kernel(CrossArgs a) {
+    typedef Ops<D, T> O;
+    constexpr int BN = sizeof(T) == 2 ? 64 : 32, DB = D / 32;
+    constexpr int TB = BN * O::RB;
+    __shared__ __attribute__((aligned(1024))) char smem[4 * TB];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
+    int logical;
+    if (!xcd_remap((long long)a.tiles * a.copies * a.BHk * a.split, logical)) return;
+    const int z = logical % a.split;
+    CrossItem it = cross_item(a, logical / a.split);
+    cross_slice(it.first, it.end, z, a.split, BN);
+    const int r = wave * 32 + l32, rc = min(r, it.count - 1);
+    const bool row_valid = r < it.count;
+    const size_t row = (size_t)it.row + rc;
+    typename O::Frag qf[O::KS], dof[O::KS];
+    float delta = 0.f;
+    {
+        const T *qrow = static_cast<const T *>(a.q) + row * D, *dorow = static_cast<const T *>(a.d_o) + row * D;
+        const T *orow = static_cast<const T *>(a.o_in) + row * D;
+#pragma unroll
+        for (int s = 0; s < O::KS; ++s) {
+            qf[s] = O::row_frag(qrow, s, half);
+            dof[s] = O::row_frag(dorow, s, half);
+            delta += O::dot(dof[s], O::row_frag(orow, s, half));
+        }
+        delta = xhalf_sum(delta);
+    }
+    const float lse2 = a.lse_in[row] * kLog2e, c = a.scale_log2;
+    if (z == 0 && row_valid && half == 0) *reinterpret_cast<f32x2 *>(a.stats + 2 * row) = f32x2{lse2, delta};
+    f32x16 dq[DB];
+#pragma unroll
+    for (int b = 0; b < DB; ++b) dq[b] = zero16();
+    if (it.first < it.end) {
+        const T *kb = static_cast<const T *>(a.k) + (size_t)it.bhk * a.M * D, *vb = static_cast<const T *>(a.v) + (size_t)it.bhk * a.M * D;
+        O ops;
+        ops.init(lane);
+        auto issue = [&](int pos, int buf) {
+            const int valid = min(BN, it.end - pos);
+            copy_tile<D, T, BN>(kb + (size_t)pos * D, valid, smem + buf * 2 * TB, wave, lane);
+            copy_tile<D, T, BN>(vb + (size_t)pos * D, valid, smem + buf * 2 * TB + TB, wave, lane);
+        };
+        issue(it.first, 0);
+        int buf = 0;
+        for (int pos = it.first; pos < it.end; pos += BN, buf ^= 1) {
+            wait_vmcnt<0>();
+            __syncthreads();
+            if (pos + BN < it.end) issue(pos + BN, buf ^ 1);
+            if (wave * 32 >= it.count) continue;
+            const char *kt = smem + buf * 2 * TB, *vt = kt + TB;
+            const int valid = it.end - pos;
+#pragma unroll
+            for (int k32 = 0; k32 < BN; k32 += 32) {
+                if (k32 >= valid) break;
+                f32x16 s = zero16(), dp = zero16();
+#pragma unroll
+                for (int i = 0; i < O::KS; ++i) s = O::mma(ops.frag(kt, k32, i), qf[i], s);
+#pragma unroll
+                for (int i = 0; i < O::KS; ++i) dp = O::mma(ops.frag(vt, k32, i), dof[i], dp);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse2));
+                    s[i] = k32 + (i >> 2) * 8 + half * 4 + (i & 3) < valid ? p * (dp[i] - delta) : 0.f;
+                }
+#pragma unroll
+                for (int ks = 0; ks < O::RS; ++ks) {
+                    const typename O::Frag f = O::pack(s, ks);
+#pragma unroll
+                    for (int b = 0; b < DB; ++b) dq[b] = O::mma(ops.tfrag(kt, k32, b, ks), f, dq[b]);
+                }
+            }
+        }
+    }
+    if (a.split > 1) {
+        if (row_valid) store_rows_f32<D>(dq, a.scale, a.part + ((size_t)z * a.rows + row) * D, half);
+    } else if constexpr (sizeof(T) == 4) {
+        if (row_valid) store_rows_f32<D>(dq, a.scale, static_cast<float *>(a.dq) + row * D, half);
+    } else {
+        __syncthreads();
+        store_rows_bf16<D>(smem, wave, lane, dq, a.scale, row_valid ? r : -1, static_cast<bf16_t *>(a.dq) + (size_t)it.row * D);
+    }
+}
+
+// The queries that a tile of states streams: the segments whose ranges meet it, cut into tiles of 32.
+struct CrossStream {
+    int n, seg[MOC_MAX_CROSS_SEGMENTS], tile_at[MOC_MAX_CROSS_SEGMENTS + 1], first[MOC_MAX_CROSS_SEGMENTS], end[MOC_MAX_CROSS_SEGMENTS];
+};
+constexpr int kStreamRows = 32;
+// (the first wave; a barrier before anyone else reads it)
+__device__ __forceinline__ void make_stream(const CrossArgs &a, int b, int key0, int key1, CrossStream &s, int lane) {
+    int n = 0, at = 0;
+    for (int s0 = 0; s0 < a.n_seg; s0 += 64) {
+        const int i = s0 + lane;
+        CrossRange r = {0, 0};
+        int tiles = 0;
+        if (i < a.n_seg) {
+            r = cross_range(a, b, i);
+            if (max(r.first, key0) < min(r.end, key1)) tiles = (a.q_off[i + 1] - a.q_off[i] + kStreamRows - 1) / kStreamRows;
+        }
+        int sum = tiles;
+#pragma unroll
+        for (int w = 1; w < 64; w <<= 1) {
+            const int o = __shfl_up(sum, w, 64);
+            if (lane >= w) sum += o;
+        }
+        const unsigned long long have = __ballot(tiles > 0);
+        if (tiles > 0) {
+            const int j = n + __popcll(have & ((1ull << lane) - 1));
+            s.seg[j] = i;
+            s.tile_at[j] = at + sum - tiles;
+            s.first[j] = r.first;
+            s.end[j] = r.end;
+        }
+        n += __popcll(have);
+        at += __shfl(sum, 63, 64);
+    }
+    if (lane == 0) { s.n = n; s.tile_at[n] = at; }
+}
+
+template <int D, typename T>
+__global__ __launch_bounds__(256, 1) void cross_dkdv_kernel(CrossArgs a) {
+    typedef Ops<D, T> O;
+    constexpr int DB = D / 32, TB = kStreamRows * O::RB;
+    __shared__ __attribute__((aligned(1024))) char smem[4 * TB];          // Q, dO, twice
+    __shared__ __attribute__((aligned(16))) float stat[2][2 * kStreamRows];
+    __shared__ CrossStream cs;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
+    const int ktiles = (a.M + kCrossKeys - 1) / kCrossKeys;
+    int logical;
+    if (!xcd_remap((long long)ktiles * a.BHk * a.split, logical)) return;
+    const int bhk = logical / (ktiles * a.split), rest = logical - bhk * ktiles * a.split;      // tiles of states that stream the
+    const int z = rest / ktiles, key0 = (rest - z * ktiles) * kCrossKeys;                       // same queries are neighbours
+    if (wave == 0) make_stream(a, bhk / a.Hk, key0, min(key0 + kCrossKeys, a.M), cs, lane);
+    __syncthreads();
+    const int per_copy = __builtin_amdgcn_readfirstlane(cs.tile_at[cs.n]);
+    const long long total = (long long)per_copy * a.copies;
+    const int t0 = (int)(total * z / a.split), t1 = (int)(total * (z + 1) / a.split);
+    const int key = key0 + wave * 32 + l32, keyc = min(key, a.M - 1);
+    const bool active = key0 + wave * 32 < a.M;
+    typename O::Frag kf[O::KS], vf[O::KS];
+    {
+        const size_t krow = ((size_t)bhk * a.M + keyc) * D;
+#pragma unroll
+        for (int s = 0; s < O::KS; ++s) {
+            kf[s] = O::row_frag(static_cast<const T *>(a.k) + krow, s, half);
+            vf[s] = O::row_frag(static_cast<const T *>(a.v) + krow, s, half);
+        }
+    }
+    f32x16 dk[DB], dv[DB];
+#pragma unroll
+    for (int b = 0; b < DB; ++b) { dk[b] = zero16(); dv[b] = zero16(); }
+    O ops;
+    ops.init(lane);
+    const float c = a.scale_log2;
+    // the next tile to copy: query head `copy` of the group, entry si of the stream, tile u of the copy
+    int copy = 0, u = 0, si = 0;
+    if (t0 < t1) {
+        copy = t0 / per_copy;
+        u = t0 - copy * per_copy;
+        while (cs.tile_at[si + 1] <= u) ++si;
+    }
+    auto issue = [&](int buf) {
+        const int seg = __builtin_amdgcn_readfirstlane(cs.seg[si]), q = a.q_off[seg] + (u - __builtin_amdgcn_readfirstlane(cs.tile_at[si])) * kStreamRows;
+        const int valid = min(kStreamRows, a.q_off[seg + 1] - q);
+        const size_t row = ((size_t)bhk * a.copies + copy) * a.N + q;
+        copy_tile<D, T, kStreamRows>(static_cast<const T *>(a.q) + row * D, valid, smem + buf * 2 * TB, wave, lane);
+        copy_tile<D, T, kStreamRows>(static_cast<const T *>(a.d_o) + row * D, valid, smem + buf * 2 * TB + TB, wave, lane);
+        if (wave == 0)       // rows past the segment get (+inf, 0): no probability
+            async_copy4_at(a.stats + 2 * (lane / 2 < valid ? row + lane / 2 : (size_t)a.rows) + (lane & 1), lds_address(stat[buf]));
+    };
+    if (t0 < t1) issue(0);
+    int buf = 0;
+    for (int t = t0; t < t1; ++t, buf ^= 1) {
+        wait_vmcnt<0>();
+        __syncthreads();
+        const int first = __builtin_amdgcn_readfirstlane(cs.first[si]), end = __builtin_amdgcn_readfirstlane(cs.end[si]);
+        if (++u == cs.tile_at[si + 1]) {
+            if (++si == cs.n) { si = 0; u = 0; ++copy; }
+        }
+        if (t + 1 < t1) issue(buf ^ 1);
+        const int kw = key0 + wave * 32;
+        if (!active || first >= kw + 32 || end <= kw) continue;
+        const bool ok = key >= first && key < end;
+        const char *qt = smem + buf * 2 * TB, *dot = qt + TB;
+        f32x16 s = zero16(), dp = zero16();
+#pragma unroll
+        for (int i = 0; i < O::KS; ++i) s = O::mma(ops.frag(qt, 0, i), kf[i], s);
+#pragma unroll
+        for (int i = 0; i < O::KS; ++i) dp = O::mma(ops.frag(dot, 0, i), vf[i], dp);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 st0 = *reinterpret_cast<const f32x4 *>(&stat[buf][2 * (g * 8 + half * 4)]);
+            const f32x4 st1 = *reinterpret_cast<const f32x4 *>(&stat[buf][2 * (g * 8 + half * 4) + 4]);
+            const float l2[4] = {st0[0], st0[2], st1[0], st1[2]}, dl[4] = {st0[1], st0[3], st1[1], st1[3]};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 4 * g + e;
+                const float p = ok ? __builtin_amdgcn_exp2f(fmaf(s[i], c, -l2[e])) : 0.f;
+                s[i] = p;
+                dp[i] = ok ? p * (dp[i] - dl[e]) : 0.f;
+            }
+        }
+#pragma unroll
+        for (int ks = 0; ks < O::RS; ++ks) {
+            const typename O::Frag pf = O::pack(s, ks), df = O::pack(dp, ks);
+#pragma unroll
+            for (int b = 0; b < DB; ++b) {
+                dv[b] = O::mma(ops.tfrag(dot, 0, b, ks), pf, dv[b]);
+                dk[b] = O::mma(ops.tfrag(qt, 0, b, ks), df, dk[b]);
+            }
+        }
+    }
+    if (key >= a.M) return;
+    const size_t krow = (size_t)bhk * a.M + key;
+    if (a.split > 1) {
+        float *p = a.kpart + (((size_t)z * a.BHk * a.M) + krow) * 2 * D;
+        store_rows_f32<D>(dk, a.scale, p, half);
+        store_rows_f32<D>(dv, 1.f, p + D, half);
+    } else {
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const size_t at = krow * D + b * 32 + g * 8 + half * 4;
+                Io<T>::store4(static_cast<T *>(a.dk) + at, dk[b][4 * g] * a.scale, dk[b][4 * g + 1] * a.scale, dk[b][4 * g + 2] * a.scale,
+                              dk[b][4 * g + 3] * a.scale);
+                Io<T>::store4(static_cast<T *>(a.dv) + at, dv[b][4 * g], dv[b][4 * g + 1], dv[b][4 * g + 2], dv[b][4 * g + 3]);
+            }
+    }
+}
+
+// out = sum of the splits' rows in their order: dQ (one output of n words of four features) or dK and dV (rows of two)
+template <int D, typename T>
+__global__ __launch_bounds__(256) void cross_sum_kernel(const float *__restrict__ part, int split, long long rows, T *out0, T *out1) {
+    constexpr int W = D / 4;
+    const long long words = rows * W * (out1 ? 2 : 1), i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= words) return;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    for (int z = 0; z < split; ++z) s += *reinterpret_cast<const f32x4 *>(part + (z * words + i) * 4);
+    const long long row = out1 ? i / (2 * W) : i / W;
+    const int x = (int)(out1 ? i % (2 * W) : i % W);
+    T *out = x < W ? out0 : out1;
+    Io<T>::store4(out + row * D + (x % W) * 4, s[0], s[1], s[2], s[3]);
+}
+
+// the statistics of the rows that pad a ragged tile of queries
+__global__ void cross_pad_kernel(float *stats) { stats[threadIdx.x] = threadIdx.x ? 0.f : INFINITY; }
+
+template <int D, typename T> static void bwd_dispatch(CrossArgs a, const CrossPlan &p, hipStream_t st) {
+    cross_pad_kernel<<<1, 2, 0, st>>>(a.stats + 2 * a.rows);
+    a.split = p.split_dq;
+    {
+        MOC_PROF("cross_dq", st);
+        cross_dq_kernel<D, T><<<xcd_grid((long long)a.tiles * a.copies * a.BHk * a.split), 256, 0, st>>>(a);
+    }
+    if (a.split > 1) {
+        MOC_PROF("cross_sum", st);
+        cross_sum_kernel<D, T><<<(unsigned)((a.rows * (D / 4) + 255) / 256), 256, 0, st>>>(a.part, a.split, a.rows, static_cast<T *>(a.dq),
+                                                                                        static_cast<T *>(nullptr));
+    }
+    a.split = p.split_kv;
+    const long long states = (long long)a.BHk * a.M;
+    {
+        MOC_PROF("cross_dkdv", st);
+        cross_dkdv_kernel<D, T><<<xcd_grid((long long)((a.M + kCrossKeys - 1) / kCrossKeys) * a.BHk * a.split), 256, 0, st>>>(a);
+    }
+    if (a.split > 1) {
+        MOC_PROF("cross_sum", st);
+        cross_sum_kernel<D, T><<<(unsigned)((states * 2 * (D / 4) + 255) / 256), 256, 0, st>>>(a.kpart, a.split, states, static_cast<T *>(a.dk),
+                                                                                             static_cast<T *>(a.dv));
+    }
+}
+
+hipError_t launch_cross_bwd(CrossArgs a, const CrossPlan &p, int d, int dtype, hipStream_t st) {
+    if (d == 128 && dtype == MOC_BF16) bwd_dispatch<128, bf16_t>(a, p, st);
+    else if (d == 128) bwd_dispatch<128, float>(a, p, st);
+    else if (dtype == MOC_BF16) bwd_dispatch<64, bf16_t>(a, p, st);
+    else bwd_dispatch<64, float>(a, p, st);
+    return hipGetLastError();
+}
+
+// ---- how a call is cut ----------------------------------------------------------------------------
+CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, bool with_bwd) {
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    CrossPlan p;
+    const long long items = S == 1 ? (long long)B * Hk * (((long long)N * (H / Hk) + kCrossRows - 1) / kCrossRows)
+                                   : (long long)B * H * ((N + kCrossRows - 1) / kCrossRows + S - 1);
+    auto split = [](long long n, long long most) { return n >= 512 ? 1 : (int)std::max(1LL, std::min((511 + n) / n, most)); };
+    p.split_fwd = p.split_dq = split(items, (M + 255) / 256);
+    const long long rows = (long long)B * H * N, states = (long long)B * Hk * M;
+    const long long kitems = (long long)B * Hk * ((M + kCrossKeys - 1) / kCrossKeys);
+    p.split_kv = split(kitems, ((long long)N * (H / Hk) + 511) / 512);
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t x = at; at += up(bytes); return x; };
+    p.part = take(p.split_fwd > 1 ? (size_t)p.split_fwd * rows * d * 4 : 0);
+    p.part_lse = take(p.split_fwd > 1 ? (size_t)p.split_fwd * rows * 4 : 0);
+    p.stats = take(with_bwd ? (size_t)(rows + 1) * 8 : 0);
+    p.kpart = take(with_bwd && p.split_kv > 1 ? (size_t)p.split_kv * states * 2 * d * 4 : 0);
+    p.total = at;
+    return p;
+}
+
+}  // namespace moc

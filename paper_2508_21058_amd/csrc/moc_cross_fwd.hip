@@ -1,0 +1,154 @@
+// Cross attention forward: o = softmax(q K^T scale) V over the range of encoder states that a query's segment attends.
+//
+// One pass with a running maximum and sum. A workgroup owns 128 queries, four waves of 32, and streams the range's states through LDS in
+// double-buffered tiles. S^T = K Q^T and O^T = V^T P^T, so that a lane owns a query: its statistics are scalars and the scores feed the second
+// product from the registers they are in. Calls of few query tiles split the range over workgroups, whose results a second launch joins.
+#include "moc_cross.h"
+
+namespace moc {
+
+template <int D, typename T>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void cross_fwd_kernel(CrossArgs a) {
+    typedef Ops<D, T> O;
+    constexpr int BN = sizeof(T) == 2 ? 64 : 32, DB = D / 32;
+    constexpr int TB = BN * O::RB;
+    __shared__ __attribute__((aligned(1024))) char smem[4 * TB];      // K, V, twice
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
+    int logical;
+    if (!xcd_remap((long long)a.tiles * a.copies * a.BHk * a.split, logical)) return;
+    const int z = logical % a.split;
+    CrossItem it = cross_item(a, logical / a.split);
+    cross_slice(it.first, it.end, z, a.split, BN);
+    const int r = wave * 32 + l32, rc = min(r, it.count - 1);
+    const bool row_valid = r < it.count;
+    const size_t row = (size_t)it.row + rc;
+    T *out = static_cast<T *>(a.o) + row * D;
+    float *pout = a.split > 1 ? a.part + ((size_t)z * a.rows + row) * D : nullptr;
+    float *lout = a.split > 1 ? a.part_lse + (size_t)z * a.rows + row : a.lse + row;
+    f32x16 oacc[DB];
+#pragma unroll
+    for (int b = 0; b < DB; ++b) oacc[b] = zero16();
+    float m_run = -INFINITY, l_run = 0.f;
+    if (it.first < it.end) {
+        const T *kb = static_cast<const T *>(a.k) + (size_t)it.bhk * a.M * D, *vb = static_cast<const T *>(a.v) + (size_t)it.bhk * a.M * D;
+        const T *qrow = static_cast<const T *>(a.q) + row * D;
+        typename O::Frag qf[O::KS];
+#pragma unroll
+        for (int s = 0; s < O::KS; ++s) qf[s] = O::row_frag(qrow, s, half);
+        O ops;
+        ops.init(lane);
+        const float c = a.scale_log2;
+        auto issue = [&](int pos, int buf) {
+            const int valid = min(BN, it.end - pos);
+            copy_tile<D, T, BN>(kb + (size_t)pos * D, valid, smem + buf * 2 * TB, wave, lane);
+            copy_tile<D, T, BN>(vb + (size_t)pos * D, valid, smem + buf * 2 * TB + TB, wave, lane);
+        };
+        issue(it.first, 0);
+        int buf = 0;
+        for (int pos = it.first; pos < it.end; pos += BN, buf ^= 1) {
+            wait_vmcnt<0>();
+            __syncthreads();
+            if (pos + BN < it.end) issue(pos + BN, buf ^ 1);
+            if (wave * 32 >= it.count) continue;
+            const char *kt = smem + buf * 2 * TB, *vt = kt + TB;
+            const int valid = it.end - pos;
+#pragma unroll
+            for (int kb32 = 0; kb32 < BN; kb32 += 32) {
+                if (kb32 >= valid) break;
+                f32x16 s = zero16();
+#pragma unroll
+                for (int i = 0; i < O::KS; ++i) s = O::mma(ops.frag(kt, kb32, i), qf[i], s);
+                if (valid < kb32 + 32) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (kb32 + (i >> 2) * 8 + half * 4 + (i & 3) >= valid) s[i] = -INFINITY;
+                }
+                float mx = s[0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+                const float m_new = fmaxf(m_run, xhalf_max(mx));
+                if (__any((m_new - m_run) * c > 8.f)) {      // moved, and the sums rescaled, only when it has grown by 2^8
+                    const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * c);
+                    l_run *= alpha;
+#pragma unroll
+                    for (int b = 0; b < DB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) oacc[b][i] *= alpha;
+                    m_run = m_new;
+                }
+                const float mc = m_run * c;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -mc));
+                    l_run += s[i];
+                }
+#pragma unroll
+                for (int ks = 0; ks < O::RS; ++ks) {
+                    const typename O::Frag pf = O::pack(s, ks);
+#pragma unroll
+                    for (int b = 0; b < DB; ++b) oacc[b] = O::mma(ops.tfrag(vt, kb32, b, ks), pf, oacc[b]);
+                }
+            }
+        }
+    }
+    const float l = xhalf_sum(l_run);
+    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;      // nothing attended: o = 0, lse = -inf
+    const float lse = l > 0.f || l != l ? m_run * a.scale + logf(l) : -INFINITY;
+    if (row_valid && half == 0) *lout = lse;
+    if (a.split > 1) {
+        if (row_valid) store_rows_f32<D>(oacc, inv, pout, half);
+    } else if constexpr (sizeof(T) == 4) {
+        if (row_valid) store_rows_f32<D>(oacc, inv, out, half);
+    } else {
+        __syncthreads();
+        store_rows_bf16<D>(smem, wave, lane, oacc, inv, row_valid ? r : -1, static_cast<bf16_t *>(a.o) + (size_t)it.row * D);
+    }
+}
+
+// Joins the results of split calls: lse = log sum_z exp(lse_z), o = sum_z exp(lse_z - lse) o_z, in the order of the splits.
+template <int D, typename T> __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
+    constexpr int LPR = D / 4;
+    const long long row = (long long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+    const int c = threadIdx.x % LPR * 4;
+    if (row >= a.rows) return;
+    float mx = -INFINITY;
+    bool bad = false;
+    for (int z = 0; z < a.split; ++z) {
+        const float x = a.part_lse[(size_t)z * a.rows + row];
+        mx = fmaxf(mx, x);
+        bad |= x != x;
+    }
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    if (mx > -INFINITY || bad)
+        for (int z = 0; z < a.split; ++z) {
+            const float w = expf(a.part_lse[(size_t)z * a.rows + row] - mx);
+            sum += w;
+            o += w * *reinterpret_cast<const f32x4 *>(a.part + ((size_t)z * a.rows + row) * D + c);
+        }
+    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+    Io<T>::store4(static_cast<T *>(a.o) + row * D + c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    if (c == 0) a.lse[row] = sum > 0.f || sum != sum ? mx + logf(sum) : -INFINITY;
+}
+
+template <int D, typename T> static void fwd_dispatch(const CrossArgs &a, hipStream_t st) {
+    {
+        MOC_PROF("cross_fwd", st);
+        cross_fwd_kernel<D, T><<<xcd_grid((long long)a.tiles * a.copies * a.BHk * a.split), 256, 0, st>>>(a);
+    }
+    if (a.split > 1) {
+        constexpr int rows = 256 / (D / 4);
+        MOC_PROF("cross_join", st);
+        cross_join_kernel<D, T><<<(unsigned)((a.rows + rows - 1) / rows), 256, 0, st>>>(a);
+    }
+}
+
+hipError_t launch_cross_fwd(const CrossArgs &a, int d, int dtype, hipStream_t st) {
+    if (d == 128 && dtype == MOC_BF16) fwd_dispatch<128, bf16_t>(a, st);
+    else if (d == 128) fwd_dispatch<128, float>(a, st);
+    else if (dtype == MOC_BF16) fwd_dispatch<64, bf16_t>(a, st);
+    else fwd_dispatch<64, float>(a, st);
+    return hipGetLastError();
+}
+
+}  // namespace moc
