@@ -18,12 +18,12 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(CSRC, "_build")
 LIB = os.path.join(HERE, "libmoc.so")
 UNITS = ["moc_api", "moc_pool", "moc_route", "moc_lists", "moc_attn_fwd", "moc_attn_bwd", "moc_attn_dkdv", "moc_probe", "moc_perturb", "moc_outer",
-         "moc_rope", "moc_cross_fwd", "moc_cross_bwd"]
+         "moc_rope", "moc_cross_fwd", "moc_cross_bwd", "moc_cross_dkdv"]
 # -Wno-inline-asm: the tile-copy asm lists m0 (which it sets) as clobbered; clang warns that m0 is reserved
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", "-Wno-inline-asm",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
-# matrix results in vector registers: the accumulation registers of this unit are its own (see mfma32_acc)
-UNIT_FLAGS = {"moc_attn_dkdv": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+# matrix results in vector registers: the accumulation registers of these units are their own (see mfma32_acc)
+UNIT_FLAGS = {u: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for u in ("moc_attn_dkdv", "moc_cross_dkdv")}
 
 
 def _deps():

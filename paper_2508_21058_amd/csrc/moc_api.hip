@@ -1110,7 +1110,7 @@ int moc_cross_attn_workspace_bytes(int32_t B, int32_t H, int32_t Hk, int32_t N, 
     if (!bytes) return fail(MOC_ERR_NULL, "bytes is NULL");
     const int rc = check_cross(B, H, Hk, N, M, d, S, dtype);
     if (rc) return rc;
-    *bytes = moc::cross_plan(B, H, Hk, N, M, d, S, with_bwd != 0).total;
+    *bytes = moc::cross_plan(B, H, Hk, N, M, d, S, dtype, with_bwd != 0).total;
     return MOC_OK;
 }
 
@@ -1125,7 +1125,7 @@ int moc_cross_attn_fwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, i
     moc::CrossArgs a{};
     rc = cross_args(B, H, Hk, N, M, d, S, q_offsets, kv_ranges, softmax_scale, a);
     if (rc) return rc;
-    const moc::CrossPlan p = moc::cross_plan(B, H, Hk, N, M, d, S, false);
+    const moc::CrossPlan p = moc::cross_plan(B, H, Hk, N, M, d, S, dtype, false);
     if (p.total > 0 && (!workspace || workspace_bytes < p.total)) return fail(MOC_ERR_WORKSPACE, "cross attention workspace too small");
     if (misaligned(workspace)) return fail(MOC_ERR_ALIGN, "workspace must be 16-byte aligned");
     char *ws = static_cast<char *>(workspace);
@@ -1150,7 +1150,7 @@ int moc_cross_attn_bwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, i
     moc::CrossArgs a{};
     rc = cross_args(B, H, Hk, N, M, d, S, q_offsets, kv_ranges, softmax_scale, a);
     if (rc) return rc;
-    const moc::CrossPlan p = moc::cross_plan(B, H, Hk, N, M, d, S, true);
+    const moc::CrossPlan p = moc::cross_plan(B, H, Hk, N, M, d, S, dtype, true);
     if (!workspace || workspace_bytes < p.total) return fail(MOC_ERR_WORKSPACE, "cross attention workspace too small (with_bwd)");
     if (misaligned(workspace)) return fail(MOC_ERR_ALIGN, "workspace must be 16-byte aligned");
     char *ws = static_cast<char *>(workspace);
@@ -1159,6 +1159,8 @@ int moc_cross_attn_bwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, i
     a.stats = reinterpret_cast<float *>(ws + p.stats);
     a.part = reinterpret_cast<float *>(ws + p.part);
     a.kpart = reinterpret_cast<float *>(ws + p.kpart);
+    a.items = reinterpret_cast<moc::CrossKeys *>(ws + p.items);
+    a.max_items = p.max_items;
     const hipError_t e = moc::launch_cross_bwd(a, p, d, dtype, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? MOC_OK : hip_fail(e, "cross attention backward kernels");
 }

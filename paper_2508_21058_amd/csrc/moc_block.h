@@ -35,14 +35,22 @@ hipError_t launch_rows_bwd(RowArgs a, int B, int d, int dtype, bool halves, floa
 
 // ---- cross attention ----------------------------------------------------------------------------
 struct CrossRange { int32_t first, end; };
+// A tile of states of the wide key-stationary pass and the segments that attend all of it (none: its gradients are zero). The
+// tiles of a sample cover its states once.
+struct CrossKeys {
+    int32_t start, len, pad[2];
+    uint32_t segments[MOC_MAX_CROSS_SEGMENTS / 32];
+};
 struct CrossArgs {
     const void *q, *k, *v, *o_in, *d_o;
     void *o, *dq, *dk, *dv;
     float *lse;                        // forward: out
     const float *lse_in;               // backward
-    float *stats;                      // [B * H * N + 1][2] (lse * log2 e, delta); last pair (+inf, 0)
+    float *stats;                      // [B * H * N + 1] records (lse * log2 e, delta, query of the key head << 5, 0); last one (+inf, 0, 0, 0)
     float *part, *part_lse;            // split calls: [split][B * H * N][d], [split][B * H * N]
     float *kpart;                      // split dK / dV: [split][B * Hk * M][2][d]
+    CrossKeys *items;                  // wide tiles: [B][max_items]
+    int max_items;
     const CrossRange *ranges;          // [B][n_seg] or nullptr
     long long rows;                    // B * H * N
     int N, M, n_seg;                   // tokens of a query head (all heads of a group where copies is 1 and H > Hk), states
@@ -56,10 +64,15 @@ struct CrossArgs {
 // Sizes of a call that follow from its arguments alone, and the places in its workspace (byte offsets).
 struct CrossPlan {
     int split_fwd, split_dq, split_kv;
-    size_t stats, part, part_lse, kpart, total;
+    bool wide;                         // dK and dV in tiles of 256 states (moc_cross_dkdv.hip)
+    int max_items;
+    size_t stats, part, part_lse, kpart, items, total;
 };
-CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, bool with_bwd);
+CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype, bool with_bwd);
 hipError_t launch_cross_fwd(const CrossArgs &a, int d, int dtype, hipStream_t st);
+// the records of padding rows and, of wide tiles, the items; then the tiles themselves
+void launch_cross_items(const CrossArgs &a, bool wide, int B, hipStream_t st);
+void launch_cross_dkdv_wide(const CrossArgs &a, hipStream_t st);
 hipError_t launch_cross_bwd(CrossArgs a, const CrossPlan &p, int d, int dtype, hipStream_t st);
 
 }  // namespace moc

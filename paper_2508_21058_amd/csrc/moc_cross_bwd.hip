@@ -10,6 +10,12 @@
 
 namespace moc {
 
+// What the key-stationary pass reads of a query.
+__device__ __forceinline__ void store_record(const CrossArgs &a, const CrossItem &it, size_t row, float lse2, float delta) {
+    const int word = (int)((uint32_t)(row - (size_t)it.bhk * a.copies * a.N) << 5);
+    *reinterpret_cast<f32x4 *>(a.stats + 4 * row) = f32x4{lse2, delta, __int_as_float(word), 0.f};
+}
+
 template <int D, typename T>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void cross_dq_kernel(CrossArgs a) {
     typedef Ops<D, T> O;
@@ -39,7 +45,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void cross_dq_kernel(C
         delta = xhalf_sum(delta);
     }
     const float lse2 = a.lse_in[row] * kLog2e, c = a.scale_log2;
-    if (z == 0 && row_valid && half == 0) *reinterpret_cast<f32x2 *>(a.stats + 2 * row) = f32x2{lse2, delta};
+    if (z == 0 && row_valid && half == 0) store_record(a, it, row, lse2, delta);
     f32x16 dq[DB];
 #pragma unroll
     for (int b = 0; b < DB; ++b) dq[b] = zero16();
@@ -178,7 +184,7 @@ __global__ __launch_bounds__(256, 1) void cross_dkdv_kernel(CrossArgs a) {
         copy_tile<D, T, kStreamRows>(static_cast<const T *>(a.q) + row * D, valid, smem + buf * 2 * TB, wave, lane);
         copy_tile<D, T, kStreamRows>(static_cast<const T *>(a.d_o) + row * D, valid, smem + buf * 2 * TB + TB, wave, lane);
         if (wave == 0)       // rows past the segment get (+inf, 0): no probability
-            async_copy4_at(a.stats + 2 * (lane / 2 < valid ? row + lane / 2 : (size_t)a.rows) + (lane & 1), lds_address(stat[buf]));
+            async_copy4_at(a.stats + 4 * (lane / 2 < valid ? row + lane / 2 : (size_t)a.rows) + (lane & 1), lds_address(stat[buf]));
     };
     if (t0 < t1) issue(0);
     int buf = 0;
@@ -255,11 +261,8 @@ __global__ __launch_bounds__(256) void cross_sum_kernel(const float *__restrict_
     Io<T>::store4(out + row * D + (x % W) * 4, s[0], s[1], s[2], s[3]);
 }
 
-// the statistics of the rows that pad a ragged tile of queries
-__global__ void cross_pad_kernel(float *stats) { stats[threadIdx.x] = threadIdx.x ? 0.f : INFINITY; }
-
 template <int D, typename T> static void bwd_dispatch(CrossArgs a, const CrossPlan &p, hipStream_t st) {
-    cross_pad_kernel<<<1, 2, 0, st>>>(a.stats + 2 * a.rows);
+    launch_cross_items(a, p.wide, a.BHk / a.Hk, st);
     a.split = p.split_dq;
     {
         MOC_PROF("cross_dq", st);
@@ -272,7 +275,9 @@ template <int D, typename T> static void bwd_dispatch(CrossArgs a, const CrossPl
     }
     a.split = p.split_kv;
     const long long states = (long long)a.BHk * a.M;
-    {
+    if (p.wide) {
+        launch_cross_dkdv_wide(a, st);
+    } else {
         MOC_PROF("cross_dkdv", st);
         cross_dkdv_kernel<D, T><<<xcd_grid((long long)((a.M + kCrossKeys - 1) / kCrossKeys) * a.BHk * a.split), 256, 0, st>>>(a);
     }
@@ -292,22 +297,26 @@ hipError_t launch_cross_bwd(CrossArgs a, const CrossPlan &p, int d, int dtype, h
 }
 
 // ---- how a call is cut ----------------------------------------------------------------------------
-CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, bool with_bwd) {
+CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype, bool with_bwd) {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     CrossPlan p;
     const long long items = S == 1 ? (long long)B * Hk * (((long long)N * (H / Hk) + kCrossRows - 1) / kCrossRows)
                                    : (long long)B * H * ((N + kCrossRows - 1) / kCrossRows + S - 1);
-    auto split = [](long long n, long long most) { return n >= 512 ? 1 : (int)std::max(1LL, std::min((511 + n) / n, most)); };
-    p.split_fwd = p.split_dq = split(items, (M + 255) / 256);
-    const long long rows = (long long)B * H * N, states = (long long)B * Hk * M;
-    const long long kitems = (long long)B * Hk * ((M + kCrossKeys - 1) / kCrossKeys);
-    p.split_kv = split(kitems, ((long long)N * (H / Hk) + 511) / 512);
+    auto split = [](long long n, long long want, long long most) { return n >= want ? 1 : (int)std::max(1LL, std::min((want - 1 + n) / n, most)); };
+    p.split_fwd = p.split_dq = split(items, 512, (M + 255) / 256);
+    const long long rows = (long long)B * H * N, states = (long long)B * Hk * M, per_head = (long long)N * (H / Hk);
+    // (a record holds the row of a query among those of its key head in 26 bits)
+    p.wide = d == 128 && dtype == MOC_BF16 && per_head < (1 << 26);
+    p.max_items = M / kWideTile + 2 * S + 1;
+    if (p.wide) p.split_kv = split((long long)B * Hk * ((M + kWideTile - 1) / kWideTile), 1024, (per_head + 255) / 256);
+    else p.split_kv = split((long long)B * Hk * ((M + kCrossKeys - 1) / kCrossKeys), 512, (per_head + 511) / 512);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t x = at; at += up(bytes); return x; };
     p.part = take(p.split_fwd > 1 ? (size_t)p.split_fwd * rows * d * 4 : 0);
     p.part_lse = take(p.split_fwd > 1 ? (size_t)p.split_fwd * rows * 4 : 0);
-    p.stats = take(with_bwd ? (size_t)(rows + 1) * 8 : 0);
+    p.stats = take(with_bwd ? (size_t)(rows + 1) * 16 : 0);
     p.kpart = take(with_bwd && p.split_kv > 1 ? (size_t)p.split_kv * states * 2 * d * 4 : 0);
+    p.items = take(with_bwd && p.wide ? (size_t)B * p.max_items * sizeof(CrossKeys) : 0);
     p.total = at;
     return p;
 }

@@ -1,0 +1,177 @@
+// dK / dV of cross attention on tiles of 256 states, heads of 128 features in bf16: the key-stationary pass of moc_dkdv_wide.h.
+//
+// That pass has no masks: every query of its stream attends every key of its tile. So a sample's states are cut where a range of one
+// of its segments begins or ends, and the pieces into tiles; a tile streams the queries of the segments whose ranges hold it, all of
+// them or, where the call has few tiles, one part in `split`. States of no range are tiles without segments, whose gradients are zero.
+// Ranges are on the device, so the cutting is too: a workgroup a sample, in the launch that also writes the padding record.
+#include "moc_block.h"
+#include "moc_dkdv_wide.h"
+
+namespace moc {
+
+constexpr int kCuts = 2 * MOC_MAX_CROSS_SEGMENTS + 2;
+__global__ __launch_bounds__(256) void cross_items_kernel(CrossArgs a, bool wide) {
+    const int tid = threadIdx.x, b = blockIdx.x, S = a.n_seg;
+    if (b == 0 && tid < 4) a.stats[4 * (size_t)a.rows + tid] = tid ? 0.f : INFINITY;
+    if (!wide) return;
+    __shared__ int first[MOC_MAX_CROSS_SEGMENTS], end[MOC_MAX_CROSS_SEGMENTS], cut[kCuts], sorted[kCuts], tile_at[kCuts];
+    __shared__ uint32_t segments[kCuts][MOC_MAX_CROSS_SEGMENTS / 32];
+    const int n = 2 * S + 2;
+    if (tid < S) {
+        CrossRange r = {0, a.M};
+        if (a.ranges) r = a.ranges[(size_t)b * S + tid];
+        r.first = max(r.first, 0);
+        r.end = min(r.end, a.M);
+        if (r.end <= r.first || a.q_off[tid + 1] == a.q_off[tid]) r.first = r.end = 0;
+        first[tid] = cut[2 * tid] = r.first;
+        end[tid] = cut[2 * tid + 1] = r.end;
+    }
+    if (tid == 0) { cut[n - 2] = 0; cut[n - 1] = a.M; }
+    __syncthreads();
+    for (int i = tid; i < n; i += 256) {
+        const int x = cut[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += cut[j] < x || (cut[j] == x && j < i);
+        sorted[rank] = x;
+    }
+    __syncthreads();
+    // piece i: states [sorted[i], sorted[i + 1]), its tiles from tile_at[i] on
+    for (int i = tid; i < n; i += 256) {
+        int at = 0;
+        for (int j = 0; j < i; ++j) at += (sorted[j + 1] - sorted[j] + kWideTile - 1) / kWideTile;
+        tile_at[i] = at;
+        uint32_t in[MOC_MAX_CROSS_SEGMENTS / 32] = {};
+        for (int s = 0; s < S && i + 1 < n; ++s)
+            if (first[s] <= sorted[i] && end[s] >= sorted[i + 1]) in[s >> 5] |= 1u << (s & 31);
+        for (int w = 0; w < MOC_MAX_CROSS_SEGMENTS / 32; ++w) segments[i][w] = in[w];
+    }
+    __syncthreads();
+    const int total = tile_at[n - 1];
+    CrossKeys *out = a.items + (size_t)b * a.max_items;
+    for (int t = tid; t < a.max_items; t += 256) {
+        CrossKeys k{};
+        if (t < total) {
+            int i = 0, hi = n - 1;                        // the last piece with tile_at <= t (empty pieces have the next one's)
+            while (hi - i > 1) {
+                const int mid = (i + hi) >> 1;
+                if (tile_at[mid] <= t) i = mid; else hi = mid;
+            }
+            k.start = sorted[i] + (t - tile_at[i]) * kWideTile;
+            k.len = min(kWideTile, sorted[i + 1] - k.start);
+            for (int w = 0; w < MOC_MAX_CROSS_SEGMENTS / 32; ++w) k.segments[w] = segments[i][w];
+        }
+        out[t] = k;
+    }
+}
+
+namespace wide {
+// Pieces of contiguous queries: the segments of a tile, for every query head of the group in turn, of them `stages` stages.
+struct PieceSource {
+    int n_direct, q_start, q_len;                       // the first piece, in queries of the key head
+    const CrossArgs &a;
+    const CrossKeys &keys;
+    const char *inf_rec, *records;                      // (records of the key head)
+    const char *rec_ptr;
+    int first, rec_left, copy, seg, stages;             // of the piece: its first query and queries left; stages left behind it
+    __device__ __forceinline__ PieceSource(const CrossArgs &args, const CrossKeys &k) : a(args), keys(k) {}
+    __device__ __forceinline__ static int stages_of(const CrossArgs &a, int s) { return (a.q_off[s + 1] - a.q_off[s] + R - 1) / R; }
+    __device__ __forceinline__ int next_segment(int s) const {      // the first segment of the tile from s on, or n_seg
+        for (; s < a.n_seg; ++s)
+            if (keys.segments[s >> 5] >> (s & 31) & 1u) break;
+        return s;
+    }
+    // the piece at (copy, seg) from its stage `skip` on
+    __device__ __forceinline__ void enter(int skip) {
+        first = copy * a.N + a.q_off[seg] + skip * R;
+        rec_left = a.q_off[seg + 1] - a.q_off[seg] - skip * R;
+        const int n = (rec_left + R - 1) / R;
+        if (n > stages) rec_left = stages * R;
+        stages -= min(n, stages);
+        rec_ptr = records + (size_t)first * 16;
+    }
+    __device__ __forceinline__ void advance() {
+        seg = next_segment(seg + 1);
+        if (seg == a.n_seg) { ++copy; seg = next_segment(0); }
+        enter(0);
+    }
+    __device__ __forceinline__ void issue(uint32_t dst, uint32_t rec_off, int rec_row, int rec_sel) {
+        if (rec_left >= R) {
+            copy4(rec_ptr, rec_off, dst);
+        } else {
+            if (rec_left <= 0 && stages > 0) advance();
+            // (past the last stage rec_left - 1 is negative and leads back to the last record)
+            const char *const at = rec_ptr + (min(rec_row, rec_left - 1) * 16 + rec_sel);
+            copy4(rec_row >= rec_left && rec_sel == 0 ? inf_rec : at, dst);
+        }
+        rec_ptr += RECB;
+        rec_left -= R;
+    }
+};
+}  // namespace wide
+
+template <bool BIG>
+__global__ __launch_bounds__(256, 1) void cross_dkdv_wide_kernel(CrossArgs a) {
+    using namespace wide;
+    __shared__ __attribute__((aligned(1024))) char smem[LDS];
+    int logical;
+    if (!xcd_remap((long long)a.max_items * a.BHk * a.split, logical)) return;
+    const int per = a.max_items * a.split, bhk = logical / per, rest = logical - bhk * per, z = rest / a.max_items;
+    const CrossKeys &keys = a.items[(size_t)(bhk / a.Hk) * a.max_items + (rest - z * a.max_items)];
+    const int key_start = __builtin_amdgcn_readfirstlane(keys.start), key_len = __builtin_amdgcn_readfirstlane(keys.len);
+    if (key_len == 0) return;
+    const size_t head = (size_t)bhk * a.M + key_start;
+    auto store = [&](int kr, int col, const f32x4 &k4, const f32x4 &v4) {
+        if (a.split == 1) {
+            Io<bf16_t>::store4(static_cast<bf16_t *>(a.dk) + (head + kr) * D + col, k4[0], k4[1], k4[2], k4[3]);
+            Io<bf16_t>::store4(static_cast<bf16_t *>(a.dv) + (head + kr) * D + col, v4[0], v4[1], v4[2], v4[3]);
+        } else {
+            float *p = a.kpart + ((size_t)z * a.BHk * a.M + head + kr) * 2 * D + col;
+            *reinterpret_cast<f32x4 *>(p) = k4;
+            *reinterpret_cast<f32x4 *>(p + D) = v4;
+        }
+    };
+    PieceSource src(a, keys);
+    int per_copy = 0;
+    for (int s = src.next_segment(0); s < a.n_seg; s = src.next_segment(s + 1)) per_copy += PieceSource::stages_of(a, s);
+    const long long total = (long long)per_copy * a.copies;
+    const int s0 = (int)(total * z / a.split), n_st = (int)(total * (z + 1) / a.split) - s0;
+    if (n_st == 0) {
+        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+        for (int i = threadIdx.x; i < key_len * (D / 4); i += 256) store(i / (D / 4), i % (D / 4) * 4, zero, zero);
+        return;
+    }
+    src.copy = s0 / per_copy;
+    int skip = s0 - src.copy * per_copy;
+    src.seg = src.next_segment(0);
+    while (skip >= PieceSource::stages_of(a, src.seg)) {
+        skip -= PieceSource::stages_of(a, src.seg);
+        src.seg = src.next_segment(src.seg + 1);
+    }
+    const size_t rows = (size_t)bhk * a.copies * a.N;
+    src.records = reinterpret_cast<const char *>(a.stats) + rows * 16;
+    src.inf_rec = reinterpret_cast<const char *>(a.stats) + (size_t)a.rows * 16;
+    src.stages = n_st;
+    src.enter(skip);
+    src.q_start = src.first;
+    src.q_len = src.rec_left;
+    src.n_direct = (src.q_len + R - 1) / R;
+    const char *const qbase = static_cast<const char *>(uniform_ptr(static_cast<const char *>(a.q) + rows * RB));
+    const char *const dobase = static_cast<const char *>(uniform_ptr(static_cast<const char *>(a.d_o) + rows * RB));
+    const size_t states = (size_t)bhk * a.M * RB;
+    dkdv_wide<BIG>(smem, src, n_st, qbase, dobase, static_cast<const char *>(a.k) + states, static_cast<const char *>(a.v) + states, key_start,
+                   key_len, a.scale, a.scale_log2, store);
+}
+
+void launch_cross_items(const CrossArgs &a, bool wide, int B, hipStream_t st) {
+    MOC_PROF("cross_items", st);
+    cross_items_kernel<<<wide ? B : 1, 256, 0, st>>>(a, wide);
+}
+
+void launch_cross_dkdv_wide(const CrossArgs &a, hipStream_t st) {
+    MOC_PROF("cross_dkdv_wide", st);
+    const int grid = xcd_grid((long long)a.max_items * a.BHk * a.split);
+    if ((long long)a.copies * a.N * wide::RB >= (1ll << 32)) cross_dkdv_wide_kernel<true><<<grid, 256, 0, st>>>(a);
+    else cross_dkdv_wide_kernel<false><<<grid, 256, 0, st>>>(a);
+}
+
+}  // namespace moc
