@@ -402,7 +402,7 @@ int moc_rope(int32_t B, int32_t N, int32_t H, int32_t d, int dtype, const moc_ro
  *   o DEVICE out [B,H,N,d];  lse DEVICE out [B,H,N] float.
  * MOC_BF16: products on bf16 matrix cores, softmax and sums in float, probabilities and dS rounded to
  * bf16 for the second products. MOC_F32: everything in float, the products on float matrix cores (unlike
- * moc_attn_*). softmax_scale finite and > 0. B * H <= 65535, N, M < 2^26, B * H * N and B * Hk * M < 2^31.
+ * moc_attn_*). softmax_scale finite and > 0. B * H <= 65535, H / Hk * N and M < 2^26, B * H * N and B * Hk * M < 2^31.
  *
  * moc_cross_attn_bwd: dq [B,H,N,d], dk, dv [B,Hk,M,d] (fully overwritten; dk and dv are summed over the
  * query heads of a key head) from the forward's o and lse and d_o [B,H,N,d]. Every sum has a fixed order: same

@@ -439,51 +439,73 @@ def rope_plan(positions: torch.Tensor, axis_pairs, freq=None, base: float = 1000
     return RopePlan(positions, axis_pairs, freq, halves)
 
 
-def _same_device(first: torch.Tensor, *others):
+def _ptrs(*ts):
+    return [None if t is None else t.data_ptr() for t in ts]
+
+
+def _on(first: torch.Tensor, *others):
+    """Checks that all tensors share a device; -> what makes it the current one (None: it is already) and its stream."""
+    if not first.is_cuda:
+        raise ValueError("tensors must be CUDA tensors")
+    dev = first.device
     for t in others:
-        if t is not None and t.device != first.device:
+        if t is not None and t.device != dev:
             raise ValueError("tensors must be on one device")
-    return torch.cuda.device(first.device)
+    return None if torch._C._cuda_getDevice() == dev.index else dev.index, torch._C._cuda_getCurrentRawStream(dev.index)
 
 
-def _rows(t: Optional[torch.Tensor], token_major: bool):
-    """moc_rows of a [B, N, heads, d] (token_major) or [B, heads, N, d] tensor; None stays None."""
-    if t is None:
-        return None
-    if not t.is_cuda or t.dim() != 4 or t.stride(3) != 1:
-        raise ValueError("tensors must be 4-dimensional CUDA tensors with contiguous features")
-    n, h = (1, 2) if token_major else (2, 1)
-    return _Rows(t.data_ptr(), t.stride(0), t.stride(h), t.stride(n))
+def _call(where: str, device: Optional[int], *args):
+    if device is None:
+        rc = getattr(_lib, where)(*args)
+    else:
+        with torch.cuda.device(device):
+            rc = getattr(_lib, where)(*args)
+    if rc != 0:
+        raise MocError(rc, where)
 
 
-def _ref(s):
-    return None if s is None else C.byref(s)
+def _rows(t: torch.Tensor, token_major: bool):
+    """moc_rows of a [B, N, heads, d] (token_major) or [B, heads, N, d] tensor."""
+    s = t.stride()
+    if len(s) != 4 or s[3] != 1:
+        raise ValueError("tensors must be 4-dimensional with contiguous features")
+    return _Rows(t.data_ptr(), s[0], s[2], s[1]) if token_major else _Rows(t.data_ptr(), s[0], s[1], s[2])
 
 
 def _same_dtype(first: torch.Tensor, *others):
+    dt = first.dtype
     for t in others:
-        if t is not None and t.dtype != first.dtype:
+        if t is not None and t.dtype != dt:
             raise TypeError("tensors must have one dtype")
     return _dtype_code(first)
 
 
 def _weight(w: Optional[torch.Tensor], d: int):
-    if w is not None and not (w.is_cuda and w.is_contiguous() and w.dtype == torch.float32 and w.numel() == d):
-        raise ValueError("weights must be contiguous float32 CUDA tensors of d values")
-    return w
+    if w is None:
+        return None
+    if w.dtype != torch.float32 or w.shape != (d,) or not w.is_contiguous():
+        raise ValueError("weights must be contiguous float32 tensors of d values")
+    return w.data_ptr()
+
+
+def _need_like(t: torch.Tensor, shape, like: torch.Tensor):
+    """A contiguous tensor of a shape, of `like`'s dtype and device."""
+    if t.shape != shape or t.dtype != like.dtype or t.device != like.device or not t.is_contiguous():
+        raise ValueError(f"need a contiguous {like.dtype} tensor {tuple(shape)} on {like.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 def _token_shape(q, k, v):
-    """B, N, H, Hk, d of token-major projections, any of which may be None."""
-    some = [t for t in (q, k, v) if t is not None]
-    if not some:
+    """B, N, H, Hk, d of token-major projections, any of which may be None, and the first of them."""
+    some = q if q is not None else k if k is not None else v
+    if some is None:
         raise ValueError("q, k and v are all None")
-    B, N, _, d = some[0].shape
-    Hk = (k if k is not None else v).shape[2] if k is not None or v is not None else 1
-    for t, heads in ((q, None), (k, Hk), (v, Hk)):
-        if t is not None and (t.shape[0], t.shape[1], t.shape[3]) != (B, N, d) or t is not None and heads not in (None, t.shape[2]):
+    B, N, H, d = some.shape
+    kv = k if k is not None else v
+    Hk = H if kv is None else kv.shape[2]
+    for t, heads in ((q, H), (k, Hk), (v, Hk)):
+        if t is not None and t.shape != (B, N, heads, d):
             raise ValueError("q, k and v must be [B, N, heads, d] of one B, N and d, k and v of as many heads")
-    return B, N, q.shape[2] if q is not None else Hk, Hk, d
+    return B, N, H, Hk, d, some
 
 
 def _plan(rope: Optional[RopePlan], N: int, device):
@@ -493,37 +515,29 @@ def _plan(rope: Optional[RopePlan], N: int, device):
         raise ValueError(f"tensor has N={N}, positions have N={rope.N}")
     if rope.positions.device != device:
         raise ValueError("tensors must be on one device")
-    return rope.struct
+    return C.byref(rope.struct)
 
 
 def qk_norm_rope(q, k=None, v=None, q_weight=None, k_weight=None, rope: Optional[RopePlan] = None, eps: float = 1e-6, out=None):
     """RMS norm of every head of q and k and the rotation by `rope` (None: not turned), from token-major projections
     [B, N, heads, d] (any strides) to contiguous head-major [B, heads, N, d]; v is moved as it is. Any of q, k, v may be
     None. -> (q, k, v), None where the input is None. `out`: the three tensors to fill."""
-    B, N, H, Hk, d = _token_shape(q, k, v)
-    some = q if q is not None else k if k is not None else v
+    B, N, H, Hk, d, some = _token_shape(q, k, v)
+    lib()
     dt = _same_dtype(some, q, k, v)
-    rq, rk, rv = (_rows(t, True) for t in (q, k, v))
-    with _same_device(some, q, k, v, q_weight, k_weight):
-        if out is None:
-            out = tuple(None if t is None else torch.empty(B, t.shape[2], N, d, dtype=t.dtype, device=t.device) for t in (q, k, v))
-        else:
-            _need_like([(o, None if t is None else (B, t.shape[2], N, d)) for o, t in zip(out, (q, k, v))], some)
-        plan = _plan(rope, N, some.device)
-        _check(lib().moc_qk_norm_rope(B, N, H, Hk, d, dt, _ref(rq), _ref(rk), _ref(rv), _ptr(_weight(q_weight, d)),
-                                      _ptr(_weight(k_weight, d)), float(eps), _ref(plan), *(_ptr(t) for t in out), _stream()),
-               "moc_qk_norm_rope")
+    device, stream = _on(some, q, k, v, q_weight, k_weight)
+    if out is None:
+        out = [None if t is None else torch.empty((B, t.shape[2], N, d), dtype=t.dtype, device=t.device) for t in (q, k, v)]
+    else:
+        for o, t in zip(out, (q, k, v)):
+            if (o is None) != (t is None):
+                raise ValueError("out must hold a tensor for each of q, k and v that is given")
+            if o is not None:
+                _need_like(o, (B, t.shape[2], N, d), some)
+    rows = [None if t is None else C.byref(_rows(t, True)) for t in (q, k, v)]
+    _call("moc_qk_norm_rope", device, B, N, H, Hk, d, dt, *rows, _weight(q_weight, d), _weight(k_weight, d), eps,
+          _plan(rope, N, some.device), *_ptrs(*out), stream)
     return tuple(out)
-
-
-def _need_like(pairs, like: torch.Tensor):
-    """Contiguous tensors of the shapes, of `like`'s dtype and device; None for None."""
-    for t, shape in pairs:
-        if (t is None) != (shape is None):
-            raise ValueError("a tensor is missing, or one was given that belongs to none")
-        if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != like.dtype or t.device != like.device
-                              or not t.is_contiguous()):
-            raise ValueError(f"need a contiguous {like.dtype} tensor {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
 
 
 def qk_norm_rope_workspace(B: int, N: int, H: int, Hk: int, d: int, dtype: torch.dtype, device="cuda") -> torch.Tensor:
@@ -538,28 +552,27 @@ def qk_norm_rope_bwd(q, k, d_q_out, d_k_out, d_v_out=None, q_weight=None, k_weig
     """Gradients of qk_norm_rope from those of its outputs (contiguous [B, heads, N, d]) and its inputs q and k
     -> dq, dk, dv (token-major [B, N, heads, d]) and dq_weight, dk_weight ([d] float32); None where nothing was given.
     `out` = (dq, dk, dv) tensors to fill, of any strides."""
-    d_v_tokens = None if d_v_out is None else d_v_out.transpose(1, 2)
-    B, N, H, Hk, d = _token_shape(q, k, d_v_tokens)
+    B, N, H, Hk, d, some = _token_shape(q, k, None if d_v_out is None else d_v_out.transpose(1, 2))
+    lib()
     grads = (d_q_out, d_k_out, d_v_out)
-    some = next(t for t in (q, k, d_v_out) if t is not None)
     dt = _same_dtype(some, q, k, *grads)
-    _need_like([(g, None if t is None else (B, t.shape[2], N, d)) for g, t in zip(grads, (q, k, d_v_tokens))], some)
-    with _same_device(some, q, k, *grads, q_weight, k_weight, workspace):
-        if out is None:
-            out = tuple(None if g is None else torch.empty(B, N, g.shape[1], d, dtype=g.dtype, device=g.device) for g in grads)
-        for o, g in zip(out, grads):
-            if (o is None) != (g is None) or (o is not None and (tuple(o.shape) != (B, N, g.shape[1], d) or o.dtype != g.dtype
-                                                                or o.device != g.device)):
-                raise ValueError("out must be the gradients [B, N, heads, d] of the inputs")
-        dqw = None if q is None else torch.empty(d, dtype=torch.float32, device=some.device)
-        dkw = None if k is None else torch.empty(d, dtype=torch.float32, device=some.device)
-        ws = workspace if workspace is not None else qk_norm_rope_workspace(B, N, H, Hk, d, some.dtype, some.device)
-        rows = [_rows(t, True) for t in (q, k, *out)]
-        plan = _plan(rope, N, some.device)
-        _check(lib().moc_qk_norm_rope_bwd(B, N, H, Hk, d, dt, _ref(rows[0]), _ref(rows[1]), _ptr(_weight(q_weight, d)),
-                                          _ptr(_weight(k_weight, d)), float(eps), _ref(plan), *(_ptr(g) for g in grads),
-                                          *(_ref(r) for r in rows[2:]), _ptr(dqw), _ptr(dkw), _ptr(ws), ws.numel(), _stream()),
-               "moc_qk_norm_rope_bwd")
+    device, stream = _on(some, q, k, *grads, q_weight, k_weight, workspace)
+    for g, t, heads in zip(grads, (q, k, d_v_out), (H, Hk, Hk)):
+        if (g is None) != (t is None):
+            raise ValueError("the gradients of q's and k's outputs go with q and k")
+        if g is not None:
+            _need_like(g, (B, heads, N, d), some)
+    if out is None:
+        out = [None if g is None else torch.empty((B, N, g.shape[1], d), dtype=g.dtype, device=g.device) for g in grads]
+    for o, g in zip(out, grads):
+        if (o is None) != (g is None) or o is not None and (o.shape != (B, N, g.shape[1], d) or o.dtype != g.dtype or o.device != g.device):
+            raise ValueError("out must be the gradients [B, N, heads, d] of the inputs")
+    dw = torch.empty((2, d), dtype=torch.float32, device=some.device)
+    dqw, dkw = None if q is None else dw[0], None if k is None else dw[1]
+    ws = workspace if workspace is not None else qk_norm_rope_workspace(B, N, H, Hk, d, some.dtype, some.device)
+    rows = [None if t is None else C.byref(_rows(t, True)) for t in (q, k, *out)]
+    _call("moc_qk_norm_rope_bwd", device, B, N, H, Hk, d, dt, *rows[:2], _weight(q_weight, d), _weight(k_weight, d), eps,
+          _plan(rope, N, some.device), *_ptrs(*grads), *rows[2:], *_ptrs(dqw, dkw), ws.data_ptr(), ws.numel(), stream)
     return (*out, dqw, dkw)
 
 
@@ -568,27 +581,30 @@ def apply_rope(x: torch.Tensor, rope: RopePlan, inverse: bool = False, out: Opti
     the rotation. `out` may be x itself (in place) or a tensor of any strides; without it the result is contiguous."""
     rx = _rows(x, False)
     B, H, N, d = x.shape
-    with _same_device(x, out):
-        if out is None:
-            out = torch.empty(B, H, N, d, dtype=x.dtype, device=x.device)
-        elif out.shape != x.shape or out.dtype != x.dtype:
-            raise ValueError("out must have the shape and dtype of x")
-        ro = _rows(out, False)
-        _check(lib().moc_rope(B, N, H, d, _dtype_code(x), _ref(rx), _ref(_plan(rope, N, x.device)), int(bool(inverse)),
-                              _ref(ro), _stream()), "moc_rope")
+    lib()
+    device, stream = _on(x, out)
+    if out is None:
+        out = torch.empty((B, H, N, d), dtype=x.dtype, device=x.device)
+    elif out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError("out must have the shape and dtype of x")
+    _call("moc_rope", device, B, N, H, d, _dtype_code(x), C.byref(rx), _plan(rope, N, x.device), int(bool(inverse)),
+          C.byref(_rows(out, False)), stream)
     return out
 
 
 def _cross_shape(q, k, v, kv_ranges, q_offsets):
     if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[3]:
         raise ValueError("need q [B, H, N, d] and k, v [B, Hk, M, d]")
-    _need_contig(q, k, v, kv_ranges)
-    (B, H, N, d), (Hk, M) = q.shape, k.shape[1:3]
-    off = None if q_offsets is None else _i32(q_offsets)
-    S = 1 if off is None else off.shape[0] - 1
-    if kv_ranges is not None and (kv_ranges.dtype != torch.int32 or tuple(kv_ranges.shape) != (B, S, 2)):
-        raise ValueError(f"kv_ranges must be an int32 tensor {(B, S, 2)}")
-    return B, H, Hk, N, M, d, S, off
+    if not (q.is_contiguous() and k.is_contiguous() and v.is_contiguous()):
+        raise ValueError("tensors must be contiguous")
+    B, H, N, d = q.shape
+    off, S = None, 1
+    if q_offsets is not None:
+        off = _i32(q_offsets)
+        S = off.shape[0] - 1
+    if kv_ranges is not None and (kv_ranges.dtype != torch.int32 or kv_ranges.shape != (B, S, 2) or not kv_ranges.is_contiguous()):
+        raise ValueError(f"kv_ranges must be a contiguous int32 tensor {(B, S, 2)}")
+    return B, H, k.shape[1], N, k.shape[2], d, S, off
 
 
 def cross_attn_workspace(B: int, H: int, Hk: int, N: int, M: int, d: int, dtype: torch.dtype, with_bwd: bool,
@@ -599,47 +615,53 @@ def cross_attn_workspace(B: int, H: int, Hk: int, N: int, M: int, d: int, dtype:
     return torch.empty(max(nbytes.value, 16), dtype=torch.uint8, device=device)
 
 
+def _need_lse(lse, q):
+    if lse.shape != q.shape[:3] or lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous float32 tensor [B, H, N]")
+
+
 def cross_attn_fwd(q, k, v, kv_ranges: Optional[torch.Tensor] = None, q_offsets=None, scale: Optional[float] = None,
                    workspace: Optional[torch.Tensor] = None, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
     """Attention of q [B, H, N, d] to encoder states k, v [B, Hk, M, d] -> o [B, H, N, d], lse [B, H, N] fp32.
     q_offsets [S+1] (host) cuts the queries into segments, kv_ranges [B, S, 2] int32 (device) says which states
     [first, end) a segment of a sample attends; an empty range gives o = 0, lse = -inf."""
     B, H, Hk, N, M, d, S, off = _cross_shape(q, k, v, kv_ranges, q_offsets)
+    lib()
     dt = _same_dtype(q, k, v)
-    with _same_device(q, k, v, kv_ranges, workspace):
-        scale = float(d ** -0.5 if scale is None else scale)
-        ws = workspace if workspace is not None else cross_attn_workspace(B, H, Hk, N, M, d, q.dtype, False, S, q.device)
-        if out is None:
-            out = torch.empty_like(q), torch.empty(B, H, N, dtype=torch.float32, device=q.device)
-        else:
-            _need_like([(out[0], q.shape)], q)
-            _need_lse(out[1], q)
-        _check(lib().moc_cross_attn_fwd(B, H, Hk, N, M, d, dt, _ptr(q), _ptr(k), _ptr(v), S,
-                                        None if off is None else off.ctypes.data, _ptr(kv_ranges), scale, _ptr(out[0]),
-                                        _ptr(out[1]), _ptr(ws), ws.numel(), _stream()), "moc_cross_attn_fwd")
-    return tuple(out)
-
-
-def _need_lse(lse, q):
-    if tuple(lse.shape) != tuple(q.shape[:3]) or lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous():
-        raise ValueError("lse must be a contiguous float32 tensor [B, H, N]")
+    device, stream = _on(q, k, v, kv_ranges, workspace)
+    ws = workspace if workspace is not None else cross_attn_workspace(B, H, Hk, N, M, d, q.dtype, False, S, q.device)
+    if out is None:
+        o, lse = torch.empty_like(q), torch.empty((B, H, N), dtype=torch.float32, device=q.device)
+    else:
+        o, lse = out
+        _need_like(o, q.shape, q)
+        _need_lse(lse, q)
+    _call("moc_cross_attn_fwd", device, B, H, Hk, N, M, d, dt, q.data_ptr(), k.data_ptr(), v.data_ptr(), S,
+          None if off is None else off.ctypes.data, None if kv_ranges is None else kv_ranges.data_ptr(),
+          d ** -0.5 if scale is None else scale, o.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(), stream)
+    return o, lse
 
 
 def cross_attn_bwd(q, k, v, o, lse, d_o, kv_ranges: Optional[torch.Tensor] = None, q_offsets=None, scale: Optional[float] = None,
                    workspace: Optional[torch.Tensor] = None, out=None):
     """-> dq [B, H, N, d], dk, dv [B, Hk, M, d] from the forward's o and lse and the gradient d_o of o."""
     B, H, Hk, N, M, d, S, off = _cross_shape(q, k, v, kv_ranges, q_offsets)
+    lib()
     dt = _same_dtype(q, k, v, o, d_o)
-    _need_like([(o, q.shape), (d_o, q.shape)], q)
+    device, stream = _on(q, k, v, kv_ranges, workspace)
+    _need_like(o, q.shape, q)
+    _need_like(d_o, q.shape, q)
     _need_lse(lse, q)
-    with _same_device(q, k, v, kv_ranges, workspace):
-        scale = float(d ** -0.5 if scale is None else scale)
-        ws = workspace if workspace is not None else cross_attn_workspace(B, H, Hk, N, M, d, q.dtype, True, S, q.device)
-        if out is None:
-            out = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
-        else:
-            _need_like([(out[0], q.shape), (out[1], k.shape), (out[2], v.shape)], q)
-        _check(lib().moc_cross_attn_bwd(B, H, Hk, N, M, d, dt, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o), S,
-                                        None if off is None else off.ctypes.data, _ptr(kv_ranges), scale,
-                                        *(_ptr(t) for t in out), _ptr(ws), ws.numel(), _stream()), "moc_cross_attn_bwd")
-    return tuple(out)
+    ws = workspace if workspace is not None else cross_attn_workspace(B, H, Hk, N, M, d, q.dtype, True, S, q.device)
+    if out is None:
+        dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    else:
+        dq, dk, dv = out
+        _need_like(dq, q.shape, q)
+        _need_like(dk, k.shape, q)
+        _need_like(dv, k.shape, q)
+    _call("moc_cross_attn_bwd", device, B, H, Hk, N, M, d, dt, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+          lse.data_ptr(), d_o.data_ptr(), S, None if off is None else off.ctypes.data,
+          None if kv_ranges is None else kv_ranges.data_ptr(), d ** -0.5 if scale is None else scale, dq.data_ptr(),
+          dk.data_ptr(), dv.data_ptr(), ws.data_ptr(), ws.numel(), stream)
+    return dq, dk, dv

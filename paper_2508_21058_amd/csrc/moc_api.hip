@@ -953,7 +953,7 @@ int check_cross(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t 
     if (d != 64 && d != 128) return fail(MOC_ERR_SHAPE, "d must be 64 or 128");
     if (S < 1 || S > MOC_MAX_CROSS_SEGMENTS) return fail(MOC_ERR_SHAPE, "need 1 <= S <= MOC_MAX_CROSS_SEGMENTS");
     if ((long long)B * H > 65535) return fail(MOC_ERR_SHAPE, "B * H must be <= 65535");
-    if (N >= (1 << 26) || M >= (1 << 26)) return fail(MOC_ERR_SHAPE, "N and M must be < 2^26");
+    if ((long long)N * (H / Hk) >= (1 << 26) || M >= (1 << 26)) return fail(MOC_ERR_SHAPE, "H / Hk * N and M must be < 2^26");
     if ((long long)B * H * N >= (1LL << 31) || (long long)B * Hk * M >= (1LL << 31))
         return fail(MOC_ERR_SHAPE, "B * H * N and B * Hk * M must be < 2^31");
     return MOC_OK;
@@ -982,12 +982,6 @@ int cross_args(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t d
     a.copies = S == 1 ? 1 : H / Hk;
     a.N = S == 1 ? N * (H / Hk) : N;
     for (int s = 0; s <= S; ++s) a.q_off[s] = S == 1 ? s * a.N : q_offsets[s];
-    a.tiles = 0;
-    for (int s = 0; s < S; ++s) {
-        a.tile_at[s] = a.tiles;
-        a.tiles += (a.q_off[s + 1] - a.q_off[s] + 127) / 128;
-    }
-    a.tile_at[S] = a.tiles;
     return MOC_OK;
 }
 
@@ -1160,6 +1154,7 @@ int moc_cross_attn_bwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, i
     a.part = reinterpret_cast<float *>(ws + p.part);
     a.kpart = reinterpret_cast<float *>(ws + p.kpart);
     a.items = reinterpret_cast<moc::CrossKeys *>(ws + p.items);
+    a.item_counts = reinterpret_cast<moc::CrossCount *>(ws + p.item_counts);
     a.max_items = p.max_items;
     const hipError_t e = moc::launch_cross_bwd(a, p, d, dtype, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? MOC_OK : hip_fail(e, "cross attention backward kernels");

@@ -41,6 +41,7 @@ struct CrossKeys {
     int32_t start, len, pad[2];
     uint32_t segments[MOC_MAX_CROSS_SEGMENTS / 32];
 };
+struct CrossCount { int32_t live, idle; };             // of a sample: tiles of segments (the first ones) and without any
 struct CrossArgs {
     const void *q, *k, *v, *o_in, *d_o;
     void *o, *dq, *dk, *dv;
@@ -50,26 +51,29 @@ struct CrossArgs {
     float *part, *part_lse;            // split calls: [split][B * H * N][d], [split][B * H * N]
     float *kpart;                      // split dK / dV: [split][B * Hk * M][2][d]
     CrossKeys *items;                  // wide tiles: [B][max_items]
+    CrossCount *item_counts;           // [B]
     int max_items;
     const CrossRange *ranges;          // [B][n_seg] or nullptr
     long long rows;                    // B * H * N
     int N, M, n_seg;                   // tokens of a query head (all heads of a group where copies is 1 and H > Hk), states
     int copies;                        // query heads of a key head that are walked one by one
     int Hk, BHk, tiles;                // tiles: query tiles of one copy
-    int split;
+    int split, tile_rows;              // tile_rows: queries of a query tile
     float scale, scale_log2;
     int32_t q_off[MOC_MAX_CROSS_SEGMENTS + 1];
     int32_t tile_at[MOC_MAX_CROSS_SEGMENTS + 1];      // first query tile of a segment
 };
 // Sizes of a call that follow from its arguments alone, and the places in its workspace (byte offsets).
+void cross_tiles(CrossArgs &a, int tile_rows);                      // cuts the segments into query tiles
+int cross_resident_rows(const CrossArgs &a, int waves);             // queries of an item of the resident passes; 0: too few for them
 struct CrossPlan {
     int split_fwd, split_dq, split_kv;
     bool wide;                         // dK and dV in tiles of 256 states (moc_cross_dkdv.hip)
     int max_items;
-    size_t stats, part, part_lse, kpart, items, total;
+    size_t stats, part, part_lse, kpart, items, item_counts, total;
 };
 CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype, bool with_bwd);
-hipError_t launch_cross_fwd(const CrossArgs &a, int d, int dtype, hipStream_t st);
+hipError_t launch_cross_fwd(CrossArgs a, int d, int dtype, hipStream_t st);
 // the records of padding rows and, of wide tiles, the items; then the tiles themselves
 void launch_cross_items(const CrossArgs &a, bool wide, int B, hipStream_t st);
 void launch_cross_dkdv_wide(const CrossArgs &a, hipStream_t st);

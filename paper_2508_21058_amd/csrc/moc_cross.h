@@ -96,7 +96,7 @@ __device__ __forceinline__ void copy_tile(const T *first, int valid, char *tile,
     }
 }
 
-// Work item of the query-stationary passes: up to kCrossRows queries of one segment of one query head.
+// Work item of the query-stationary passes: up to tile_rows queries of one segment of one query head.
 struct CrossItem {
     int bhk, count, first, end;      // key head of all samples, queries, range of states
     long long row;                   // first query in [B * H * N]
@@ -120,8 +120,8 @@ __device__ __forceinline__ CrossItem cross_item(const CrossArgs &a, int logical)
         const int mid = (s + hi) >> 1;
         if (a.tile_at[mid] <= t) s = mid; else hi = mid;
     }
-    const int q = a.q_off[s] + (t - a.tile_at[s]) * kCrossRows;
-    it.count = min(kCrossRows, a.q_off[s + 1] - q);
+    const int q = a.q_off[s] + (t - a.tile_at[s]) * a.tile_rows;
+    it.count = min(a.tile_rows, a.q_off[s + 1] - q);
     it.row = ((long long)it.bhk * a.copies + copy) * a.N + q;
     const CrossRange r = cross_range(a, it.bhk / a.Hk, s);
     it.first = __builtin_amdgcn_readfirstlane(r.first);
@@ -135,6 +135,26 @@ __device__ __forceinline__ void cross_slice(int &first, int &end, int z, int n, 
     first = min(end, f + (int)((long long)tiles * z / n) * tile);
     end = min(end, f + (int)((long long)tiles * (z + 1) / n) * tile);
 }
+
+// Keys and values of the resident passes: NW waves share two halves of kHalf rows of each, which fill a compute unit's LDS.
+//   a range of at most 2 kHalf states is loaded once and stays; the waves go through the item's queries, 32 at a time, on their own;
+//   a longer one passes through the halves in turn, a barrier a half, for NW blocks of queries at a time.
+template <int D, int NW> struct Resident {
+    static constexpr int kHalf = 160 * 128 / D, RB = D * 2, HB = kHalf * RB, V0 = 2 * HB, LDS = 4 * HB;
+    static_assert(LDS == 160 * 1024);
+    // rows [0, valid) of K and V, the last repeated up to a whole block of 32, to row `at` of the regions
+    static __device__ __forceinline__ void load(char *smem, const bf16_t *k, const bf16_t *v, int valid, int at, int wave, int lane) {
+        constexpr int GR = RB / 16, RPI = 64 / GR;
+        const int rows = (valid + 31) & ~31;
+        const uint32_t dst = lds_address(smem) + at * RB;
+        for (int n = wave; n * RPI < rows; n += NW) {
+            const int row = n * RPI + lane / GR;
+            const uint32_t off = (uint32_t)min(row, valid - 1) * RB + (((lane % GR) ^ SwTile<D>::sw(row)) << 4);
+            cross_copy16(k, off, dst + n * 1024);
+            cross_copy16(v, off, dst + V0 + n * 1024);
+        }
+    }
+};
 
 // A wave's 32 x D transposed accumulator (lane: row l32, four-feature pieces) times `scale` to the float rows at `out`.
 template <int D> __device__ __forceinline__ void store_rows_f32(const f32x16 *acc, float scale, float *row, int half) {

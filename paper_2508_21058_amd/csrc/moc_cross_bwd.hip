@@ -31,34 +31,43 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void cross_dq_kernel(C
     const int r = wave * 32 + l32, rc = min(r, it.count - 1);
     const bool row_valid = r < it.count;
     const size_t row = (size_t)it.row + rc;
+    const bool some = it.first < it.end;
+    const T *kb = static_cast<const T *>(a.k) + (size_t)it.bhk * a.M * D, *vb = static_cast<const T *>(a.v) + (size_t)it.bhk * a.M * D;
+    auto issue = [&](int pos, int buf) {
+        const int valid = min(BN, it.end - pos);
+        copy_tile<D, T, BN>(kb + (size_t)pos * D, valid, smem + buf * 2 * TB, wave, lane);
+        copy_tile<D, T, BN>(vb + (size_t)pos * D, valid, smem + buf * 2 * TB + TB, wave, lane);
+    };
+    if (some) issue(it.first, 0);
+    // All of the item's loads go out before anything waits for one: left to the compiler, the products of delta came between them
+    // (114k queries of 24 heads, 256 states: 836 us, this way 718).
     typename O::Frag qf[O::KS], dof[O::KS];
-    float delta = 0.f;
+    float delta = 0.f, lse2;
     {
         const T *qrow = static_cast<const T *>(a.q) + row * D, *dorow = static_cast<const T *>(a.d_o) + row * D;
         const T *orow = static_cast<const T *>(a.o_in) + row * D;
+        typename O::Frag of[O::KS];
+        lse2 = a.lse_in[row] * kLog2e;
 #pragma unroll
         for (int s = 0; s < O::KS; ++s) {
-            qf[s] = O::row_frag(qrow, s, half);
+            of[s] = O::row_frag(orow, s, half);
             dof[s] = O::row_frag(dorow, s, half);
-            delta += O::dot(dof[s], O::row_frag(orow, s, half));
         }
+#pragma unroll
+        for (int s = 0; s < O::KS; ++s) qf[s] = O::row_frag(qrow, s, half);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int s = 0; s < O::KS; ++s) delta += O::dot(dof[s], of[s]);
         delta = xhalf_sum(delta);
     }
-    const float lse2 = a.lse_in[row] * kLog2e, c = a.scale_log2;
+    const float c = a.scale_log2;
     if (z == 0 && row_valid && half == 0) store_record(a, it, row, lse2, delta);
     f32x16 dq[DB];
 #pragma unroll
     for (int b = 0; b < DB; ++b) dq[b] = zero16();
-    if (it.first < it.end) {
-        const T *kb = static_cast<const T *>(a.k) + (size_t)it.bhk * a.M * D, *vb = static_cast<const T *>(a.v) + (size_t)it.bhk * a.M * D;
+    if (some) {
         O ops;
         ops.init(lane);
-        auto issue = [&](int pos, int buf) {
-            const int valid = min(BN, it.end - pos);
-            copy_tile<D, T, BN>(kb + (size_t)pos * D, valid, smem + buf * 2 * TB, wave, lane);
-            copy_tile<D, T, BN>(vb + (size_t)pos * D, valid, smem + buf * 2 * TB + TB, wave, lane);
-        };
-        issue(it.first, 0);
         int buf = 0;
         for (int pos = it.first; pos < it.end; pos += BN, buf ^= 1) {
             wait_vmcnt<0>();
@@ -136,7 +145,7 @@ __device__ __forceinline__ void make_stream(const CrossArgs &a, int b, int key0,
 }
 
 template <int D, typename T>
-__global__ __launch_bounds__(256, 1) void cross_dkdv_kernel(CrossArgs a) {
+__global__ __launch_bounds__(256, D == 64 && sizeof(T) == 2 ? 2 : 1) void cross_dkdv_kernel(CrossArgs a) {
     typedef Ops<D, T> O;
     constexpr int DB = D / 32, TB = kStreamRows * O::RB;
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB];          // Q, dO, twice
@@ -263,6 +272,7 @@ __global__ __launch_bounds__(256) void cross_sum_kernel(const float *__restrict_
 
 template <int D, typename T> static void bwd_dispatch(CrossArgs a, const CrossPlan &p, hipStream_t st) {
     launch_cross_items(a, p.wide, a.BHk / a.Hk, st);
+    cross_tiles(a, kCrossRows);
     a.split = p.split_dq;
     {
         MOC_PROF("cross_dq", st);
@@ -275,7 +285,7 @@ template <int D, typename T> static void bwd_dispatch(CrossArgs a, const CrossPl
     }
     a.split = p.split_kv;
     const long long states = (long long)a.BHk * a.M;
-    if (p.wide) {
+    if constexpr (D == 128 && sizeof(T) == 2) {
         launch_cross_dkdv_wide(a, st);
     } else {
         MOC_PROF("cross_dkdv", st);
@@ -305,11 +315,25 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
     auto split = [](long long n, long long want, long long most) { return n >= want ? 1 : (int)std::max(1LL, std::min((want - 1 + n) / n, most)); };
     p.split_fwd = p.split_dq = split(items, 512, (M + 255) / 256);
     const long long rows = (long long)B * H * N, states = (long long)B * Hk * M, per_head = (long long)N * (H / Hk);
-    // (a record holds the row of a query among those of its key head in 26 bits)
-    p.wide = d == 128 && dtype == MOC_BF16 && per_head < (1 << 26);
+    p.wide = d == 128 && dtype == MOC_BF16;
     p.max_items = M / kWideTile + 2 * S + 1;
-    if (p.wide) p.split_kv = split((long long)B * Hk * ((M + kWideTile - 1) / kWideTile), 1024, (per_head + 255) / 256);
-    else p.split_kv = split((long long)B * Hk * ((M + kCrossKeys - 1) / kCrossKeys), 512, (per_head + 511) / 512);
+    if (p.wide) {
+        // Parts of the queries that workgroups of one tile of states share. Rounds of the chip are whole and take as long as a part, but a
+        // round with units to spare runs at a higher clock: full rounds take 1.2 times as long per item. A part costs its sums, written and
+        // read again. Microseconds: 0.75 for 16 queries, 6 to begin and end, 6 TB/s. 33k queries, 4,357 states, 24 heads (432 tiles) 1 / 2 / 3
+        // / 4 / 8 parts: 3,112 / 3,488 / 3,508 / 3,597 / 3,373 us; eight shots of 14k queries with captions of 100 to 512 states 1,431 / 1,135 /
+        // 1,089 / 1,065 / 1,163. (The sums may take half a gigabyte.)
+        const long long tiles = (long long)B * Hk * ((M + kWideTile - 1) / kWideTile);
+        const double stages = std::max(1.0, (double)per_head / S / 16), sums = (double)states * d * 16 / 6e6;
+        double best = 0;
+        for (long long s = 1; s <= std::min(64LL, (per_head + 255) / 256) && (s == 1 || s * states * d * 8 <= 512 << 20); ++s) {
+            const double item = 0.75 * stages / s + 6, rounds = (double)((tiles * s + kComputeUnits - 1) / kComputeUnits);
+            const double us = std::max(rounds, 1.2 * tiles * s / kComputeUnits) * item + (s > 1 ? s * sums + 5 : 0);
+            if (s == 1 || us < best) { best = us; p.split_kv = (int)s; }
+        }
+    } else {
+        p.split_kv = split((long long)B * Hk * ((M + kCrossKeys - 1) / kCrossKeys), 512, (per_head + 127) / 128);
+    }
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t x = at; at += up(bytes); return x; };
     p.part = take(p.split_fwd > 1 ? (size_t)p.split_fwd * rows * d * 4 : 0);
@@ -317,6 +341,7 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
     p.stats = take(with_bwd ? (size_t)(rows + 1) * 16 : 0);
     p.kpart = take(with_bwd && p.split_kv > 1 ? (size_t)p.split_kv * states * 2 * d * 4 : 0);
     p.items = take(with_bwd && p.wide ? (size_t)B * p.max_items * sizeof(CrossKeys) : 0);
+    p.item_counts = take(with_bwd && p.wide ? (size_t)B * sizeof(CrossCount) : 0);
     p.total = at;
     return p;
 }

@@ -35,33 +35,43 @@ __global__ __launch_bounds__(256) void cross_items_kernel(CrossArgs a, bool wide
         sorted[rank] = x;
     }
     __syncthreads();
-    // piece i: states [sorted[i], sorted[i + 1]), its tiles from tile_at[i] on
+    // piece i: states [sorted[i], sorted[i + 1]), of a range or of none; its tiles from tile_at[i] on, those of ranges first
     for (int i = tid; i < n; i += 256) {
-        int at = 0;
-        for (int j = 0; j < i; ++j) at += (sorted[j + 1] - sorted[j] + kWideTile - 1) / kWideTile;
-        tile_at[i] = at;
-        uint32_t in[MOC_MAX_CROSS_SEGMENTS / 32] = {};
-        for (int s = 0; s < S && i + 1 < n; ++s)
-            if (first[s] <= sorted[i] && end[s] >= sorted[i + 1]) in[s >> 5] |= 1u << (s & 31);
-        for (int w = 0; w < MOC_MAX_CROSS_SEGMENTS / 32; ++w) segments[i][w] = in[w];
+        for (int w = 0; w < MOC_MAX_CROSS_SEGMENTS / 32; ++w) {
+            uint32_t in = 0;
+            for (int s = 32 * w; s < min(32 * w + 32, S) && i + 1 < n; ++s)
+                if (first[s] <= sorted[i] && end[s] >= sorted[i + 1]) in |= 1u << (s & 31);
+            segments[i][w] = in;
+        }
     }
     __syncthreads();
-    const int total = tile_at[n - 1];
+    auto attended = [&](int i) { return (segments[i][0] | segments[i][1] | segments[i][2] | segments[i][3]) != 0; };
+    static_assert(MOC_MAX_CROSS_SEGMENTS == 128, "four words of segments");
+    for (int i = tid; i + 1 < n; i += 256) {
+        const bool mine = attended(i);
+        int at = 0;
+        for (int j = 0; j + 1 < n; ++j) {
+            const bool other = attended(j);
+            if (other == mine ? j < i : other) at += (sorted[j + 1] - sorted[j] + kWideTile - 1) / kWideTile;
+        }
+        tile_at[i] = at;
+    }
+    __syncthreads();
     CrossKeys *out = a.items + (size_t)b * a.max_items;
-    for (int t = tid; t < a.max_items; t += 256) {
-        CrossKeys k{};
-        if (t < total) {
-            int i = 0, hi = n - 1;                        // the last piece with tile_at <= t (empty pieces have the next one's)
-            while (hi - i > 1) {
-                const int mid = (i + hi) >> 1;
-                if (tile_at[mid] <= t) i = mid; else hi = mid;
-            }
-            k.start = sorted[i] + (t - tile_at[i]) * kWideTile;
+    int live = 0, total = 0;
+    for (int i = 0; i + 1 < n; ++i) {
+        const int tiles = (sorted[i + 1] - sorted[i] + kWideTile - 1) / kWideTile;
+        total += tiles;
+        live += attended(i) ? tiles : 0;
+        for (int t = tid; t < tiles; t += 256) {
+            CrossKeys k{};
+            k.start = sorted[i] + t * kWideTile;
             k.len = min(kWideTile, sorted[i + 1] - k.start);
             for (int w = 0; w < MOC_MAX_CROSS_SEGMENTS / 32; ++w) k.segments[w] = segments[i][w];
+            out[tile_at[i] + t] = k;
         }
-        out[t] = k;
     }
+    if (tid == 0) a.item_counts[b] = CrossCount{live, total - live};
 }
 
 namespace wide {
@@ -113,12 +123,54 @@ template <bool BIG>
 __global__ __launch_bounds__(256, 1) void cross_dkdv_wide_kernel(CrossArgs a) {
     using namespace wide;
     __shared__ __attribute__((aligned(1024))) char smem[LDS];
-    int logical;
-    if (!xcd_remap((long long)a.max_items * a.BHk * a.split, logical)) return;
-    const int per = a.max_items * a.split, bhk = logical / per, rest = logical - bhk * per, z = rest / a.max_items;
-    const CrossKeys &keys = a.items[(size_t)(bhk / a.Hk) * a.max_items + (rest - z * a.max_items)];
+    // Tiles that stream come first, then those without a segment, both in slices of the XCDs. (Were they mixed, tiles that end at
+    // once would take every second or fourth workgroup, and the shader engines that these go to would idle: one live tile of four,
+    // 114k queries of 24 heads, 256 states 2,300 us, packed 722.)
+    int l, bhk, z, item;
+    {
+        const int lane = threadIdx.x & 63, B = a.BHk / a.Hk;
+        auto units = [&](int b, bool live) {
+            if (b >= B) return 0;
+            const CrossCount n = a.item_counts[b];
+            return live ? n.live * a.split * a.Hk : n.idle * a.Hk;
+        };
+        int total[2] = {0, 0};
+        for (int b = lane; b < B; b += 64) { total[0] += units(b, true); total[1] += units(b, false); }
+#pragma unroll
+        for (int w = 1; w < 64; w <<= 1) { total[0] += __shfl_xor(total[0], w, 64); total[1] += __shfl_xor(total[1], w, 64); }
+        const int x = blockIdx.x % kXcds, p = blockIdx.x / kXcds, per_live = (total[0] + kXcds - 1) / kXcds, per_idle = (total[1] + kXcds - 1) / kXcds;
+        const bool live = p < per_live;
+        l = live ? x * per_live + p : x * per_idle + p - per_live;
+        if (l >= total[live ? 0 : 1] || (!live && p - per_live >= per_idle)) return;
+        int b0 = 0, mine, at;
+        while (true) {                                       // the sample of unit l
+            if (b0 >= B) return;
+            mine = units(b0 + lane, live);
+            at = mine;
+#pragma unroll
+            for (int w = 1; w < 64; w <<= 1) {
+                const int o = __shfl_up(at, w, 64);
+                if (lane >= w) at += o;
+            }
+            const int all = __shfl(at, 63, 64);
+            if (l < all) break;
+            l -= all;
+            b0 += 64;
+        }
+        const int who = __ffsll((unsigned long long)__ballot(l < at)) - 1;
+        l -= __shfl(at - mine, who, 64);
+        const CrossCount n = a.item_counts[b0 + who];
+        const int per = live ? n.live * a.split : n.idle;
+        const int hk = l / per, rest = l - hk * per;
+        z = live ? rest / n.live : 0;
+        item = live ? rest - z * n.live : n.live + rest;
+        bhk = (b0 + who) * a.Hk + hk;
+        bhk = __builtin_amdgcn_readfirstlane(bhk);
+        z = __builtin_amdgcn_readfirstlane(z);
+        item = __builtin_amdgcn_readfirstlane(item);
+    }
+    const CrossKeys &keys = a.items[(size_t)(bhk / a.Hk) * a.max_items + item];
     const int key_start = __builtin_amdgcn_readfirstlane(keys.start), key_len = __builtin_amdgcn_readfirstlane(keys.len);
-    if (key_len == 0) return;
     const size_t head = (size_t)bhk * a.M + key_start;
     auto store = [&](int kr, int col, const f32x4 &k4, const f32x4 &v4) {
         if (a.split == 1) {
@@ -137,6 +189,7 @@ __global__ __launch_bounds__(256, 1) void cross_dkdv_wide_kernel(CrossArgs a) {
     const int s0 = (int)(total * z / a.split), n_st = (int)(total * (z + 1) / a.split) - s0;
     if (n_st == 0) {
         const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+        for (; z < a.split; z = per_copy ? a.split : z + 1)      // (a tile without segments is one item for all parts)
         for (int i = threadIdx.x; i < key_len * (D / 4); i += 256) store(i / (D / 4), i % (D / 4) * 4, zero, zero);
         return;
     }
@@ -169,7 +222,7 @@ void launch_cross_items(const CrossArgs &a, bool wide, int B, hipStream_t st) {
 
 void launch_cross_dkdv_wide(const CrossArgs &a, hipStream_t st) {
     MOC_PROF("cross_dkdv_wide", st);
-    const int grid = xcd_grid((long long)a.max_items * a.BHk * a.split);
+    const int grid = xcd_grid((long long)a.max_items * a.BHk * a.split) + 2 * kXcds;      // (each kind rounds its slices up)
     if ((long long)a.copies * a.N * wide::RB >= (1ll << 32)) cross_dkdv_wide_kernel<true><<<grid, 256, 0, st>>>(a);
     else cross_dkdv_wide_kernel<false><<<grid, 256, 0, st>>>(a);
 }

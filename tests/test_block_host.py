@@ -88,7 +88,7 @@ def test_rope_refuses(call, want):
     (dict(S=0), -2), (dict(S=129, off=[0] * 129 + [10]), -2), (dict(S=2), -1), (dict(S=2, off=[0, 4, 9]), -3),
     (dict(S=2, off=[1, 4, 10]), -3), (dict(S=3, off=[0, 6, 4, 10]), -3), (dict(S=2, off=[0, 12, 10]), -3), (dict(scale=0.0), -2),
     (dict(scale=-1.0), -2), (dict(scale=float("nan")), -2), (dict(scale=float("inf")), -2), (dict(B=40000), -2), (dict(M=1 << 26), -2),
-    (dict(N=1 << 26), -2), (dict(B=1, H=64, Hk=1, N=1 << 25), -2), (dict(B=1, H=64, Hk=64, M=1 << 25), -2),
+    (dict(N=1 << 26), -2), (dict(N=1 << 25), -2), (dict(B=1, H=64, Hk=1, N=1 << 25), -2), (dict(B=1, H=64, Hk=64, M=1 << 25), -2),
     (dict(t=(None, P, P, P, P)), -1), (dict(t=(P, P, P, P, None)), -1), (dict(t=(P, P + 8, P, P, P)), -8), (dict(ranges=P + 4), -8),
     (dict(ws=None, M=4096), -7), (dict(nbytes=16, M=4096), -7), (dict(ws=P + 4), -8),
 ])
@@ -119,9 +119,9 @@ def test_workspace_sizes():
     assert size(1, 24, 24, 114368, 512, 8, 1) >= 24 * 114368 * 16         # the statistics of the backward
     assert lib.moc_cross_attn_workspace_bytes(1, 1, 1, 1, 1, 128, 1, 0, 0, None) == -1
     # partial sums stay within a bound that does not grow with the call
-    for shape in [(1, 24, 24, 4_000_000, 64), (1, 1, 1, 60_000_000, 1), (3, 8, 2, 1, 2_000_000), (1, 48, 48, 700_000, 9000)]:
+    for shape in [(1, 24, 24, 4_000_000, 64), (1, 1, 1, 60_000_000, 1), (3, 8, 2, 1, 2_000_000), (1, 2, 1, 33_000_000, 100), (1, 48, 48, 700_000, 9000)]:
         stats = shape[0] * shape[1] * shape[3] * 16
-        assert size(*shape, 1, 1) <= stats + (400 << 20), shape
+        assert size(*shape, 1, 1) <= stats + (600 << 20), shape
 
 
 def test_binding_refuses_on_the_host():
