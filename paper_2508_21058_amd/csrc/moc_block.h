@@ -59,13 +59,13 @@ struct CrossArgs {
     int copies;                        // query heads of a key head that are walked one by one
     int Hk, BHk, tiles;                // tiles: query tiles of one copy
     int split, tile_rows;              // tile_rows: queries of a query tile
+    int cut_at;                        // dQ: workgroups from here on cut the states, a sample each
     float scale, scale_log2;
     int32_t q_off[MOC_MAX_CROSS_SEGMENTS + 1];
     int32_t tile_at[MOC_MAX_CROSS_SEGMENTS + 1];      // first query tile of a segment
 };
 // Sizes of a call that follow from its arguments alone, and the places in its workspace (byte offsets).
 void cross_tiles(CrossArgs &a, int tile_rows);                      // cuts the segments into query tiles
-int cross_resident_rows(const CrossArgs &a, int waves);             // queries of an item of the resident passes; 0: too few for them
 struct CrossPlan {
     int split_fwd, split_dq, split_kv;
     bool wide;                         // dK and dV in tiles of 256 states (moc_cross_dkdv.hip)
@@ -74,8 +74,6 @@ struct CrossPlan {
 };
 CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype, bool with_bwd);
 hipError_t launch_cross_fwd(CrossArgs a, int d, int dtype, hipStream_t st);
-// the records of padding rows and, of wide tiles, the items; then the tiles themselves
-void launch_cross_items(const CrossArgs &a, bool wide, int B, hipStream_t st);
 void launch_cross_dkdv_wide(const CrossArgs &a, hipStream_t st);
 hipError_t launch_cross_bwd(CrossArgs a, const CrossPlan &p, int d, int dtype, hipStream_t st);
 

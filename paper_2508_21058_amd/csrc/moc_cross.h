@@ -49,22 +49,26 @@ template <int D> struct Ops<D, bf16_t> {
 template <int D> struct Ops<D, float> {
     typedef f32x4 Frag;
     static constexpr int KS = D / 8, RS = 4, RB = D * 4;
-    int l32, half;
-    __device__ __forceinline__ void init(int lane) { l32 = lane & 31; half = lane >> 5; }
+    // Lane-dependent byte offsets; what depends on the step, the block or the tile goes into the instruction.
+    int row[8];      // row operand of steps s and s + 8
+    int tr[4];       // transposed operand, element e of any step: the swizzle's low bits are the lane's, bit 3 flips neighbouring blocks
+    __device__ __forceinline__ void init(int lane) {
+        const int l32 = lane & 31, half = lane >> 5;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) row[s] = l32 * RB + (((2 * s + half) ^ (l32 & 15)) << 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) tr[e] = (4 * half + e) * RB + (((l32 >> 2) ^ (4 * half + e)) << 4) + (l32 & 3) * 4;
+    }
     static __device__ __forceinline__ int swizzle(int row) { return row & 15; }
     // step s: features 8 s + 4 half .. + 4, one for each of four matrix instructions
     __device__ __forceinline__ Frag frag(const char *tile, int row0, int s) const {
-        return *reinterpret_cast<const f32x4 *>(tile + (row0 + l32) * RB + (((2 * s + half) ^ (l32 & 15)) << 4));
+        return *reinterpret_cast<const f32x4 *>(tile + row[s & 7] + row0 * RB + (s >> 3) * 256);
     }
     // rows 8 s + 4 half + e, the rows of accumulator registers 4 s + e
     __device__ __forceinline__ Frag tfrag(const char *tile, int row0, int b, int s) const {
         f32x4 r;
-        const int f = 32 * b + l32;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int row = row0 + 8 * s + 4 * half + e;
-            r[e] = *reinterpret_cast<const float *>(tile + row * RB + (((f >> 2) ^ (row & 15)) << 4) + (f & 3) * 4);
-        }
+        for (int e = 0; e < 4; ++e) r[e] = *reinterpret_cast<const float *>(tile + tr[e] + (row0 + 8 * s) * RB + (b ^ (s & 1)) * 128);
         return r;
     }
     static __device__ __forceinline__ Frag pack(const f32x16 &acc, int s) { return f32x4{acc[4 * s], acc[4 * s + 1], acc[4 * s + 2], acc[4 * s + 3]}; }
@@ -136,25 +140,72 @@ __device__ __forceinline__ void cross_slice(int &first, int &end, int z, int n, 
     end = min(end, f + (int)((long long)tiles * (z + 1) / n) * tile);
 }
 
-// Keys and values of the resident passes: NW waves share two halves of kHalf rows of each, which fill a compute unit's LDS.
-//   a range of at most 2 kHalf states is loaded once and stays; the waves go through the item's queries, 32 at a time, on their own;
-//   a longer one passes through the halves in turn, a barrier a half, for NW blocks of queries at a time.
-template <int D, int NW> struct Resident {
-    static constexpr int kHalf = 160 * 128 / D, RB = D * 2, HB = kHalf * RB, V0 = 2 * HB, LDS = 4 * HB;
-    static_assert(LDS == 160 * 1024);
-    // rows [0, valid) of K and V, the last repeated up to a whole block of 32, to row `at` of the regions
-    static __device__ __forceinline__ void load(char *smem, const bf16_t *k, const bf16_t *v, int valid, int at, int wave, int lane) {
-        constexpr int GR = RB / 16, RPI = 64 / GR;
-        const int rows = (valid + 31) & ~31;
-        const uint32_t dst = lds_address(smem) + at * RB;
-        for (int n = wave; n * RPI < rows; n += NW) {
-            const int row = n * RPI + lane / GR;
-            const uint32_t off = (uint32_t)min(row, valid - 1) * RB + (((lane % GR) ^ SwTile<D>::sw(row)) << 4);
-            cross_copy16(k, off, dst + n * 1024);
-            cross_copy16(v, off, dst + V0 + n * 1024);
+// Cuts the states of sample b into the tiles of the wide key-stationary pass: a workgroup of 256 threads. The tiles of segments come
+// first.
+constexpr int kCuts = 2 * MOC_MAX_CROSS_SEGMENTS + 2;
+struct CutLds {
+    int first[MOC_MAX_CROSS_SEGMENTS], end[MOC_MAX_CROSS_SEGMENTS], cut[kCuts], sorted[kCuts], tile_at[kCuts];
+    uint32_t segments[kCuts][MOC_MAX_CROSS_SEGMENTS / 32];
+};
+__device__ __forceinline__ void cross_cut(const CrossArgs &a, int b, CutLds &m) {
+    auto &first = m.first, &end = m.end;
+    auto &cut = m.cut, &sorted = m.sorted, &tile_at = m.tile_at;
+    auto &segments = m.segments;
+    const int tid = threadIdx.x, S = a.n_seg;
+    const int n = 2 * S + 2;
+    if (tid < S) {
+        CrossRange r = cross_range(a, b, tid);
+        if (r.end <= r.first || a.q_off[tid + 1] == a.q_off[tid]) r.first = r.end = 0;
+        first[tid] = cut[2 * tid] = r.first;
+        end[tid] = cut[2 * tid + 1] = r.end;
+    }
+    if (tid == 0) { cut[n - 2] = 0; cut[n - 1] = a.M; }
+    __syncthreads();
+    for (int i = tid; i < n; i += 256) {
+        const int x = cut[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += cut[j] < x || (cut[j] == x && j < i);
+        sorted[rank] = x;
+    }
+    __syncthreads();
+    // piece i: states [sorted[i], sorted[i + 1]), of a range or of none; its tiles from tile_at[i] on, those of ranges first
+    for (int i = tid; i < n; i += 256) {
+        for (int w = 0; w < MOC_MAX_CROSS_SEGMENTS / 32; ++w) {
+            uint32_t in = 0;
+            for (int s = 32 * w; s < min(32 * w + 32, S) && i + 1 < n; ++s)
+                if (first[s] <= sorted[i] && end[s] >= sorted[i + 1]) in |= 1u << (s & 31);
+            segments[i][w] = in;
         }
     }
-};
+    __syncthreads();
+    auto attended = [&](int i) { return (segments[i][0] | segments[i][1] | segments[i][2] | segments[i][3]) != 0; };
+    static_assert(MOC_MAX_CROSS_SEGMENTS == 128, "four words of segments");
+    for (int i = tid; i + 1 < n; i += 256) {
+        const bool mine = attended(i);
+        int at = 0;
+        for (int j = 0; j + 1 < n; ++j) {
+            const bool other = attended(j);
+            if (other == mine ? j < i : other) at += (sorted[j + 1] - sorted[j] + kWideTile - 1) / kWideTile;
+        }
+        tile_at[i] = at;
+    }
+    __syncthreads();
+    CrossKeys *out = a.items + (size_t)b * a.max_items;
+    int live = 0, total = 0;
+    for (int i = 0; i + 1 < n; ++i) {
+        const int tiles = (sorted[i + 1] - sorted[i] + kWideTile - 1) / kWideTile;
+        total += tiles;
+        live += attended(i) ? tiles : 0;
+        for (int t = tid; t < tiles; t += 256) {
+            CrossKeys k{};
+            k.start = sorted[i] + t * kWideTile;
+            k.len = min(kWideTile, sorted[i + 1] - k.start);
+            for (int w = 0; w < MOC_MAX_CROSS_SEGMENTS / 32; ++w) k.segments[w] = segments[i][w];
+            out[tile_at[i] + t] = k;
+        }
+    }
+    if (tid == 0) a.item_counts[b] = CrossCount{live, total - live};
+}
 
 // A wave's 32 x D transposed accumulator (lane: row l32, four-feature pieces) times `scale` to the float rows at `out`.
 template <int D> __device__ __forceinline__ void store_rows_f32(const f32x16 *acc, float scale, float *row, int half) {

@@ -17,12 +17,16 @@ __device__ __forceinline__ void store_record(const CrossArgs &a, const CrossItem
 }
 
 template <int D, typename T>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void cross_dq_kernel(CrossArgs a) {
+__global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossArgs a) {
     typedef Ops<D, T> O;
     constexpr int BN = sizeof(T) == 2 ? 64 : 32, DB = D / 32;
     constexpr int TB = BN * O::RB;
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
+    // what the key-stationary pass needs besides the records: that of padding rows and, of wide tiles, the list of them
+    if (blockIdx.x == 0 && tid < 4) a.stats[4 * (size_t)a.rows + tid] = tid ? 0.f : INFINITY;
+    if constexpr (D == 128 && sizeof(T) == 2)
+        if ((int)blockIdx.x >= a.cut_at) { cross_cut(a, blockIdx.x - a.cut_at, *reinterpret_cast<CutLds *>(smem)); return; }
     int logical;
     if (!xcd_remap((long long)a.tiles * a.copies * a.BHk * a.split, logical)) return;
     const int z = logical % a.split;
@@ -145,7 +149,7 @@ __device__ __forceinline__ void make_stream(const CrossArgs &a, int b, int key0,
 }
 
 template <int D, typename T>
-__global__ __launch_bounds__(256, D == 64 && sizeof(T) == 2 ? 2 : 1) void cross_dkdv_kernel(CrossArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkdv_kernel(CrossArgs a) {
     typedef Ops<D, T> O;
     constexpr int DB = D / 32, TB = kStreamRows * O::RB;
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB];          // Q, dO, twice
@@ -263,6 +267,7 @@ __global__ __launch_bounds__(256) void cross_sum_kernel(const float *__restrict_
     const long long words = rows * W * (out1 ? 2 : 1), i = (long long)blockIdx.x * 256 + threadIdx.x;
     if (i >= words) return;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
     for (int z = 0; z < split; ++z) s += *reinterpret_cast<const f32x4 *>(part + (z * words + i) * 4);
     const long long row = out1 ? i / (2 * W) : i / W;
     const int x = (int)(out1 ? i % (2 * W) : i % W);
@@ -271,12 +276,12 @@ __global__ __launch_bounds__(256) void cross_sum_kernel(const float *__restrict_
 }
 
 template <int D, typename T> static void bwd_dispatch(CrossArgs a, const CrossPlan &p, hipStream_t st) {
-    launch_cross_items(a, p.wide, a.BHk / a.Hk, st);
     cross_tiles(a, kCrossRows);
     a.split = p.split_dq;
     {
         MOC_PROF("cross_dq", st);
-        cross_dq_kernel<D, T><<<xcd_grid((long long)a.tiles * a.copies * a.BHk * a.split), 256, 0, st>>>(a);
+        a.cut_at = xcd_grid((long long)a.tiles * a.copies * a.BHk * a.split);
+        cross_dq_kernel<D, T><<<a.cut_at + (p.wide ? a.BHk / a.Hk : 0), 256, 0, st>>>(a);
     }
     if (a.split > 1) {
         MOC_PROF("cross_sum", st);

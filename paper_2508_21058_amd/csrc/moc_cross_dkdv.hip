@@ -3,76 +3,11 @@
 // That pass has no masks: every query of its stream attends every key of its tile. So a sample's states are cut where a range of one
 // of its segments begins or ends, and the pieces into tiles; a tile streams the queries of the segments whose ranges hold it, all of
 // them or, where the call has few tiles, one part in `split`. States of no range are tiles without segments, whose gradients are zero.
-// Ranges are on the device, so the cutting is too: a workgroup a sample, in the launch that also writes the padding record.
+// Ranges are on the device, so the cutting is too (cross_cut).
 #include "moc_block.h"
 #include "moc_dkdv_wide.h"
 
 namespace moc {
-
-constexpr int kCuts = 2 * MOC_MAX_CROSS_SEGMENTS + 2;
-__global__ __launch_bounds__(256) void cross_items_kernel(CrossArgs a, bool wide) {
-    const int tid = threadIdx.x, b = blockIdx.x, S = a.n_seg;
-    if (b == 0 && tid < 4) a.stats[4 * (size_t)a.rows + tid] = tid ? 0.f : INFINITY;
-    if (!wide) return;
-    __shared__ int first[MOC_MAX_CROSS_SEGMENTS], end[MOC_MAX_CROSS_SEGMENTS], cut[kCuts], sorted[kCuts], tile_at[kCuts];
-    __shared__ uint32_t segments[kCuts][MOC_MAX_CROSS_SEGMENTS / 32];
-    const int n = 2 * S + 2;
-    if (tid < S) {
-        CrossRange r = {0, a.M};
-        if (a.ranges) r = a.ranges[(size_t)b * S + tid];
-        r.first = max(r.first, 0);
-        r.end = min(r.end, a.M);
-        if (r.end <= r.first || a.q_off[tid + 1] == a.q_off[tid]) r.first = r.end = 0;
-        first[tid] = cut[2 * tid] = r.first;
-        end[tid] = cut[2 * tid + 1] = r.end;
-    }
-    if (tid == 0) { cut[n - 2] = 0; cut[n - 1] = a.M; }
-    __syncthreads();
-    for (int i = tid; i < n; i += 256) {
-        const int x = cut[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += cut[j] < x || (cut[j] == x && j < i);
-        sorted[rank] = x;
-    }
-    __syncthreads();
-    // piece i: states [sorted[i], sorted[i + 1]), of a range or of none; its tiles from tile_at[i] on, those of ranges first
-    for (int i = tid; i < n; i += 256) {
-        for (int w = 0; w < MOC_MAX_CROSS_SEGMENTS / 32; ++w) {
-            uint32_t in = 0;
-            for (int s = 32 * w; s < min(32 * w + 32, S) && i + 1 < n; ++s)
-                if (first[s] <= sorted[i] && end[s] >= sorted[i + 1]) in |= 1u << (s & 31);
-            segments[i][w] = in;
-        }
-    }
-    __syncthreads();
-    auto attended = [&](int i) { return (segments[i][0] | segments[i][1] | segments[i][2] | segments[i][3]) != 0; };
-    static_assert(MOC_MAX_CROSS_SEGMENTS == 128, "four words of segments");
-    for (int i = tid; i + 1 < n; i += 256) {
-        const bool mine = attended(i);
-        int at = 0;
-        for (int j = 0; j + 1 < n; ++j) {
-            const bool other = attended(j);
-            if (other == mine ? j < i : other) at += (sorted[j + 1] - sorted[j] + kWideTile - 1) / kWideTile;
-        }
-        tile_at[i] = at;
-    }
-    __syncthreads();
-    CrossKeys *out = a.items + (size_t)b * a.max_items;
-    int live = 0, total = 0;
-    for (int i = 0; i + 1 < n; ++i) {
-        const int tiles = (sorted[i + 1] - sorted[i] + kWideTile - 1) / kWideTile;
-        total += tiles;
-        live += attended(i) ? tiles : 0;
-        for (int t = tid; t < tiles; t += 256) {
-            CrossKeys k{};
-            k.start = sorted[i] + t * kWideTile;
-            k.len = min(kWideTile, sorted[i + 1] - k.start);
-            for (int w = 0; w < MOC_MAX_CROSS_SEGMENTS / 32; ++w) k.segments[w] = segments[i][w];
-            out[tile_at[i] + t] = k;
-        }
-    }
-    if (tid == 0) a.item_counts[b] = CrossCount{live, total - live};
-}
 
 namespace wide {
 // Pieces of contiguous queries: the segments of a tile, for every query head of the group in turn, of them `stages` stages.
@@ -213,11 +148,6 @@ __global__ __launch_bounds__(256, 1) void cross_dkdv_wide_kernel(CrossArgs a) {
     const size_t states = (size_t)bhk * a.M * RB;
     dkdv_wide<BIG>(smem, src, n_st, qbase, dobase, static_cast<const char *>(a.k) + states, static_cast<const char *>(a.v) + states, key_start,
                    key_len, a.scale, a.scale_log2, store);
-}
-
-void launch_cross_items(const CrossArgs &a, bool wide, int B, hipStream_t st) {
-    MOC_PROF("cross_items", st);
-    cross_items_kernel<<<wide ? B : 1, 256, 0, st>>>(a, wide);
 }
 
 void launch_cross_dkdv_wide(const CrossArgs &a, hipStream_t st) {

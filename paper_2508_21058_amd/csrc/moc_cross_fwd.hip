@@ -11,7 +11,7 @@ namespace moc {
 // In bf16 three workgroups share a compute unit (168 registers, tiles of 32 states): 114k queries of 24 heads, eight shots of captions of 100 to 512
 // states 569 -> 506 us against two of 64-state tiles (of 32: 594), 33k queries against 4,357 states 1,886 -> 1,835.
 template <int D, typename T>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 1) void cross_fwd_kernel(CrossArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cross_fwd_kernel(CrossArgs a) {
     typedef Ops<D, T> O;
     constexpr int BN = 32, DB = D / 32;
     constexpr int TB = BN * O::RB;
