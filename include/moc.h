@@ -356,8 +356,8 @@ typedef struct moc_rope_plan {
  *   q_weight, k_weight  DEVICE [d] float or NULL (ones); eps finite and >= 0.
  *   q_out, k_out, v_out DEVICE out, contiguous [B, heads, N, d], NULL where the input is NULL.
  * Rows are in float, sums too; results are rounded once, to `dtype`. N here is free of any
- * layout (an encoder's states have their own); B * heads * N < 2^31. Outputs must not
- * overlap inputs.
+ * layout (an encoder's states have their own); B * N < 2^28, B * heads * N < 2^31. Outputs
+ * must not overlap inputs.
  *
  * moc_qk_norm_rope_bwd: gradients of the same call. d_q_out, d_k_out, d_v_out (DEVICE in,
  * contiguous like the outputs) -> dq, dk, dv (DEVICE out, moc_rows: token-major, or slices of
@@ -402,13 +402,14 @@ int moc_rope(int32_t B, int32_t N, int32_t H, int32_t d, int dtype, const moc_ro
  *   o DEVICE out [B,H,N,d];  lse DEVICE out [B,H,N] float.
  * MOC_BF16: products on bf16 matrix cores, softmax and sums in float, probabilities and dS rounded to
  * bf16 for the second products. MOC_F32: everything in float, the products on float matrix cores (unlike
- * moc_attn_*). softmax_scale finite and > 0. B * H <= 65535, H / Hk * N and M < 2^26, B * H * N and B * Hk * M < 2^31.
+ * moc_attn_*). softmax_scale finite and > 0. B * H <= 65535, H / Hk * N and M < 2^26, B * H * N and B * Hk * M < 2^31,
+ * B * H * (N / 128 + S) and B * Hk * (M / 256 + 2 S) < 2^24 - 2048.
  *
  * moc_cross_attn_bwd: dq [B,H,N,d], dk, dv [B,Hk,M,d] (fully overwritten; dk and dv are summed over the
  * query heads of a key head) from the forward's o and lse and d_o [B,H,N,d]. Every sum has a fixed order: same
  * input, same bits. workspace: moc_cross_attn_workspace_bytes(..., with_bwd) bytes, which
- * serve both calls; nothing is kept in it between calls. No call allocates or waits, so they
- * can be captured into a HIP graph.
+ * serve both calls; nothing is kept in it between calls, and calls that may run side by side need one
+ * each. No call allocates or waits, so they can be captured into a HIP graph.
  */
 #define MOC_MAX_CROSS_SEGMENTS 128
 int moc_cross_attn_workspace_bytes(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t d, int32_t S, int dtype,

@@ -905,7 +905,9 @@ int check_heads(int32_t B, int32_t N, int32_t H, int32_t d, int dtype) {
     if (dtype != MOC_BF16 && dtype != MOC_F32) return fail(MOC_ERR_DTYPE, "dtype must be MOC_BF16 or MOC_F32");
     if (B <= 0 || N <= 0 || H <= 0) return fail(MOC_ERR_SHAPE, "B, N and the heads must be positive");
     if (d != 64 && d != 128) return fail(MOC_ERR_SHAPE, "d must be 64 or 128");
-    if ((long long)B * N >= (1LL << 31) || (long long)B * N * H >= (1LL << 31)) return fail(MOC_ERR_SHAPE, "B * heads * N must be < 2^31");
+    // (a launch has fewer than 2^32 threads: sixteen a token of 128 features)
+    if ((long long)B * N >= (1LL << 28) || (long long)B * N * H >= (1LL << 31))
+        return fail(MOC_ERR_SHAPE, "B * N must be < 2^28 and B * heads * N < 2^31");
     return MOC_OK;
 }
 
@@ -956,6 +958,9 @@ int check_cross(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t 
     if ((long long)N * (H / Hk) >= (1 << 26) || M >= (1 << 26)) return fail(MOC_ERR_SHAPE, "H / Hk * N and M must be < 2^26");
     if ((long long)B * H * N >= (1LL << 31) || (long long)B * Hk * M >= (1LL << 31))
         return fail(MOC_ERR_SHAPE, "B * H * N and B * Hk * M must be < 2^31");
+    // (a launch has fewer than 2^32 threads, 256 a workgroup)
+    const long long tiles = (long long)B * H * ((N + 127) / 128 + S - 1), pieces = (long long)B * Hk * (M / 256 + 2 * S + 1);
+    if (tiles >= (1 << 24) - 1024 || pieces >= (1 << 24) - 1024) return fail(MOC_ERR_SHAPE, "too many tiles: B * H * (N / 128 + S) or B * Hk * (M / 256 + 2 S)");
     return MOC_OK;
 }
 

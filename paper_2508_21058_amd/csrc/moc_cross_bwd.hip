@@ -331,7 +331,8 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
         const long long tiles = (long long)B * Hk * ((M + kWideTile - 1) / kWideTile);
         const double stages = std::max(1.0, (double)per_head / S / 16), sums = (double)states * d * 16 / 6e6;
         double best = 0;
-        for (long long s = 1; s <= std::min(64LL, (per_head + 255) / 256) && (s == 1 || s * states * d * 8 <= 512 << 20); ++s) {
+        for (long long s = 1; s <= std::min(64LL, (per_head + 255) / 256) &&
+                              (s == 1 || (s * states * d * 8 <= 512 << 20 && (long long)B * Hk * p.max_items * s < 1 << 20)); ++s) {
             const double item = 0.75 * stages / s + 6, rounds = (double)((tiles * s + kComputeUnits - 1) / kComputeUnits);
             const double us = std::max(rounds, 1.2 * tiles * s / kComputeUnits) * item + (s > 1 ? s * sums + 5 : 0);
             if (s == 1 || us < best) { best = us; p.split_kv = (int)s; }

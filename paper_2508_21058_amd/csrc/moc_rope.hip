@@ -13,22 +13,29 @@
 
 namespace moc {
 
-constexpr int kRowThreads = 256, kRowWgs = 1024;      // workgroups wanted: four a compute unit
+constexpr int kRowThreads = 256;
+// Workgroups wanted. The forward takes many short ones, so that the last round of the chip is short, but at least eight heads each where there are
+// enough tokens, since each forms the angles anew: 33k tokens of 24 heads 91 us with a workgroup per 16 tokens (2,080 of them, 2,048 at a time),
+// 85 with three, 83 with eight; 6k tokens (q, k and v) 41.5 with three, 43.5 with 18, 55.5 with 36. The backward's take
+// several blocks of tokens one after the other, so that the weights' partial sums are few: 1,024, 2,048, 4,096 of them 60, 61, 77 us (two samples of
+// 16k tokens, twelve and four heads of 64).
+constexpr int kRowWgs = 6144, kRowWgsFew = 512, kRowHeadsMin = 8, kRowWgsBwd = 1024;
 
 RowGrid row_grid(int B, int N, int heads_total, int d, bool bwd) {
     RowGrid g;
     g.tokens = kRowThreads / (d / 8);
     g.blocks = (int)(((long long)B * N + g.tokens - 1) / g.tokens);
-    g.groups = std::max(1, std::min(heads_total, (kRowWgs + g.blocks - 1) / g.blocks));
+    auto groups = [&](int want, int most) { return std::max(1, std::min(most, (want + g.blocks - 1) / g.blocks)); };
+    g.groups = bwd ? groups(kRowWgsBwd, heads_total)
+                   : std::max(groups(kRowWgs, heads_total / kRowHeadsMin), groups(kRowWgsFew, heads_total));
     g.per_group = (heads_total + g.groups - 1) / g.groups;
     g.groups = (heads_total + g.per_group - 1) / g.per_group;
-    // the backward's workgroups take several blocks of tokens, so that the weights' partial sums are few
-    g.grid_x = bwd ? std::min(g.blocks, std::max(1, kRowWgs / g.groups)) : g.blocks;
+    g.grid_x = bwd ? std::min(g.blocks, std::max(1, kRowWgsBwd / g.groups)) : g.blocks;
     return g;
 }
 
-// (no call has more than kRowWgs workgroups that sum)
-size_t rows_partial_bytes(int d) { return (size_t)kRowWgs * 2 * d * sizeof(float); }
+// (no call has more than kRowWgsBwd workgroups that sum)
+size_t rows_partial_bytes(int d) { return (size_t)kRowWgsBwd * 2 * d * sizeof(float); }
 
 // Sum over the LPR (8 or 16) neighbouring lanes of a row, in all of them.
 template <int CTRL> __device__ __forceinline__ float lane_add(float v) {

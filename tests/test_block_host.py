@@ -50,7 +50,7 @@ def cross_bwd(t=(P,) * 6, g=(P,) * 3, ws=P, nbytes=1 << 30, scale=0.1, S=1, off=
 
 
 @pytest.mark.parametrize("call,want", [
-    (dict(d=96), -2), (dict(B=0), -2), (dict(N=0), -2), (dict(H=0), -2), (dict(Hk=-1), -2), (dict(N=1 << 30, B=2), -2),
+    (dict(d=96), -2), (dict(B=0), -2), (dict(N=0), -2), (dict(H=0), -2), (dict(Hk=-1), -2), (dict(N=1 << 30, B=2), -2), (dict(N=1 << 27, B=2, H=1, Hk=1), -2),
     (dict(N=1 << 24, H=128), -2), (dict(dt=2), -6), (dict(eps=-1e-6), -2), (dict(eps=float("nan")), -2), (dict(eps=float("inf")), -2),
     (dict(q=None, k=None, v=None, out=(None,) * 3), -1), (dict(q=None), -1), (dict(out=(P, None, P)), -1),
     (dict(q=rows(data=None)), -1), (dict(q=rows(data=P + 8)), -8), (dict(k=rows(n=132)), -8), (dict(v=rows(h=4)), -8),
@@ -89,6 +89,7 @@ def test_rope_refuses(call, want):
     (dict(S=2, off=[1, 4, 10]), -3), (dict(S=3, off=[0, 6, 4, 10]), -3), (dict(S=2, off=[0, 12, 10]), -3), (dict(scale=0.0), -2),
     (dict(scale=-1.0), -2), (dict(scale=float("nan")), -2), (dict(scale=float("inf")), -2), (dict(B=40000), -2), (dict(M=1 << 26), -2),
     (dict(N=1 << 26), -2), (dict(N=1 << 25), -2), (dict(B=1, H=64, Hk=1, N=1 << 25), -2), (dict(B=1, H=64, Hk=64, M=1 << 25), -2),
+    (dict(B=65535, H=1, Hk=1, N=1, S=128, off=[0] * 128 + [1]), -2), (dict(B=3000, H=16, Hk=16, N=40000, S=128, off=[0] * 128 + [40000]), -2),
     (dict(t=(None, P, P, P, P)), -1), (dict(t=(P, P, P, P, None)), -1), (dict(t=(P, P + 8, P, P, P)), -8), (dict(ranges=P + 4), -8),
     (dict(ws=None, M=4096), -7), (dict(nbytes=16, M=4096), -7), (dict(ws=P + 4), -8),
 ])

@@ -90,6 +90,7 @@ def check(B, H, Hk, N, M, d, dtype, ranges=None, offs=None, scale=None, seed=0):
     o, lse = mb.cross_attn_fwd(q, k, v, workspace=ws, **kw)
     near("o", o, ref["o"])
     near("lse", lse, ref["lse"])
+    assert (o[(lse == -math.inf)] == 0).all()
     ws.fill_(255)
     grads = mb.cross_attn_bwd(q, k, v, o, lse, d_o, workspace=ws, **kw)
     for n, g in zip(("dq", "dk", "dv"), grads):
@@ -134,6 +135,36 @@ def test_many_segments_and_another_scale():
     offs = [N * s // S for s in range(S + 1)]
     ranges = [[(4 * s, 4 * s + 1 + s % 12) for s in range(S)]]
     check(1, 2, 1, N, M, 64, torch.bfloat16, ranges=ranges, offs=offs, scale=0.31)
+
+
+def test_more_samples_than_a_wave_has_lanes():
+    """130 samples, most of them without a state."""
+    B, M = 130, 40
+    ranges = [[(0, 0 if b % 3 else 1 + b % M)] for b in range(B)]
+    check(B, 2, 1, 9, M, 128, torch.bfloat16, ranges=ranges)
+
+
+def random_case(seed):
+    g = np.random.default_rng(seed)
+    B, Hk, G, S = int(g.integers(1, 4)), int(g.integers(1, 4)), int(g.integers(1, 4)), int(g.choice([1, 1, 2, 5, 40]))
+    N, M = (int(2 ** g.uniform(0, top)) for top in (10, 10.5))
+    d, dtype = int(g.choice([64, 128, 128])), torch.bfloat16 if g.random() < 0.7 else torch.float32
+    offs = [0] + sorted(g.integers(0, N + 1, S - 1).tolist()) + [N]
+    kind = g.random()
+    def one(s):
+        if kind < 0.3:
+            return 0, int(g.integers(0, M + 1))
+        if kind < 0.6:
+            return M * s // S, M * (s + 1) // S
+        a, b = g.integers(-3, M + 4, 2)
+        return int(a), int(b)
+    ranges = None if kind > 0.9 else [[one(s) for s in range(S)] for _ in range(B)]
+    return dict(B=B, H=Hk * G, Hk=Hk, N=N, M=M, d=d, dtype=dtype, ranges=ranges, offs=offs if S > 1 else None, seed=seed)
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_random_shapes(seed):
+    check(**random_case(seed))
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
