@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Tuple
 
 import numpy as np
@@ -401,10 +402,6 @@ MOC_MAX_AXES = 4
 MOC_MAX_CROSS_SEGMENTS = 128
 
 
-class _Rows(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_h", C.c_int64), ("stride_n", C.c_int64)]
-
-
 class _RopePlan(C.Structure):
     _fields_ = [("positions", C.c_void_p), ("freq", C.c_void_p), ("n_axes", C.c_int32),
                 ("axis_pairs", C.c_int32 * MOC_MAX_AXES), ("halves", C.c_int32)]
@@ -454,22 +451,27 @@ def _on(first: torch.Tensor, *others):
     return None if torch._C._cuda_getDevice() == dev.index else dev.index, torch._C._cuda_getCurrentRawStream(dev.index)
 
 
-def _call(where: str, device: Optional[int], *args):
+def _call(fn, device: Optional[int], *args):
     if device is None:
-        rc = getattr(_lib, where)(*args)
+        rc = fn(*args)
     else:
         with torch.cuda.device(device):
-            rc = getattr(_lib, where)(*args)
+            rc = fn(*args)
     if rc != 0:
-        raise MocError(rc, where)
+        raise MocError(rc, fn.__name__)
 
 
-def _rows(t: torch.Tensor, token_major: bool):
-    """moc_rows of a [B, N, heads, d] (token_major) or [B, heads, N, d] tensor."""
+_ROWS = struct.Struct("Pqqq")           # moc_rows; a bytes object passes as a pointer to it
+
+
+def _rows(t: Optional[torch.Tensor], token_major: bool):
+    """moc_rows of a [B, N, heads, d] (token_major) or [B, heads, N, d] tensor; None stays None."""
+    if t is None:
+        return None
     s = t.stride()
     if len(s) != 4 or s[3] != 1:
         raise ValueError("tensors must be 4-dimensional with contiguous features")
-    return _Rows(t.data_ptr(), s[0], s[2], s[1]) if token_major else _Rows(t.data_ptr(), s[0], s[1], s[2])
+    return _ROWS.pack(t.data_ptr(), s[0], s[2], s[1]) if token_major else _ROWS.pack(t.data_ptr(), s[0], s[1], s[2])
 
 
 def _same_dtype(first: torch.Tensor, *others):
@@ -523,7 +525,7 @@ def qk_norm_rope(q, k=None, v=None, q_weight=None, k_weight=None, rope: Optional
     [B, N, heads, d] (any strides) to contiguous head-major [B, heads, N, d]; v is moved as it is. Any of q, k, v may be
     None. -> (q, k, v), None where the input is None. `out`: the three tensors to fill."""
     B, N, H, Hk, d, some = _token_shape(q, k, v)
-    lib()
+    l = lib()
     dt = _same_dtype(some, q, k, v)
     device, stream = _on(some, q, k, v, q_weight, k_weight)
     if out is None:
@@ -534,8 +536,8 @@ def qk_norm_rope(q, k=None, v=None, q_weight=None, k_weight=None, rope: Optional
                 raise ValueError("out must hold a tensor for each of q, k and v that is given")
             if o is not None:
                 _need_like(o, (B, t.shape[2], N, d), some)
-    rows = [None if t is None else C.byref(_rows(t, True)) for t in (q, k, v)]
-    _call("moc_qk_norm_rope", device, B, N, H, Hk, d, dt, *rows, _weight(q_weight, d), _weight(k_weight, d), eps,
+    rows = _rows(q, True), _rows(k, True), _rows(v, True)
+    _call(l.moc_qk_norm_rope, device, B, N, H, Hk, d, dt, *rows, _weight(q_weight, d), _weight(k_weight, d), eps,
           _plan(rope, N, some.device), *_ptrs(*out), stream)
     return tuple(out)
 
@@ -553,7 +555,7 @@ def qk_norm_rope_bwd(q, k, d_q_out, d_k_out, d_v_out=None, q_weight=None, k_weig
     -> dq, dk, dv (token-major [B, N, heads, d]) and dq_weight, dk_weight ([d] float32); None where nothing was given.
     `out` = (dq, dk, dv) tensors to fill, of any strides."""
     B, N, H, Hk, d, some = _token_shape(q, k, None if d_v_out is None else d_v_out.transpose(1, 2))
-    lib()
+    l = lib()
     grads = (d_q_out, d_k_out, d_v_out)
     dt = _same_dtype(some, q, k, *grads)
     device, stream = _on(some, q, k, *grads, q_weight, k_weight, workspace)
@@ -570,9 +572,8 @@ def qk_norm_rope_bwd(q, k, d_q_out, d_k_out, d_v_out=None, q_weight=None, k_weig
     dw = torch.empty((2, d), dtype=torch.float32, device=some.device)
     dqw, dkw = None if q is None else dw[0], None if k is None else dw[1]
     ws = workspace if workspace is not None else qk_norm_rope_workspace(B, N, H, Hk, d, some.dtype, some.device)
-    rows = [None if t is None else C.byref(_rows(t, True)) for t in (q, k, *out)]
-    _call("moc_qk_norm_rope_bwd", device, B, N, H, Hk, d, dt, *rows[:2], _weight(q_weight, d), _weight(k_weight, d), eps,
-          _plan(rope, N, some.device), *_ptrs(*grads), *rows[2:], *_ptrs(dqw, dkw), ws.data_ptr(), ws.numel(), stream)
+    _call(l.moc_qk_norm_rope_bwd, device, B, N, H, Hk, d, dt, _rows(q, True), _rows(k, True), _weight(q_weight, d), _weight(k_weight, d), eps,
+          _plan(rope, N, some.device), *_ptrs(*grads), *[_rows(o, True) for o in out], *_ptrs(dqw, dkw), ws.data_ptr(), ws.numel(), stream)
     return (*out, dqw, dkw)
 
 
@@ -581,14 +582,14 @@ def apply_rope(x: torch.Tensor, rope: RopePlan, inverse: bool = False, out: Opti
     the rotation. `out` may be x itself (in place) or a tensor of any strides; without it the result is contiguous."""
     rx = _rows(x, False)
     B, H, N, d = x.shape
-    lib()
+    l = lib()
     device, stream = _on(x, out)
     if out is None:
         out = torch.empty((B, H, N, d), dtype=x.dtype, device=x.device)
     elif out.shape != x.shape or out.dtype != x.dtype:
         raise ValueError("out must have the shape and dtype of x")
-    _call("moc_rope", device, B, N, H, d, _dtype_code(x), C.byref(rx), _plan(rope, N, x.device), int(bool(inverse)),
-          C.byref(_rows(out, False)), stream)
+    _call(l.moc_rope, device, B, N, H, d, _dtype_code(x), rx, _plan(rope, N, x.device), int(bool(inverse)),
+          _rows(out, False), stream)
     return out
 
 
@@ -626,7 +627,7 @@ def cross_attn_fwd(q, k, v, kv_ranges: Optional[torch.Tensor] = None, q_offsets=
     q_offsets [S+1] (host) cuts the queries into segments, kv_ranges [B, S, 2] int32 (device) says which states
     [first, end) a segment of a sample attends; an empty range gives o = 0, lse = -inf."""
     B, H, Hk, N, M, d, S, off = _cross_shape(q, k, v, kv_ranges, q_offsets)
-    lib()
+    l = lib()
     dt = _same_dtype(q, k, v)
     device, stream = _on(q, k, v, kv_ranges, workspace)
     ws = workspace if workspace is not None else cross_attn_workspace(B, H, Hk, N, M, d, q.dtype, False, S, q.device)
@@ -636,7 +637,7 @@ def cross_attn_fwd(q, k, v, kv_ranges: Optional[torch.Tensor] = None, q_offsets=
         o, lse = out
         _need_like(o, q.shape, q)
         _need_lse(lse, q)
-    _call("moc_cross_attn_fwd", device, B, H, Hk, N, M, d, dt, q.data_ptr(), k.data_ptr(), v.data_ptr(), S,
+    _call(l.moc_cross_attn_fwd, device, B, H, Hk, N, M, d, dt, q.data_ptr(), k.data_ptr(), v.data_ptr(), S,
           None if off is None else off.ctypes.data, None if kv_ranges is None else kv_ranges.data_ptr(),
           d ** -0.5 if scale is None else scale, o.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(), stream)
     return o, lse
@@ -646,7 +647,7 @@ def cross_attn_bwd(q, k, v, o, lse, d_o, kv_ranges: Optional[torch.Tensor] = Non
                    workspace: Optional[torch.Tensor] = None, out=None):
     """-> dq [B, H, N, d], dk, dv [B, Hk, M, d] from the forward's o and lse and the gradient d_o of o."""
     B, H, Hk, N, M, d, S, off = _cross_shape(q, k, v, kv_ranges, q_offsets)
-    lib()
+    l = lib()
     dt = _same_dtype(q, k, v, o, d_o)
     device, stream = _on(q, k, v, kv_ranges, workspace)
     _need_like(o, q.shape, q)
@@ -660,7 +661,7 @@ def cross_attn_bwd(q, k, v, o, lse, d_o, kv_ranges: Optional[torch.Tensor] = Non
         _need_like(dq, q.shape, q)
         _need_like(dk, k.shape, q)
         _need_like(dv, k.shape, q)
-    _call("moc_cross_attn_bwd", device, B, H, Hk, N, M, d, dt, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+    _call(l.moc_cross_attn_bwd, device, B, H, Hk, N, M, d, dt, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
           lse.data_ptr(), d_o.data_ptr(), S, None if off is None else off.ctypes.data,
           None if kv_ranges is None else kv_ranges.data_ptr(), d ** -0.5 if scale is None else scale, dq.data_ptr(),
           dk.data_ptr(), dv.data_ptr(), ws.data_ptr(), ws.numel(), stream)

@@ -338,7 +338,7 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
             if (s == 1 || us < best) { best = us; p.split_kv = (int)s; }
         }
     } else {
-        p.split_kv = split((long long)B * Hk * ((M + kCrossKeys - 1) / kCrossKeys), 512, (per_head + 127) / 128);
+        p.split_kv = split((long long)B * Hk * ((M + kCrossKeys - 1) / kCrossKeys), 512, (per_head + 63) / 64);
     }
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t x = at; at += up(bytes); return x; };

@@ -12,7 +12,7 @@ P = 0x10000
 
 
 def rows(data=P, b=1 << 20, h=128, n=1 << 12):
-    return mb._Rows(data, b, h, n)
+    return mb._ROWS.pack(data or 0, b, h, n)
 
 
 def plan(positions=P, freq=P, n_axes=3, pairs=(22, 21, 21), halves=0):
@@ -20,7 +20,7 @@ def plan(positions=P, freq=P, n_axes=3, pairs=(22, 21, 21), halves=0):
 
 
 def ref(x):
-    return None if x is None else C.byref(x)
+    return x if x is None or isinstance(x, bytes) else C.byref(x)
 
 
 def norm(B=1, N=8, H=2, Hk=2, d=128, dt=0, q=rows(), k=rows(), v=rows(), wq=P, wk=P, eps=1e-6, rope=plan(), out=(P, P, P)):
