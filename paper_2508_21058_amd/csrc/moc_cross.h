@@ -21,6 +21,7 @@ template <int D> struct Ops<D, bf16_t> {
     static constexpr int KS = D / 16, RS = 2, RB = D * 2;
     LaneOffs<D> lo;
     __device__ __forceinline__ void init(int lane) { lo.init(lane); }
+    __device__ __forceinline__ void pin() { lo.pin(); }      // (see LaneOffs)
     __device__ __forceinline__ Frag frag(const char *tile, int row0, int s) const {
         return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(tile + lo.row[s] + row0 * RB));
     }
@@ -58,6 +59,12 @@ template <int D> struct Ops<D, float> {
         for (int s = 0; s < 8; ++s) row[s] = l32 * RB + (((2 * s + half) ^ (l32 & 15)) << 4);
 #pragma unroll
         for (int e = 0; e < 4; ++e) tr[e] = (4 * half + e) * RB + (((l32 >> 2) ^ (4 * half + e)) << 4) + (l32 & 3) * 4;
+    }
+    __device__ __forceinline__ void pin() {
+#pragma unroll
+        for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(row[s]));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) asm volatile("" : "+v"(tr[e]));
     }
     static __device__ __forceinline__ int swizzle(int row) { return row & 15; }
     // step s: features 8 s + 4 half .. + 4, one for each of four matrix instructions

@@ -17,7 +17,7 @@ __device__ __forceinline__ void store_record(const CrossArgs &a, const CrossItem
 }
 
 template <int D, typename T>
-__global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossArgs a) {
+__global__ __launch_bounds__(256, D == 64 && sizeof(T) == 2 ? 3 : 2) void cross_dq_kernel(CrossArgs a) {
     typedef Ops<D, T> O;
     constexpr int BN = sizeof(T) == 2 ? 64 : 32, DB = D / 32;
     constexpr int TB = BN * O::RB;
@@ -72,26 +72,32 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossArgs a) {
     if (some) {
         O ops;
         ops.init(lane);
-        int buf = 0;
-        for (int pos = it.first; pos < it.end; pos += BN, buf ^= 1) {
+        auto tile = [&](auto which, int pos) {                // (as in the forward)
+            constexpr int BUF = decltype(which)::value;
             wait_vmcnt<0>();
             __syncthreads();
-            if (pos + BN < it.end) issue(pos + BN, buf ^ 1);
-            if (wave * 32 >= it.count) continue;
-            const char *kt = smem + buf * 2 * TB, *vt = kt + TB;
+            if (pos + BN < it.end) issue(pos + BN, BUF ^ 1);
+            if (wave * 32 >= it.count) return;
+            const char *kt = smem + BUF * 2 * TB, *vt = kt + TB;
             const int valid = it.end - pos;
 #pragma unroll
             for (int k32 = 0; k32 < BN; k32 += 32) {
                 if (k32 >= valid) break;
+                ops.pin();
                 f32x16 s = zero16(), dp = zero16();
 #pragma unroll
                 for (int i = 0; i < O::KS; ++i) s = O::mma(ops.frag(kt, k32, i), qf[i], s);
 #pragma unroll
                 for (int i = 0; i < O::KS; ++i) dp = O::mma(ops.frag(vt, k32, i), dof[i], dp);
+                if (valid >= k32 + 32) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse2));
-                    s[i] = k32 + (i >> 2) * 8 + half * 4 + (i & 3) < valid ? p * (dp[i] - delta) : 0.f;
+                    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse2)) * (dp[i] - delta);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float p = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse2));
+                        s[i] = k32 + (i >> 2) * 8 + half * 4 + (i & 3) < valid ? p * (dp[i] - delta) : 0.f;
+                    }
                 }
 #pragma unroll
                 for (int ks = 0; ks < O::RS; ++ks) {
@@ -100,6 +106,10 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossArgs a) {
                     for (int b = 0; b < DB; ++b) dq[b] = O::mma(ops.tfrag(kt, k32, b, ks), f, dq[b]);
                 }
             }
+        };
+        for (int pos = it.first; pos < it.end; pos += 2 * BN) {
+            tile(IC<0>{}, pos);
+            if (pos + BN < it.end) tile(IC<1>{}, pos + BN);
         }
     }
     if (a.split > 1) {
@@ -200,8 +210,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkdv_kernel(CrossA
             async_copy4_at(a.stats + 4 * (lane / 2 < valid ? row + lane / 2 : (size_t)a.rows) + (lane & 1), lds_address(stat[buf]));
     };
     if (t0 < t1) issue(0);
-    int buf = 0;
-    for (int t = t0; t < t1; ++t, buf ^= 1) {
+    auto tile = [&](auto which, int t) {
+        constexpr int buf = decltype(which)::value;
         wait_vmcnt<0>();
         __syncthreads();
         const int first = __builtin_amdgcn_readfirstlane(cs.first[si]), end = __builtin_amdgcn_readfirstlane(cs.end[si]);
@@ -210,7 +220,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkdv_kernel(CrossA
         }
         if (t + 1 < t1) issue(buf ^ 1);
         const int kw = key0 + wave * 32;
-        if (!active || first >= kw + 32 || end <= kw) continue;
+        if (!active || first >= kw + 32 || end <= kw) return;
+        ops.pin();
         const bool ok = key >= first && key < end;
         const char *qt = smem + buf * 2 * TB, *dot = qt + TB;
         f32x16 s = zero16(), dp = zero16();
@@ -240,6 +251,10 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkdv_kernel(CrossA
                 dk[b] = O::mma(ops.tfrag(qt, 0, b, ks), df, dk[b]);
             }
         }
+    };
+    for (int t = t0; t < t1; t += 2) {
+        tile(IC<0>{}, t);
+        if (t + 1 < t1) tile(IC<1>{}, t + 1);
     }
     if (key >= a.M) return;
     const size_t krow = (size_t)bhk * a.M + key;

@@ -48,51 +48,55 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cross_fwd_kernel(
         typename O::Frag qf[O::KS];
 #pragma unroll
         for (int s = 0; s < O::KS; ++s) qf[s] = O::row_frag(qrow, s, half);
-        int buf = 0;
-        for (int pos = it.first; pos < it.end; pos += BN, buf ^= 1) {
+        // One tile; the buffers take turns in a loop unrolled by two, so that LDS addresses are constants beside the lane's offsets.
+        auto tile = [&](auto which, int pos) {
+            constexpr int BUF = decltype(which)::value;
             wait_vmcnt<0>();
             __syncthreads();
-            if (pos + BN < it.end) issue(pos + BN, buf ^ 1);
-            if (wave * 32 >= it.count) continue;
-            const char *kt = smem + buf * 2 * TB, *vt = kt + TB;
+            if (pos + BN < it.end) issue(pos + BN, BUF ^ 1);
+            if (wave * 32 >= it.count) return;
+            ops.pin();
+            const char *kt = smem + BUF * 2 * TB, *vt = kt + TB;
             const int valid = it.end - pos;
+            f32x16 s = zero16();
 #pragma unroll
-            for (int kb32 = 0; kb32 < BN; kb32 += 32) {
-                if (kb32 >= valid) break;
-                f32x16 s = zero16();
+            for (int i = 0; i < O::KS; ++i) s = O::mma(ops.frag(kt, 0, i), qf[i], s);
+            if (valid < BN) {
 #pragma unroll
-                for (int i = 0; i < O::KS; ++i) s = O::mma(ops.frag(kt, kb32, i), qf[i], s);
-                if (valid < kb32 + 32) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (kb32 + (i >> 2) * 8 + half * 4 + (i & 3) >= valid) s[i] = -INFINITY;
-                }
-                float mx = s[0];
-#pragma unroll
-                for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
-                const float m_new = fmaxf(m_run, xhalf_max(mx));
-                if (__any((m_new - m_run) * c > 8.f)) {      // moved, and the sums rescaled, only when it has grown by 2^8
-                    const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * c);
-                    l_run *= alpha;
-#pragma unroll
-                    for (int b = 0; b < DB; ++b)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) oacc[b][i] *= alpha;
-                    m_run = m_new;
-                }
-                const float mc = m_run * c;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -mc));
-                    l_run += s[i];
-                }
-#pragma unroll
-                for (int ks = 0; ks < O::RS; ++ks) {
-                    const typename O::Frag pf = O::pack(s, ks);
-#pragma unroll
-                    for (int b = 0; b < DB; ++b) oacc[b] = O::mma(ops.tfrag(vt, kb32, b, ks), pf, oacc[b]);
-                }
+                for (int i = 0; i < 16; ++i)
+                    if ((i >> 2) * 8 + half * 4 + (i & 3) >= valid) s[i] = -INFINITY;
             }
+            float mx = s[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+            const float m_new = fmaxf(m_run, xhalf_max(mx));
+            if (pos == it.first) {
+                m_run = m_new;
+            } else if (__any((m_new - m_run) * c > 8.f)) {      // moved, and the sums rescaled, only when it has grown by 2^8
+                const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * c);
+                l_run *= alpha;
+#pragma unroll
+                for (int b = 0; b < DB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) oacc[b][i] *= alpha;
+                m_run = m_new;
+            }
+            const float mc = m_run * c;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -mc));
+                l_run += s[i];
+            }
+#pragma unroll
+            for (int ks = 0; ks < O::RS; ++ks) {
+                const typename O::Frag pf = O::pack(s, ks);
+#pragma unroll
+                for (int b = 0; b < DB; ++b) oacc[b] = O::mma(ops.tfrag(vt, 0, b, ks), pf, oacc[b]);
+            }
+        };
+        for (int pos = it.first; pos < it.end; pos += 2 * BN) {
+            tile(IC<0>{}, pos);
+            if (pos + BN < it.end) tile(IC<1>{}, pos + BN);
         }
     }
     const float l = xhalf_sum(l_run);
