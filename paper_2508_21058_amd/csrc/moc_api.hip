@@ -1129,7 +1129,7 @@ int moc_cross_attn_fwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, i
     if (misaligned(workspace)) return fail(MOC_ERR_ALIGN, "workspace must be 16-byte aligned");
     char *ws = static_cast<char *>(workspace);
     a.q = q; a.k = k; a.v = v; a.o = o; a.lse = lse;
-    a.split = p.split_fwd;
+    a.split = p.split_q;
     a.part = reinterpret_cast<float *>(ws + p.part);
     a.part_lse = reinterpret_cast<float *>(ws + p.part_lse);
     const hipError_t e = moc::launch_cross_fwd(a, d, dtype, static_cast<hipStream_t>(stream));

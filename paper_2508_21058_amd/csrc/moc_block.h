@@ -1,5 +1,5 @@
 // Arguments and launchers of the operators around the layer: head norms with rotation (moc_rope.hip) and cross attention
-// (moc_cross_fwd.hip, moc_cross_bwd.hip).
+// (moc_cross_fwd.hip, moc_cross_bwd.hip, moc_cross_dkdv.hip).
 #pragma once
 #include "moc_internal.h"
 
@@ -23,7 +23,7 @@ struct RowArgs {
     float *partial;                            // backward: [workgroups][2][d] sums for the weights' gradients
     int n_axes, axis_end[MOC_MAX_AXES];        // pairs [axis_end[a - 1], axis_end[a]) turn with axis a
     int N, n_tokens;                           // n_tokens = B * N
-    int heads_total, heads_per_group, groups, blocks;
+    int heads_total, heads_per_group, blocks;
     float eps, sign;                           // sign -1: the inverse rotation
 };
 // How a pass is cut: workgroups take `tokens` tokens of heads_per_group of all heads at a time.
@@ -58,16 +58,16 @@ struct CrossArgs {
     int N, M, n_seg;                   // tokens of a query head (all heads of a group where copies is 1 and H > Hk), states
     int copies;                        // query heads of a key head that are walked one by one
     int Hk, BHk, tiles;                // tiles: query tiles of one copy
-    int split, tile_rows;              // tile_rows: queries of a query tile
+    int split;                         // parts of a range of states (forward, dQ) or of the queries (dK / dV)
     int cut_at;                        // dQ: workgroups from here on cut the states, a sample each
     float scale, scale_log2;
     int32_t q_off[MOC_MAX_CROSS_SEGMENTS + 1];
     int32_t tile_at[MOC_MAX_CROSS_SEGMENTS + 1];      // first query tile of a segment
 };
+void cross_tiles(CrossArgs &a);        // cuts the segments into query tiles
 // Sizes of a call that follow from its arguments alone, and the places in its workspace (byte offsets).
-void cross_tiles(CrossArgs &a, int tile_rows);                      // cuts the segments into query tiles
 struct CrossPlan {
-    int split_fwd, split_dq, split_kv;
+    int split_q, split_kv;
     bool wide;                         // dK and dV in tiles of 256 states (moc_cross_dkdv.hip)
     int max_items;
     size_t stats, part, part_lse, kpart, items, item_counts, total;

@@ -94,9 +94,9 @@ __device__ __forceinline__ void cross_copy16(const void *base, uint32_t off, uin
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1"
                  :: "v"(off), "s"(uniform_ptr(base)), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
 }
-template <int D, typename T, int ROWS, int NW = 4>
+template <int D, typename T, int ROWS>
 __device__ __forceinline__ void copy_tile(const T *first, int valid, char *tile, int wave, int lane) {
-    constexpr int RB = D * (int)sizeof(T), GR = RB / 16, RPI = 64 / GR, NI = ROWS / RPI;
+    constexpr int RB = D * (int)sizeof(T), GR = RB / 16, RPI = 64 / GR, NI = ROWS / RPI, NW = 4;
     static_assert(NI % NW == 0, "rows divide evenly among the waves");
     const uint32_t at = lds_address(tile);
 #pragma unroll
@@ -107,7 +107,7 @@ __device__ __forceinline__ void copy_tile(const T *first, int valid, char *tile,
     }
 }
 
-// Work item of the query-stationary passes: up to tile_rows queries of one segment of one query head.
+// Work item of the query-stationary passes: up to kCrossRows queries of one segment of one query head.
 struct CrossItem {
     int bhk, count, first, end;      // key head of all samples, queries, range of states
     long long row;                   // first query in [B * H * N]
@@ -131,8 +131,8 @@ __device__ __forceinline__ CrossItem cross_item(const CrossArgs &a, int logical)
         const int mid = (s + hi) >> 1;
         if (a.tile_at[mid] <= t) s = mid; else hi = mid;
     }
-    const int q = a.q_off[s] + (t - a.tile_at[s]) * a.tile_rows;
-    it.count = min(a.tile_rows, a.q_off[s + 1] - q);
+    const int q = a.q_off[s] + (t - a.tile_at[s]) * kCrossRows;
+    it.count = min(kCrossRows, a.q_off[s + 1] - q);
     it.row = ((long long)it.bhk * a.copies + copy) * a.N + q;
     const CrossRange r = cross_range(a, it.bhk / a.Hk, s);
     it.first = __builtin_amdgcn_readfirstlane(r.first);

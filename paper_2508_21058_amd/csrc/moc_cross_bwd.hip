@@ -4,8 +4,13 @@
 //
 // Two passes without atomics: dQ over the queries, as the forward goes (it forms delta on its way in and leaves the
 // statistics), then dK and dV over the states: a workgroup owns 128 states of a key head and streams the queries of every segment whose
-// range meets them, 32 at a time, of all the query heads that share the key head. The states are few and the queries many, so the
-// queries of a tile of states are split over workgroups, whose sums a last launch adds in a fixed order.
+// range meets them, 32 at a time, of all the query heads that share the key head (bf16 heads of 128 features: 256 states, moc_cross_dkdv.hip).
+// The states are few and the queries many, so the queries of a tile of states are split over workgroups, whose sums a last launch adds
+// in a fixed order.
+//
+// What bounds it: at long ranges the products (33k queries, 4,357 states, 24 heads: dQ 2.4 ms, 1,080 TFLOP/s with the scores it forms again; a
+// library product of 8,192 x 8,192 matrices reaches 1,170 on this chip, which then holds less than its clock); at short ones the rows of
+// q, o, dO and dQ and what an item costs besides its products (114k queries, 256 states: 718 us, 2.8 GB, 750 TFLOP/s).
 #include "moc_cross.h"
 
 namespace moc {
@@ -291,8 +296,8 @@ __global__ __launch_bounds__(256) void cross_sum_kernel(const float *__restrict_
 }
 
 template <int D, typename T> static void bwd_dispatch(CrossArgs a, const CrossPlan &p, hipStream_t st) {
-    cross_tiles(a, kCrossRows);
-    a.split = p.split_dq;
+    cross_tiles(a);
+    a.split = p.split_q;
     {
         MOC_PROF("cross_dq", st);
         a.cut_at = xcd_grid((long long)a.tiles * a.copies * a.BHk * a.split);
@@ -333,7 +338,7 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
     const long long items = S == 1 ? (long long)B * Hk * (((long long)N * (H / Hk) + kCrossRows - 1) / kCrossRows)
                                    : (long long)B * H * ((N + kCrossRows - 1) / kCrossRows + S - 1);
     auto split = [](long long n, long long want, long long most) { return n >= want ? 1 : (int)std::max(1LL, std::min((want - 1 + n) / n, most)); };
-    p.split_fwd = p.split_dq = split(items, 512, (M + 255) / 256);
+    p.split_q = split(items, 512, (M + 255) / 256);
     const long long rows = (long long)B * H * N, states = (long long)B * Hk * M, per_head = (long long)N * (H / Hk);
     p.wide = d == 128 && dtype == MOC_BF16;
     p.max_items = M / kWideTile + 2 * S + 1;
@@ -357,8 +362,8 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
     }
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t x = at; at += up(bytes); return x; };
-    p.part = take(p.split_fwd > 1 ? (size_t)p.split_fwd * rows * d * 4 : 0);
-    p.part_lse = take(p.split_fwd > 1 ? (size_t)p.split_fwd * rows * 4 : 0);
+    p.part = take(p.split_q > 1 ? (size_t)p.split_q * rows * d * 4 : 0);
+    p.part_lse = take(p.split_q > 1 ? (size_t)p.split_q * rows * 4 : 0);
     p.stats = take(with_bwd ? (size_t)(rows + 1) * 16 : 0);
     p.kpart = take(with_bwd && p.split_kv > 1 ? (size_t)p.split_kv * states * 2 * d * 4 : 0);
     p.items = take(with_bwd && p.wide ? (size_t)B * p.max_items * sizeof(CrossKeys) : 0);

@@ -3,13 +3,13 @@
 // One pass with a running maximum and sum. A workgroup owns 128 queries, four waves of 32, and streams the range's states through LDS in
 // double-buffered tiles. S^T = K Q^T and O^T = V^T P^T, so that a lane owns a query: its statistics are scalars and the scores feed the second
 // product from the registers they are in. Calls of few query tiles split the range over workgroups, whose results a second launch joins.
+//
+// In bf16 three workgroups share a compute unit (168 registers, tiles of 32 states): 114k queries of 24 heads, eight shots of captions of 100 to 512
+// states 569 -> 506 us against two of 64-state tiles (of 32: 594), 33k queries against 4,357 states 1,886 -> 1,835.
 #include "moc_cross.h"
 
 namespace moc {
 
-//
-// In bf16 three workgroups share a compute unit (168 registers, tiles of 32 states): 114k queries of 24 heads, eight shots of captions of 100 to 512
-// states 569 -> 506 us against two of 64-state tiles (of 32: 594), 33k queries against 4,357 states 1,886 -> 1,835.
 template <int D, typename T>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cross_fwd_kernel(CrossArgs a) {
     typedef Ops<D, T> O;
@@ -157,7 +157,7 @@ template <int D, typename T> __global__ __launch_bounds__(kJoinThreads) void cro
 }
 
 template <int D, typename T> static void fwd_dispatch(CrossArgs &a, hipStream_t st) {
-    cross_tiles(a, kCrossRows);
+    cross_tiles(a);
     {
         MOC_PROF("cross_fwd", st);
         cross_fwd_kernel<D, T><<<xcd_grid((long long)a.tiles * a.copies * a.BHk * a.split), 256, 0, st>>>(a);
@@ -177,12 +177,11 @@ hipError_t launch_cross_fwd(CrossArgs a, int d, int dtype, hipStream_t st) {
 }
 
 // ---- how the queries are cut ----------------------------------------------------------------------
-void cross_tiles(CrossArgs &a, int tile_rows) {
-    a.tile_rows = tile_rows;
+void cross_tiles(CrossArgs &a) {
     a.tiles = 0;
     for (int s = 0; s < a.n_seg; ++s) {
         a.tile_at[s] = a.tiles;
-        a.tiles += (a.q_off[s + 1] - a.q_off[s] + tile_rows - 1) / tile_rows;
+        a.tiles += (a.q_off[s + 1] - a.q_off[s] + kCrossRows - 1) / kCrossRows;
     }
     a.tile_at[a.n_seg] = a.tiles;
 }

@@ -268,7 +268,6 @@ __global__ __launch_bounds__(kDwFeat *kDwSlices) void weight_grad_kernel(const f
 
 static void fill_grid(RowArgs &a, const RowGrid &g) {
     a.heads_per_group = g.per_group;
-    a.groups = g.groups;
     a.blocks = g.blocks;
 }
 
