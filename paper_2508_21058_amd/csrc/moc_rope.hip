@@ -16,10 +16,11 @@ namespace moc {
 constexpr int kRowThreads = 256;
 // Workgroups wanted. The forward takes many short ones, so that the last round of the chip is short, but at least eight heads each where there are
 // enough tokens, since each forms the angles anew: 33k tokens of 24 heads 91 us with a workgroup per 16 tokens (2,080 of them, 2,048 at a time),
-// 85 with three, 83 with eight; 6k tokens (q, k and v) 41.5 with three, 43.5 with 18, 55.5 with 36. The backward's take
-// several blocks of tokens one after the other, so that the weights' partial sums are few: 1,024, 2,048, 4,096 of them 60, 61, 77 us (two samples of
-// 16k tokens, twelve and four heads of 64).
-constexpr int kRowWgs = 6144, kRowWgsFew = 512, kRowHeadsMin = 8, kRowWgsBwd = 1024;
+// 85 with three, 83 with eight; 6k tokens (q, k and v) 41.5 with three, 43.5 with 18, 55.5 with 36. The backward's, of
+// which two fit a compute unit (174 registers), take several blocks of tokens one after the other, all of them in one round, so that the weights'
+// partial sums are few: 512, 1,024, 1,536 of them 53.5, 60.5, 66 us (two samples of 16k tokens, twelve and four heads of 64), 351, 357, 353
+// (33k tokens of 24 heads of 128).
+constexpr int kRowWgs = 6144, kRowWgsFew = 512, kRowHeadsMin = 8, kRowWgsBwd = 512;
 
 RowGrid row_grid(int B, int N, int heads_total, int d, bool bwd) {
     RowGrid g;
@@ -97,7 +98,14 @@ template <int D> __device__ __forceinline__ void thread_turns(const RowArgs &a, 
     }
 }
 
-constexpr int kRowHeads = 4;      // rows in flight a thread
+// f(Count<n>, h) for heads h0 .. h1 - 1, n of them at a time: four rows in flight a thread, what is left two and one
+template <int N> struct Count { static constexpr int value = N; };
+template <typename F> __device__ __forceinline__ void each_row(int h0, int h1, F f) {
+    int h = h0;
+    for (; h + 4 <= h1; h += 4) f(Count<4>{}, h);
+    if (h + 2 <= h1) { f(Count<2>{}, h); h += 2; }
+    if (h < h1) f(Count<1>{}, h);
+}
 
 template <int D, typename T, bool HALVES, bool NORM>
 __global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a) {
@@ -131,12 +139,13 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a) {
             for (int i = 0; i < 8; ++i) w[i] = 1.f;
             if (hp.weight) PairIo<D, HALVES, float>::load(hp.weight, c, w);
         }
-        for (int h = h0; h < h1; h += kRowHeads) {
-            float f[kRowHeads][8];
+        auto rows = [&](auto count, int h) {
+            constexpr int U = decltype(count)::value;
+            float f[U][8];
 #pragma unroll
-            for (int u = 0; u < kRowHeads; ++u) P::load(x + min(h + u, h1 - 1) * hp.x_h, c, f[u]);
+            for (int u = 0; u < U; ++u) P::load(x + (h + u) * hp.x_h, c, f[u]);
 #pragma unroll
-            for (int u = 0; u < kRowHeads; ++u) {
+            for (int u = 0; u < U; ++u) {
                 if (p < 2) {
                     float r = 1.f;
                     if (NORM) {
@@ -154,11 +163,14 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a) {
                         f[u][2 * i + 1] = y0 * sn[i] + y1 * cs[i];
                     }
                 }
-                if (valid && h + u < h1) P::store(o + (h + u) * hp.o_h, c, f[u]);
+                if (valid) P::store(o + (h + u) * hp.o_h, c, f[u]);
             }
-        }
+        };
+        each_row(h0, h1, rows);
     }
 }
+
+constexpr int kRowHeads = 4;      // of the backward, whose last rows are loaded again where four do not divide (in steps of four, two, one: more registers, 1 to 5 % slower)
 
 template <int D, typename T, bool HALVES>
 __global__ __launch_bounds__(kRowThreads) void rows_bwd_kernel(RowArgs a) {
