@@ -976,6 +976,7 @@ int cross_args(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t d
     }
     if (reinterpret_cast<uintptr_t>(kv_ranges) & 7u) return fail(MOC_ERR_ALIGN, "kv_ranges must be 8-byte aligned");
     a.ranges = reinterpret_cast<const moc::CrossRange *>(kv_ranges);
+    if (!kv_ranges) S = 1;              // every query attends all states: segments do not matter
     a.rows = (long long)B * H * N;
     a.M = M;
     a.n_seg = S;
@@ -1109,7 +1110,8 @@ int moc_cross_attn_workspace_bytes(int32_t B, int32_t H, int32_t Hk, int32_t N, 
     if (!bytes) return fail(MOC_ERR_NULL, "bytes is NULL");
     const int rc = check_cross(B, H, Hk, N, M, d, S, dtype);
     if (rc) return rc;
-    *bytes = moc::cross_plan(B, H, Hk, N, M, d, S, dtype, with_bwd != 0).total;
+    // (calls without kv_ranges are planned as one segment)
+    *bytes = std::max(moc::cross_plan(B, H, Hk, N, M, d, S, dtype, with_bwd != 0).total, moc::cross_plan(B, H, Hk, N, M, d, 1, dtype, with_bwd != 0).total);
     return MOC_OK;
 }
 
@@ -1124,7 +1126,7 @@ int moc_cross_attn_fwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, i
     moc::CrossArgs a{};
     rc = cross_args(B, H, Hk, N, M, d, S, q_offsets, kv_ranges, softmax_scale, a);
     if (rc) return rc;
-    const moc::CrossPlan p = moc::cross_plan(B, H, Hk, N, M, d, S, dtype, false);
+    const moc::CrossPlan p = moc::cross_plan(B, H, Hk, N, M, d, a.n_seg, dtype, false);
     if (p.total > 0 && (!workspace || workspace_bytes < p.total)) return fail(MOC_ERR_WORKSPACE, "cross attention workspace too small");
     if (misaligned(workspace)) return fail(MOC_ERR_ALIGN, "workspace must be 16-byte aligned");
     char *ws = static_cast<char *>(workspace);
@@ -1149,7 +1151,7 @@ int moc_cross_attn_bwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, i
     moc::CrossArgs a{};
     rc = cross_args(B, H, Hk, N, M, d, S, q_offsets, kv_ranges, softmax_scale, a);
     if (rc) return rc;
-    const moc::CrossPlan p = moc::cross_plan(B, H, Hk, N, M, d, S, dtype, true);
+    const moc::CrossPlan p = moc::cross_plan(B, H, Hk, N, M, d, a.n_seg, dtype, true);
     if (!workspace || workspace_bytes < p.total) return fail(MOC_ERR_WORKSPACE, "cross attention workspace too small (with_bwd)");
     if (misaligned(workspace)) return fail(MOC_ERR_ALIGN, "workspace must be 16-byte aligned");
     char *ws = static_cast<char *>(workspace);

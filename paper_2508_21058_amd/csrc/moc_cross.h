@@ -121,20 +121,56 @@ __device__ __forceinline__ CrossRange cross_range(const CrossArgs &a, int b, int
     }
     return r;
 }
+// Which segments of a sample attend what the segment before them attends (bit s of the 128): in a padded batch all do. Every lane of a
+// wave has to be here.
+struct SegmentBits {
+    unsigned long long lo, hi;
+    __device__ __forceinline__ bool at(int s) const { return ((s < 64 ? lo >> s : hi >> (s - 64)) & 1) != 0; }
+};
+__device__ __forceinline__ SegmentBits same_as_before(const CrossArgs &a, int b) {
+    const int lane = threadIdx.x & 63;
+    auto range = [&](int s) {
+        CrossRange r = {0, 0};
+        if (s < a.n_seg) r = cross_range(a, b, s);
+        if (r.end <= r.first) r.first = r.end = 0;
+        return r;
+    };
+    // (the exchanges are outside the conditions: lanes that skip one would hand nothing on)
+    const CrossRange r = range(lane);
+    const int rf = __shfl_up(r.first, 1, 64), re = __shfl_up(r.end, 1, 64);
+    SegmentBits m = {__ballot(lane > 0 && lane < a.n_seg && rf == r.first && re == r.end), 0};
+    if (a.n_seg > 64) {
+        const CrossRange q = range(lane + 64);
+        int qf = __shfl_up(q.first, 1, 64), qe = __shfl_up(q.end, 1, 64);
+        const int f = __shfl(r.first, 63, 64), e = __shfl(r.end, 63, 64);
+        if (lane == 0) { qf = f; qe = e; }
+        m.hi = __ballot(lane + 64 < a.n_seg && qf == q.first && qe == q.end);
+    }
+    return m;
+}
+// Neighbouring segments with one range are one run of queries, cut into whole tiles; the tiles that are then too many have no queries.
 __device__ __forceinline__ CrossItem cross_item(const CrossArgs &a, int logical) {
     CrossItem it;
     const int per_head = a.tiles * a.copies;
     it.bhk = logical / per_head;
+    const int b = it.bhk / a.Hk;
     const int rest = logical - it.bhk * per_head, copy = rest / a.tiles, t = rest - copy * a.tiles;
-    int s = 0, hi = a.n_seg;                                   // the last segment with tile_at <= t
-    while (hi - s > 1) {
-        const int mid = (s + hi) >> 1;
-        if (a.tile_at[mid] <= t) s = mid; else hi = mid;
+    int s = 0, e = 0;
+    if (a.n_seg > 1) {
+        int hi = a.n_seg;                                      // the last segment with tile_at <= t
+        while (hi - s > 1) {
+            const int mid = (s + hi) >> 1;
+            if (a.tile_at[mid] <= t) s = mid; else hi = mid;
+        }
+        const SegmentBits same = same_as_before(a, b);
+        e = s;
+        while (s > 0 && same.at(s)) --s;
+        while (e + 1 < a.n_seg && same.at(e + 1)) ++e;
     }
     const int q = a.q_off[s] + (t - a.tile_at[s]) * kCrossRows;
-    it.count = min(kCrossRows, a.q_off[s + 1] - q);
+    it.count = min(kCrossRows, a.q_off[e + 1] - q);
     it.row = ((long long)it.bhk * a.copies + copy) * a.N + q;
-    const CrossRange r = cross_range(a, it.bhk / a.Hk, s);
+    const CrossRange r = cross_range(a, b, s);
     it.first = __builtin_amdgcn_readfirstlane(r.first);
     it.end = __builtin_amdgcn_readfirstlane(r.end);
     return it;

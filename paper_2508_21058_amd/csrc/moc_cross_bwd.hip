@@ -36,6 +36,7 @@ __global__ __launch_bounds__(256, D == 64 && sizeof(T) == 2 ? 3 : 2) void cross_
     if (!xcd_remap((long long)a.tiles * a.copies * a.BHk * a.split, logical)) return;
     const int z = logical % a.split;
     CrossItem it = cross_item(a, logical / a.split);
+    if (it.count <= 0) return;
     cross_slice(it.first, it.end, z, a.split, BN);
     const int r = wave * 32 + l32, rc = min(r, it.count - 1);
     const bool row_valid = r < it.count;
@@ -127,9 +128,11 @@ __global__ __launch_bounds__(256, D == 64 && sizeof(T) == 2 ? 3 : 2) void cross_
     }
 }
 
-// The queries that a tile of states streams: the segments whose ranges meet it, cut into tiles of 32.
+// The queries that a tile of states streams: the segments whose ranges meet it, neighbours that attend the same of its states as one run, cut
+// into tiles of 32.
 struct CrossStream {
-    int n, seg[MOC_MAX_CROSS_SEGMENTS], tile_at[MOC_MAX_CROSS_SEGMENTS + 1], first[MOC_MAX_CROSS_SEGMENTS], end[MOC_MAX_CROSS_SEGMENTS];
+    int n, tile_at[MOC_MAX_CROSS_SEGMENTS + 1], query[MOC_MAX_CROSS_SEGMENTS], rows[MOC_MAX_CROSS_SEGMENTS], first[MOC_MAX_CROSS_SEGMENTS],
+        end[MOC_MAX_CROSS_SEGMENTS];
 };
 constexpr int kStreamRows = 32;
 // (the first wave; a barrier before anyone else reads it)
@@ -137,12 +140,22 @@ __device__ __forceinline__ void make_stream(const CrossArgs &a, int b, int key0,
     int n = 0, at = 0;
     for (int s0 = 0; s0 < a.n_seg; s0 += 64) {
         const int i = s0 + lane;
-        CrossRange r = {0, 0};
-        int tiles = 0;
+        int first = 0, end = 0;
         if (i < a.n_seg) {
-            r = cross_range(a, b, i);
-            if (max(r.first, key0) < min(r.end, key1)) tiles = (a.q_off[i + 1] - a.q_off[i] + kStreamRows - 1) / kStreamRows;
+            const CrossRange r = cross_range(a, b, i);
+            first = max(r.first, key0);
+            end = min(r.end, key1);
         }
+        const bool in = first < end;
+        const int f = __shfl_up(first, 1, 64), e = __shfl_up(end, 1, 64);
+        const unsigned long long joined = __ballot(in && lane > 0 && f == first && e == end);       // goes on with the run before it
+        int rows = 0;
+        if (in && !(joined >> lane & 1)) {
+            const unsigned long long rest = lane < 63 ? ~(joined >> (lane + 1)) : 1ull;
+            const int last = i + (rest ? __ffsll(rest) - 1 : 63 - lane);
+            rows = a.q_off[last + 1] - a.q_off[i];
+        }
+        const int tiles = (rows + kStreamRows - 1) / kStreamRows;
         int sum = tiles;
 #pragma unroll
         for (int w = 1; w < 64; w <<= 1) {
@@ -152,10 +165,11 @@ __device__ __forceinline__ void make_stream(const CrossArgs &a, int b, int key0,
         const unsigned long long have = __ballot(tiles > 0);
         if (tiles > 0) {
             const int j = n + __popcll(have & ((1ull << lane) - 1));
-            s.seg[j] = i;
             s.tile_at[j] = at + sum - tiles;
-            s.first[j] = r.first;
-            s.end[j] = r.end;
+            s.query[j] = a.q_off[i];
+            s.rows[j] = rows;
+            s.first[j] = first;
+            s.end[j] = end;
         }
         n += __popcll(have);
         at += __shfl(sum, 63, 64);
@@ -206,9 +220,9 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkdv_kernel(CrossA
         while (cs.tile_at[si + 1] <= u) ++si;
     }
     auto issue = [&](int buf) {
-        const int seg = __builtin_amdgcn_readfirstlane(cs.seg[si]), q = a.q_off[seg] + (u - __builtin_amdgcn_readfirstlane(cs.tile_at[si])) * kStreamRows;
-        const int valid = min(kStreamRows, a.q_off[seg + 1] - q);
-        const size_t row = ((size_t)bhk * a.copies + copy) * a.N + q;
+        const int done = (u - __builtin_amdgcn_readfirstlane(cs.tile_at[si])) * kStreamRows;
+        const int valid = min(kStreamRows, __builtin_amdgcn_readfirstlane(cs.rows[si]) - done);
+        const size_t row = ((size_t)bhk * a.copies + copy) * a.N + __builtin_amdgcn_readfirstlane(cs.query[si]) + done;
         copy_tile<D, T, kStreamRows>(static_cast<const T *>(a.q) + row * D, valid, smem + buf * 2 * TB, wave, lane);
         copy_tile<D, T, kStreamRows>(static_cast<const T *>(a.d_o) + row * D, valid, smem + buf * 2 * TB + TB, wave, lane);
         if (wave == 0)       // rows past the segment get (+inf, 0): no probability
@@ -310,7 +324,7 @@ template <int D, typename T> static void bwd_dispatch(CrossArgs a, const CrossPl
     }
     a.split = p.split_kv;
     const long long states = (long long)a.BHk * a.M;
-    if constexpr (D == 128 && sizeof(T) == 2) {
+    if (p.wide) {
         launch_cross_dkdv_wide(a, st);
     } else {
         MOC_PROF("cross_dkdv", st);
@@ -331,30 +345,43 @@ hipError_t launch_cross_bwd(CrossArgs a, const CrossPlan &p, int d, int dtype, h
     return hipGetLastError();
 }
 
+// Pairs of query and state from which on dK and dV take the wide tiles. They cost a half to a third of the others' a pair, but an item of them
+// takes 20 us to begin and end, the others' 10. The backward with the others / with these: 24 heads, 100 queries, 77 states (0.2M pairs)
+// 31 / 34 us; 300 queries, 300 states (2.2M) 57 / 59; 8 heads, 600 queries, 512 states (2.5M) 60 / 59; 24 heads, 1,000 queries, 300 states
+// (7M) 85 / 74; 2,000 queries, 512 states (25M) 124 / 95. (Shots with few states of their own among many pay later: 84 / 95 for one head of 51k queries.)
+constexpr double kCrossWidePairs = 2.5e6;
+
 // ---- how a call is cut ----------------------------------------------------------------------------
 CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype, bool with_bwd) {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     CrossPlan p;
-    const long long items = S == 1 ? (long long)B * Hk * (((long long)N * (H / Hk) + kCrossRows - 1) / kCrossRows)
-                                   : (long long)B * H * ((N + kCrossRows - 1) / kCrossRows + S - 1);
     auto split = [](long long n, long long want, long long most) { return n >= want ? 1 : (int)std::max(1LL, std::min((want - 1 + n) / n, most)); };
-    p.split_q = split(items, 512, (M + 255) / 256);
+    // Parts of the ranges of states, so that there are workgroups for all compute units, two where the states are many and the tiles certain;
+    // 128 states each at least. (Segments of one range are joined, so their number says little about that of the tiles.) 4 samples, 12 heads on 4,
+    // one query, 8,192 states: 32 parts 14 us, 16 parts 17. Three fp32 heads of 48 queries in eight segments, 1,707 states: 14 parts 23, four 63.
+    const long long items = S == 1 ? (long long)B * Hk * (((long long)N * (H / Hk) + kCrossRows - 1) / kCrossRows)
+                                   : (long long)B * H * ((N + kCrossRows - 1) / kCrossRows);
+    p.split_q = split(items, S == 1 && M >= 2048 ? 512 : 256, (M + 127) / 128);
     const long long rows = (long long)B * H * N, states = (long long)B * Hk * M, per_head = (long long)N * (H / Hk);
-    p.wide = d == 128 && dtype == MOC_BF16;
+    p.wide = d == 128 && dtype == MOC_BF16 && (double)rows * M > kCrossWidePairs;
     p.max_items = M / kWideTile + 2 * S + 1;
     if (p.wide) {
         // Parts of the queries that workgroups of one tile of states share. Rounds of the chip are whole and take as long as a part, but a
         // round with units to spare runs at a higher clock: full rounds take 1.2 times as long per item. A part costs its sums, written and
         // read again. Microseconds: 0.75 for 16 queries, 6 to begin and end, 6 TB/s. 33k queries, 4,357 states, 24 heads (432 tiles) 1 / 2 / 3
         // / 4 / 8 parts: 3,112 / 3,488 / 3,508 / 3,597 / 3,373 us; eight shots of 14k queries with captions of 100 to 512 states 1,431 / 1,135 /
-        // 1,089 / 1,065 / 1,163. (The sums may take half a gigabyte.)
-        const long long tiles = (long long)B * Hk * ((M + kWideTile - 1) / kWideTile);
-        const double stages = std::max(1.0, (double)per_head / S / 16), sums = (double)states * d * 16 / 6e6;
+        // 1,089 / 1,065 / 1,163. What the ranges of segments are is not known here: either all of them are all the states or each has its own,
+        // and the sum of both times is made small. (The sums of the parts may take half a gigabyte.)
+        const double sums = (double)states * d * 16 / 6e6;
+        auto time = [&](long long s, long long tiles, double stages) {
+            const double item = 0.75 * std::max(1.0, stages / s) + 6, rounds = (double)((tiles * s + kComputeUnits - 1) / kComputeUnits);
+            return std::max(rounds, 1.2 * tiles * s / kComputeUnits) * item + (s > 1 ? s * sums + 5 : 0);
+        };
+        const long long tiles = (long long)B * Hk * ((M + kWideTile - 1) / kWideTile), own = (long long)B * Hk * S;
         double best = 0;
-        for (long long s = 1; s <= std::min(64LL, (per_head + 255) / 256) &&
+        for (long long s = 1; s <= std::min(64LL, (per_head + 63) / 64) &&
                               (s == 1 || (s * states * d * 8 <= 512 << 20 && (long long)B * Hk * p.max_items * s < 1 << 20)); ++s) {
-            const double item = 0.75 * stages / s + 6, rounds = (double)((tiles * s + kComputeUnits - 1) / kComputeUnits);
-            const double us = std::max(rounds, 1.2 * tiles * s / kComputeUnits) * item + (s > 1 ? s * sums + 5 : 0);
+            const double us = time(s, tiles, per_head / 16.) + (S > 1 ? time(s, std::max(tiles, own), per_head / 16. / S) : 0);
             if (s == 1 || us < best) { best = us; p.split_kv = (int)s; }
         }
     } else {

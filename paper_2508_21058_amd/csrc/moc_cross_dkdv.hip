@@ -10,7 +10,7 @@
 namespace moc {
 
 namespace wide {
-// Pieces of contiguous queries: the segments of a tile, for every query head of the group in turn, of them `stages` stages.
+// Pieces of contiguous queries: the segments of a tile, neighbours as one, for every query head of the group in turn, of them `stages` stages.
 struct PieceSource {
     int n_direct, q_start, q_len;                       // the first piece, in queries of the key head
     const CrossArgs &a;
@@ -19,23 +19,27 @@ struct PieceSource {
     const char *rec_ptr;
     int first, rec_left, copy, seg, stages;             // of the piece: its first query and queries left; stages left behind it
     __device__ __forceinline__ PieceSource(const CrossArgs &args, const CrossKeys &k) : a(args), keys(k) {}
-    __device__ __forceinline__ static int stages_of(const CrossArgs &a, int s) { return (a.q_off[s + 1] - a.q_off[s] + R - 1) / R; }
+    __device__ __forceinline__ bool has(int s) const { return (keys.segments[s >> 5] >> (s & 31) & 1u) != 0; }
     __device__ __forceinline__ int next_segment(int s) const {      // the first segment of the tile from s on, or n_seg
-        for (; s < a.n_seg; ++s)
-            if (keys.segments[s >> 5] >> (s & 31) & 1u) break;
+        while (s < a.n_seg && !has(s)) ++s;
         return s;
     }
+    __device__ __forceinline__ int piece_end(int s) const {         // behind the last segment of the piece that begins at s
+        while (s < a.n_seg && has(s)) ++s;
+        return s;
+    }
+    __device__ __forceinline__ int stages_of(int s) const { return (a.q_off[piece_end(s)] - a.q_off[s] + R - 1) / R; }
     // the piece at (copy, seg) from its stage `skip` on
     __device__ __forceinline__ void enter(int skip) {
         first = copy * a.N + a.q_off[seg] + skip * R;
-        rec_left = a.q_off[seg + 1] - a.q_off[seg] - skip * R;
+        rec_left = a.q_off[piece_end(seg)] - a.q_off[seg] - skip * R;
         const int n = (rec_left + R - 1) / R;
         if (n > stages) rec_left = stages * R;
         stages -= min(n, stages);
         rec_ptr = records + (size_t)first * 16;
     }
     __device__ __forceinline__ void advance() {
-        seg = next_segment(seg + 1);
+        seg = next_segment(piece_end(seg));
         if (seg == a.n_seg) { ++copy; seg = next_segment(0); }
         enter(0);
     }
@@ -119,7 +123,7 @@ __global__ __launch_bounds__(256, 1) void cross_dkdv_wide_kernel(CrossArgs a) {
     };
     PieceSource src(a, keys);
     int per_copy = 0;
-    for (int s = src.next_segment(0); s < a.n_seg; s = src.next_segment(s + 1)) per_copy += PieceSource::stages_of(a, s);
+    for (int s = src.next_segment(0); s < a.n_seg; s = src.next_segment(src.piece_end(s))) per_copy += src.stages_of(s);
     const long long total = (long long)per_copy * a.copies;
     const int s0 = (int)(total * z / a.split), n_st = (int)(total * (z + 1) / a.split) - s0;
     if (n_st == 0) {
@@ -131,9 +135,9 @@ __global__ __launch_bounds__(256, 1) void cross_dkdv_wide_kernel(CrossArgs a) {
     src.copy = s0 / per_copy;
     int skip = s0 - src.copy * per_copy;
     src.seg = src.next_segment(0);
-    while (skip >= PieceSource::stages_of(a, src.seg)) {
-        skip -= PieceSource::stages_of(a, src.seg);
-        src.seg = src.next_segment(src.seg + 1);
+    while (skip >= src.stages_of(src.seg)) {
+        skip -= src.stages_of(src.seg);
+        src.seg = src.next_segment(src.piece_end(src.seg));
     }
     const size_t rows = (size_t)bhk * a.copies * a.N;
     src.records = reinterpret_cast<const char *>(a.stats) + rows * 16;

@@ -22,6 +22,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cross_fwd_kernel(
     if (!xcd_remap((long long)a.tiles * a.copies * a.BHk * a.split, logical)) return;
     const int z = logical % a.split;
     CrossItem it = cross_item(a, logical / a.split);
+    if (it.count <= 0) return;
     cross_slice(it.first, it.end, z, a.split, BN);
     const int r = wave * 32 + l32, rc = min(r, it.count - 1);
     const bool row_valid = r < it.count;
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cross_fwd_kernel(
     const float lse = l > 0.f || l != l ? m_run * a.scale + logf(l) : -INFINITY;
     if (row_valid && half == 0) *lout = lse;
     if (a.split > 1) {
-        if (row_valid) store_rows_f32<D>(oacc, inv, pout, half);
+        if (row_valid && it.first < it.end) store_rows_f32<D>(oacc, inv, pout, half);
     } else if constexpr (sizeof(T) == 4) {
         if (row_valid) store_rows_f32<D>(oacc, inv, out, half);
     } else {
@@ -113,43 +114,48 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cross_fwd_kernel(
     }
 }
 
-// Joins the results of split calls: lse = log sum_z exp(lse_z), o = sum_z exp(lse_z - lse) o_z. A workgroup a row: its threads take four
-// features of every kJoin-th split, and the kJoin sums are added in their order. (A thread walking all splits: 21 us for 48 rows of 32
-// splits, this 6.)
-constexpr int kJoinThreads = 256;
-template <int D, typename T> __global__ __launch_bounds__(kJoinThreads) void cross_join_kernel(CrossArgs a) {
-    constexpr int LPR = D / 4, kJoin = kJoinThreads / LPR;
-    __shared__ __attribute__((aligned(16))) float part[kJoin][D + 4];
-    __shared__ float most[kJoinThreads / 64];
-    const size_t row = blockIdx.x, rows = (size_t)a.rows;
-    const int c = threadIdx.x % LPR * 4, j = threadIdx.x / LPR;
+// Joins the results of split calls: lse = log sum_z exp(lse_z), o = sum_z exp(lse_z - lse) o_z; a split without states has lse_z = -inf and no o_z.
+// SL slices of threads share a row: slice j takes every SL-th split, four features a thread, and the slices are joined in their order. (48 rows of
+// 32 splits: one slice 21 us, eight 7; 51k rows of two splits: a workgroup of eight slices a row 43 us, of eight rows 15.)
+constexpr int kJoinThreads = 256, kJoinFew = 4;
+template <int D, typename T, int SL> __global__ __launch_bounds__(kJoinThreads) void cross_join_kernel(CrossArgs a) {
+    constexpr int LPR = D / 4, ROWS = kJoinThreads / (LPR * SL);
+    __shared__ __attribute__((aligned(16))) float part[ROWS * SL][D + 4];
+    const size_t rows = (size_t)a.rows;
+    const int c = threadIdx.x % LPR * 4, j = threadIdx.x / LPR % SL, mine = threadIdx.x / (LPR * SL);
+    const size_t row = min((size_t)blockIdx.x * ROWS + mine, rows - 1);       // (a row too many is the last one again: same values)
     float mx = -INFINITY;
-    for (int z = threadIdx.x; z < a.split; z += kJoinThreads) {
+#pragma unroll 4
+    for (int z = j; z < a.split; z += SL) {
         const float x = a.part_lse[z * rows + row];
         mx = x != x ? INFINITY : fmaxf(mx, x);              // (a NaN makes the weights NaN: inf - inf)
     }
-#pragma unroll
-    for (int w = 1; w < 64; w <<= 1) mx = fmaxf(mx, __shfl_xor(mx, w, 64));
-    if (threadIdx.x % 64 == 0) most[threadIdx.x / 64] = mx;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kJoinThreads / 64; ++w) mx = fmaxf(mx, most[w]);
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     float sum = 0.f;
-    if (mx > -INFINITY)
 #pragma unroll 4
-        for (int z = j; z < a.split; z += kJoin) {
-            const float w = expf(a.part_lse[z * rows + row] - mx);
-            sum += w;
-            o += w * *reinterpret_cast<const f32x4 *>(a.part + (z * rows + row) * D + c);
+    for (int z = j; z < a.split; z += SL) {
+        const float x = a.part_lse[z * rows + row];
+        const f32x4 part_o = *reinterpret_cast<const f32x4 *>(a.part + (z * rows + row) * D + c);      // (asked for before x is looked at)
+        if (x == -INFINITY) continue;
+        const float w = expf(x - mx);
+        sum += w;
+        o += w * part_o;
+    }
+    if (SL > 1) {
+        *reinterpret_cast<f32x4 *>(&part[mine * SL + j][c]) = o;
+        if (c == 0) { part[mine * SL + j][D] = sum; part[mine * SL + j][D + 1] = mx; }
+        __syncthreads();
+        if (j > 0) return;
+        for (int i = 1; i < SL; ++i) mx = fmaxf(mx, part[mine * SL + i][D + 1]);
+        o = f32x4{0.f, 0.f, 0.f, 0.f};
+        sum = 0.f;
+        for (int i = 0; i < SL; ++i) {
+            const float m = part[mine * SL + i][D + 1];
+            if (m == -INFINITY) continue;
+            const float w = expf(m - mx);
+            sum += w * part[mine * SL + i][D];
+            o += w * *reinterpret_cast<const f32x4 *>(&part[mine * SL + i][c]);
         }
-    *reinterpret_cast<f32x4 *>(&part[j][c]) = o;
-    if (c == 0) part[j][D] = sum;
-    __syncthreads();
-    if (j > 0) return;
-    for (int i = 1; i < kJoin; ++i) {
-        o += *reinterpret_cast<const f32x4 *>(&part[i][c]);
-        sum += part[i][D];
     }
     if (c == 0) a.lse[row] = mx > -INFINITY ? mx + logf(sum) : -INFINITY;
     const float inv = mx > -INFINITY ? 1.f / sum : 0.f;
@@ -164,7 +170,9 @@ template <int D, typename T> static void fwd_dispatch(CrossArgs &a, hipStream_t 
     }
     if (a.split > 1) {
         MOC_PROF("cross_join", st);
-        cross_join_kernel<D, T><<<(unsigned)a.rows, kJoinThreads, 0, st>>>(a);
+        constexpr int SL = kJoinThreads / (D / 4);
+        if (a.split <= kJoinFew) cross_join_kernel<D, T, 1><<<(unsigned)((a.rows + SL - 1) / SL), kJoinThreads, 0, st>>>(a);
+        else cross_join_kernel<D, T, SL><<<(unsigned)a.rows, kJoinThreads, 0, st>>>(a);
     }
 }
 

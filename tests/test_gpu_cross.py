@@ -167,6 +167,37 @@ def test_random_shapes(seed):
     check(**random_case(seed))
 
 
+LARGE = {       # more than a few million pairs: other tiles for dK and dV in bf16 with heads of 128 features
+    "whole": dict(B=2, H=6, Hk=2, N=701, M=600),
+    "padded": dict(B=4, H=4, Hk=4, N=530, M=777, ranges=[[(0, 777)], [(0, 0)], [(0, 1)], [(0, 300)]]),
+    "shots": dict(B=1, H=3, Hk=3, N=2003, M=1111, offs=[0, 300, 1000, 1003, 1700, 2003], ranges=[[(0, 77), (100, 612), (612, 615), (700, 1111), (700, 701)]]),
+    "overlapping": dict(B=2, H=3, Hk=1, N=1201, M=900, offs=[0, 1, 130, 130, 700, 1201],
+                        ranges=[[(0, 7), (5, 640), (0, 900), (640, 641), (100, 900)], [(250, 260), (30, 30), (0, 900), (200, 100), (-50, 1 << 30)]]),
+    "equal": dict(B=1, H=4, Hk=2, N=900, M=1024, offs=[0, 7, 300, 301, 555, 900], ranges=[[(3, 1001)] * 5]),
+    "few queries": dict(B=1, H=24, Hk=8, N=31, M=4097),
+    "none": dict(B=1, H=6, Hk=6, N=900, M=700, offs=[0, 450, 900], ranges=[[(5, 5), (700, 0)]]),
+}
+
+
+@pytest.mark.parametrize("name", LARGE)
+def test_larger_calls(name):
+    check(d=128, dtype=torch.bfloat16, **LARGE[name])
+
+
+@pytest.mark.parametrize("seed", range(100, 116))
+def test_random_larger_shapes(seed):
+    g = np.random.default_rng(seed)
+    c = random_case(seed)
+    N, M = (int(2 ** g.uniform(9, 11)) for _ in range(2))
+    cut = lambda x: x * M // max(1, c["N"])
+    c.update(H=c["H"] * 3, Hk=c["Hk"] * 3, N=N, M=M, d=128, dtype=torch.bfloat16)
+    if c["offs"]:
+        c["offs"] = [0] + sorted(g.integers(0, N + 1, len(c["offs"]) - 2).tolist()) + [N]
+    if c["ranges"]:
+        c["ranges"] = [[(cut(a), cut(e)) for a, e in sample] for sample in c["ranges"]]
+    check(**c)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("junk", [float("nan"), float("inf"), -3e38])
 def test_states_outside_every_range_are_never_used(junk, dtype):
