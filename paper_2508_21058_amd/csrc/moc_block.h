@@ -69,7 +69,7 @@ void cross_tiles(CrossArgs &a);        // cuts the segments into query tiles
 struct CrossPlan {
     int split_q, split_kv;
     bool wide;                         // dK and dV in tiles of 256 states (moc_cross_dkdv.hip)
-    int max_items;
+    int key_waves, max_items;          // else waves of 32 states of a workgroup
     size_t stats, part, part_lse, kpart, items, item_counts, total;
 };
 CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype, bool with_bwd);

@@ -6,7 +6,6 @@
 namespace moc {
 
 constexpr int kCrossRows = 128;      // queries of a workgroup in the query-stationary passes: four waves of 32
-constexpr int kCrossKeys = 128;      // states of a workgroup in the key-stationary pass: four waves of 32
 
 // What the kernels need of a storage type: T = bf16 runs on 32x32x16 matrix instructions, T = float on 32x32x2 ones. A tile in
 // LDS is row-major without padding, its 16-byte groups XOR-swizzled by the row (SwTile for bf16).
@@ -94,9 +93,9 @@ __device__ __forceinline__ void cross_copy16(const void *base, uint32_t off, uin
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1"
                  :: "v"(off), "s"(uniform_ptr(base)), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
 }
-template <int D, typename T, int ROWS>
+template <int D, typename T, int ROWS, int NW = 4>
 __device__ __forceinline__ void copy_tile(const T *first, int valid, char *tile, int wave, int lane) {
-    constexpr int RB = D * (int)sizeof(T), GR = RB / 16, RPI = 64 / GR, NI = ROWS / RPI, NW = 4;
+    constexpr int RB = D * (int)sizeof(T), GR = RB / 16, RPI = 64 / GR, NI = ROWS / RPI;
     static_assert(NI % NW == 0, "rows divide evenly among the waves");
     const uint32_t at = lds_address(tile);
 #pragma unroll

@@ -177,20 +177,21 @@ __device__ __forceinline__ void make_stream(const CrossArgs &a, int b, int key0,
     if (lane == 0) { s.n = n; s.tile_at[n] = at; }
 }
 
-template <int D, typename T>
-__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkdv_kernel(CrossArgs a) {
+// KW: waves of a workgroup, 32 states each
+template <int D, typename T, int KW>
+__global__ __launch_bounds__(64 * KW, D == 64 && KW * sizeof(T) != 4 ? 2 : 1) void cross_dkdv_kernel(CrossArgs a) {
     typedef Ops<D, T> O;
-    constexpr int DB = D / 32, TB = kStreamRows * O::RB;
+    constexpr int DB = D / 32, TB = kStreamRows * O::RB, KEYS = 32 * KW;
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB];          // Q, dO, twice
     __shared__ __attribute__((aligned(16))) float stat[2][2 * kStreamRows];
     __shared__ CrossStream cs;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
-    const int ktiles = (a.M + kCrossKeys - 1) / kCrossKeys;
+    const int ktiles = (a.M + KEYS - 1) / KEYS;
     int logical;
     if (!xcd_remap((long long)ktiles * a.BHk * a.split, logical)) return;
     const int bhk = logical / (ktiles * a.split), rest = logical - bhk * ktiles * a.split;      // tiles of states that stream the
-    const int z = rest / ktiles, key0 = (rest - z * ktiles) * kCrossKeys;                       // same queries are neighbours
-    if (wave == 0) make_stream(a, bhk / a.Hk, key0, min(key0 + kCrossKeys, a.M), cs, lane);
+    const int z = rest / ktiles, key0 = (rest - z * ktiles) * KEYS;                             // same queries are neighbours
+    if (wave == 0) make_stream(a, bhk / a.Hk, key0, min(key0 + KEYS, a.M), cs, lane);
     __syncthreads();
     const int per_copy = __builtin_amdgcn_readfirstlane(cs.tile_at[cs.n]);
     const long long total = (long long)per_copy * a.copies;
@@ -223,8 +224,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkdv_kernel(CrossA
         const int done = (u - __builtin_amdgcn_readfirstlane(cs.tile_at[si])) * kStreamRows;
         const int valid = min(kStreamRows, __builtin_amdgcn_readfirstlane(cs.rows[si]) - done);
         const size_t row = ((size_t)bhk * a.copies + copy) * a.N + __builtin_amdgcn_readfirstlane(cs.query[si]) + done;
-        copy_tile<D, T, kStreamRows>(static_cast<const T *>(a.q) + row * D, valid, smem + buf * 2 * TB, wave, lane);
-        copy_tile<D, T, kStreamRows>(static_cast<const T *>(a.d_o) + row * D, valid, smem + buf * 2 * TB + TB, wave, lane);
+        copy_tile<D, T, kStreamRows, KW>(static_cast<const T *>(a.q) + row * D, valid, smem + buf * 2 * TB, wave, lane);
+        copy_tile<D, T, kStreamRows, KW>(static_cast<const T *>(a.d_o) + row * D, valid, smem + buf * 2 * TB + TB, wave, lane);
         if (wave == 0)       // rows past the segment get (+inf, 0): no probability
             async_copy4_at(a.stats + 4 * (lane / 2 < valid ? row + lane / 2 : (size_t)a.rows) + (lane & 1), lds_address(stat[buf]));
     };
@@ -232,6 +233,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkdv_kernel(CrossA
     auto tile = [&](auto which, int t) {
         constexpr int buf = decltype(which)::value;
         wait_vmcnt<0>();
+        if (KW == 1) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the reads of the other buffer: a wave alone has no barrier)
         __syncthreads();
         const int first = __builtin_amdgcn_readfirstlane(cs.first[si]), end = __builtin_amdgcn_readfirstlane(cs.end[si]);
         if (++u == cs.tile_at[si + 1]) {
@@ -328,7 +330,13 @@ template <int D, typename T> static void bwd_dispatch(CrossArgs a, const CrossPl
         launch_cross_dkdv_wide(a, st);
     } else {
         MOC_PROF("cross_dkdv", st);
-        cross_dkdv_kernel<D, T><<<xcd_grid((long long)((a.M + kCrossKeys - 1) / kCrossKeys) * a.BHk * a.split), 256, 0, st>>>(a);
+        auto launch = [&](auto waves) {
+            constexpr int KW = decltype(waves)::value, KEYS = 32 * KW;
+            cross_dkdv_kernel<D, T, KW><<<xcd_grid((long long)((a.M + KEYS - 1) / KEYS) * a.BHk * a.split), 64 * KW, 0, st>>>(a);
+        };
+        if (p.key_waves == 1) launch(IC<1>{});
+        else if (p.key_waves == 2) launch(IC<2>{});
+        else launch(IC<4>{});
     }
     if (a.split > 1) {
         MOC_PROF("cross_sum", st);
@@ -345,12 +353,6 @@ hipError_t launch_cross_bwd(CrossArgs a, const CrossPlan &p, int d, int dtype, h
     return hipGetLastError();
 }
 
-// Pairs of query and state from which on dK and dV take the wide tiles. They cost a half to a third of the others' a pair, but an item of them
-// takes 20 us to begin and end, the others' 10. The backward with the others / with these: 24 heads, 100 queries, 77 states (0.2M pairs)
-// 31 / 34 us; 300 queries, 300 states (2.2M) 57 / 59; 8 heads, 600 queries, 512 states (2.5M) 60 / 59; 24 heads, 1,000 queries, 300 states
-// (7M) 85 / 74; 2,000 queries, 512 states (25M) 124 / 95. (Shots with few states of their own among many pay later: 84 / 95 for one head of 51k queries.)
-constexpr double kCrossWidePairs = 2.5e6;
-
 // ---- how a call is cut ----------------------------------------------------------------------------
 CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype, bool with_bwd) {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
@@ -363,29 +365,45 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
                                    : (long long)B * H * ((N + kCrossRows - 1) / kCrossRows);
     p.split_q = split(items, S == 1 && M >= 2048 ? 512 : 256, (M + 127) / 128);
     const long long rows = (long long)B * H * N, states = (long long)B * Hk * M, per_head = (long long)N * (H / Hk);
-    p.wide = d == 128 && dtype == MOC_BF16 && (double)rows * M > kCrossWidePairs;
     p.max_items = M / kWideTile + 2 * S + 1;
-    if (p.wide) {
-        // Parts of the queries that workgroups of one tile of states share. Rounds of the chip are whole and take as long as a part, but a
-        // round with units to spare runs at a higher clock: full rounds take 1.2 times as long per item. A part costs its sums, written and
-        // read again. Microseconds: 0.75 for 16 queries, 6 to begin and end, 6 TB/s. 33k queries, 4,357 states, 24 heads (432 tiles) 1 / 2 / 3
-        // / 4 / 8 parts: 3,112 / 3,488 / 3,508 / 3,597 / 3,373 us; eight shots of 14k queries with captions of 100 to 512 states 1,431 / 1,135 /
-        // 1,089 / 1,065 / 1,163. What the ranges of segments are is not known here: either all of them are all the states or each has its own,
-        // and the sum of both times is made small. (The sums of the parts may take half a gigabyte.)
-        const double sums = (double)states * d * 16 / 6e6;
-        auto time = [&](long long s, long long tiles, double stages) {
-            const double item = 0.75 * std::max(1.0, stages / s) + 6, rounds = (double)((tiles * s + kComputeUnits - 1) / kComputeUnits);
-            return std::max(rounds, 1.2 * tiles * s / kComputeUnits) * item + (s > 1 ? s * sums + 5 : 0);
+    p.key_waves = M <= 32 ? 1 : M <= 64 ? 2 : 4;
+    // dK and dV: parts of the queries that workgroups of one tile of states share, and (bf16, 128 features) which tiles. Rounds of workgroups on
+    // the chip are whole, a workgroup takes `begin` to begin and end and `stage` for 32 queries, and parts cost their sums, written and read again.
+    // Microseconds, fitted to calls of 16 to 114k queries. 24 heads, small / wide tiles: 64 queries, 1,024 states 16 / 29 us; 128 queries, 4,096
+    // states 54 / 58; 1,000 queries, 512 states 45 / 50; 8,000 queries, 77 states 47 / 67; 2,000 queries, 512 states 88 / 60. Small tiles, 12 fp32 heads of
+    // 33k queries, 512 states (48 tiles) in 11 / 16 parts (2.06 / 3 rounds of the chip) 2,300 / 1,620. Wide tiles, 24 heads of 33k queries, 4,357 states
+    // (432 tiles) in 1 / 2 / 3 / 4 / 8 parts 3,112 / 3,488 / 3,508 / 3,597 / 3,373. What the ranges of segments are is not known here: either all
+    // of them are all the states or each has its own, and the sum of both times is made small. (The sums of the parts may take half a gigabyte.)
+    const double stages = per_head / 32., sums = (double)states * d * 16 / 6e6;
+    const long long heads = (long long)B * Hk;
+    auto cut = [&](int keys, int per_unit, double stage, double begin, bool pieces, int &parts) {
+        const long long tiles = heads * ((M + keys - 1) / keys), units = (long long)kComputeUnits * per_unit;
+        // with ranges of their own the wide tiles are cut at them; the others meet the queries of every range that reaches into them
+        const long long own_tiles = pieces ? std::max(tiles, heads * S) : tiles;
+        const double own_stages = pieces ? stages / S : stages * std::min(1., (keys + M / S) / (double)M);
+        auto time = [&](long long s, long long n, double work) {
+            // (a round with units to spare runs at a higher clock: full rounds of matrix instructions take 1.2 times as long per item)
+            const double rounds = std::max((double)((n * s + units - 1) / units), pieces ? 1.2 * n * s / units : 0);
+            return rounds * (stage * std::max(1., work / s) + begin) + (s > 1 ? s * sums + 5 : 0);
         };
-        const long long tiles = (long long)B * Hk * ((M + kWideTile - 1) / kWideTile), own = (long long)B * Hk * S;
+        const long long most = std::min({1024LL, (per_head + 63) / 64, 3 * units / tiles + 1});
         double best = 0;
-        for (long long s = 1; s <= std::min(64LL, (per_head + 63) / 64) &&
-                              (s == 1 || (s * states * d * 8 <= 512 << 20 && (long long)B * Hk * p.max_items * s < 1 << 20)); ++s) {
-            const double us = time(s, tiles, per_head / 16.) + (S > 1 ? time(s, std::max(tiles, own), per_head / 16. / S) : 0);
-            if (s == 1 || us < best) { best = us; p.split_kv = (int)s; }
+        for (long long s = 1; s <= std::max(1LL, most) && (s == 1 || (s * states * d * 8 <= 512 << 20 && heads * p.max_items * s < 1 << 20)); s += 1 + s / 64) {
+            const double us = time(s, tiles, stages) + (S > 1 ? time(s, own_tiles, own_stages) : 0);
+            if (s == 1 || us < best) { best = us; parts = (int)s; }
         }
-    } else {
-        p.split_kv = split((long long)B * Hk * ((M + kCrossKeys - 1) / kCrossKeys), 512, (per_head + 63) / 64);
+        return best;
+    };
+    // (four waves to a compute unit, eight with heads of 64 features, or what its 160 KiB of LDS hold)
+    const int lds = 4 * kStreamRows * d * (dtype == MOC_BF16 ? 2 : 4) + (int)sizeof(CrossStream) + 512;
+    const int per_unit = std::min(163840 / lds, (d == 128 ? 4 : 8) / p.key_waves);
+    const double stage = (dtype == MOC_BF16 ? 1.5 : 8.) * d / 128 * std::max(1., per_unit * p.key_waves / 4.);
+    const double us = cut(32 * p.key_waves, per_unit, stage, 10, false, p.split_kv);
+    p.wide = false;
+    if (d == 128 && dtype == MOC_BF16) {
+        int parts;
+        p.wide = cut(kWideTile, 1, 1.5, 25, true, parts) < us;
+        if (p.wide) p.split_kv = parts;
     }
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t x = at; at += up(bytes); return x; };

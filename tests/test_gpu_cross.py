@@ -167,28 +167,39 @@ def test_random_shapes(seed):
     check(**random_case(seed))
 
 
-LARGE = {       # more than a few million pairs: other tiles for dK and dV in bf16 with heads of 128 features
-    "whole": dict(B=2, H=6, Hk=2, N=701, M=600),
-    "padded": dict(B=4, H=4, Hk=4, N=530, M=777, ranges=[[(0, 777)], [(0, 0)], [(0, 1)], [(0, 300)]]),
-    "shots": dict(B=1, H=3, Hk=3, N=2003, M=1111, offs=[0, 300, 1000, 1003, 1700, 2003], ranges=[[(0, 77), (100, 612), (612, 615), (700, 1111), (700, 701)]]),
-    "overlapping": dict(B=2, H=3, Hk=1, N=1201, M=900, offs=[0, 1, 130, 130, 700, 1201],
+WIDE = ["whole", "shots", "few heads", "none", "long padded", "long overlapping", "long equal"]    # work enough for wide tiles of states in dK's and dV's pass
+LARGE = {
+    "whole": dict(B=2, H=12, Hk=4, N=1901, M=900),
+    "padded": dict(B=4, H=8, Hk=8, N=1530, M=777, ranges=[[(0, 777)], [(0, 0)], [(0, 1)], [(0, 300)]]),
+    "shots": dict(B=1, H=8, Hk=8, N=5003, M=1111, offs=[0, 300, 2000, 2003, 3700, 5003], ranges=[[(0, 77), (100, 612), (612, 615), (700, 1111), (700, 701)]]),
+    "overlapping": dict(B=2, H=12, Hk=4, N=2201, M=900, offs=[0, 1, 130, 130, 1700, 2201],
                         ranges=[[(0, 7), (5, 640), (0, 900), (640, 641), (100, 900)], [(250, 260), (30, 30), (0, 900), (200, 100), (-50, 1 << 30)]]),
-    "equal": dict(B=1, H=4, Hk=2, N=900, M=1024, offs=[0, 7, 300, 301, 555, 900], ranges=[[(3, 1001)] * 5]),
-    "few queries": dict(B=1, H=24, Hk=8, N=31, M=4097),
-    "none": dict(B=1, H=6, Hk=6, N=900, M=700, offs=[0, 450, 900], ranges=[[(5, 5), (700, 0)]]),
+    "equal": dict(B=1, H=12, Hk=6, N=2900, M=1024, offs=[0, 7, 300, 301, 555, 2900], ranges=[[(3, 1001)] * 5]),
+    "few heads": dict(B=1, H=2, Hk=1, N=20001, M=1500),
+    "long padded": dict(B=4, H=24, Hk=24, N=3530, M=777, ranges=[[(0, 777)], [(0, 0)], [(0, 1)], [(0, 300)]]),
+    "long overlapping": dict(B=2, H=12, Hk=4, N=8201, M=900, offs=[0, 1, 130, 130, 6700, 8201],
+                             ranges=[[(0, 7), (5, 640), (0, 900), (640, 641), (100, 900)], [(250, 260), (30, 30), (0, 900), (200, 100), (-50, 1 << 30)]]),
+    "long equal": dict(B=1, H=24, Hk=12, N=8900, M=1024, offs=[0, 7, 3000, 3001, 5055, 8900], ranges=[[(3, 1001)] * 5]),
+    "none": dict(B=1, H=12, Hk=12, N=3900, M=700, offs=[0, 450, 3900], ranges=[[(5, 5), (700, 0)]]),
 }
 
 
 @pytest.mark.parametrize("name", LARGE)
 def test_larger_calls(name):
-    check(d=128, dtype=torch.bfloat16, **LARGE[name])
+    mb.prof_enable(True)
+    try:
+        check(d=128, dtype=torch.bfloat16, **LARGE[name])
+        ran = mb.prof_read()
+    finally:
+        mb.prof_enable(False)
+    assert name not in WIDE or "cross_dkdv_wide" in ran and "cross_dkdv" not in ran, ran
 
 
 @pytest.mark.parametrize("seed", range(100, 116))
 def test_random_larger_shapes(seed):
     g = np.random.default_rng(seed)
     c = random_case(seed)
-    N, M = (int(2 ** g.uniform(9, 11)) for _ in range(2))
+    N, M = (int(2 ** g.uniform(9.5, 12)) for _ in range(2))
     cut = lambda x: x * M // max(1, c["N"])
     c.update(H=c["H"] * 3, Hk=c["Hk"] * 3, N=N, M=M, d=128, dtype=torch.bfloat16)
     if c["offs"]:
