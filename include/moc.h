@@ -365,7 +365,7 @@ typedef struct moc_rope_plan {
  * sums over samples, heads and tokens; NULL where not wanted). q and k are the
  * forward's inputs; the norms are formed again from them. For v give d_v_out and dv, or
  * NULL for both. workspace: moc_qk_norm_rope_workspace_bytes bytes. Sums have a fixed
- * order: same input, same bits.
+ * order: same input, same bits. Here too outputs must not overlap inputs or each other.
  */
 int moc_qk_norm_rope(int32_t B, int32_t N, int32_t H, int32_t Hk, int32_t d, int dtype, const moc_rows *q,
                      const moc_rows *k, const moc_rows *v, const float *q_weight, const float *k_weight, float eps,
@@ -403,7 +403,7 @@ int moc_rope(int32_t B, int32_t N, int32_t H, int32_t d, int dtype, const moc_ro
  * MOC_BF16: products on bf16 matrix cores, softmax and sums in float, probabilities and dS rounded to
  * bf16 for the second products. MOC_F32: everything in float, the products on float matrix cores (unlike
  * moc_attn_*). softmax_scale finite and > 0. B * H <= 65535, H / Hk * N and M < 2^26, B * H * N and B * Hk * M < 2^31,
- * B * H * (N / 128 + S) and B * Hk * (M / 256 + 2 S) < 2^24 - 2048.
+ * B * H * (N / 128 + S) + B, B * Hk * (M / 256 + 2 S) and B * Hk * (M / 128 + 1) < 2^24 - 2048.
  *
  * moc_cross_attn_bwd: dq [B,H,N,d], dk, dv [B,Hk,M,d] (fully overwritten; dk and dv are summed over the
  * query heads of a key head) from the forward's o and lse and d_o [B,H,N,d]. Every sum has a fixed order: same

@@ -958,9 +958,11 @@ int check_cross(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t 
     if ((long long)N * (H / Hk) >= (1 << 26) || M >= (1 << 26)) return fail(MOC_ERR_SHAPE, "H / Hk * N and M must be < 2^26");
     if ((long long)B * H * N >= (1LL << 31) || (long long)B * Hk * M >= (1LL << 31))
         return fail(MOC_ERR_SHAPE, "B * H * N and B * Hk * M must be < 2^31");
-    // (a launch has fewer than 2^32 threads, 256 a workgroup)
-    const long long tiles = (long long)B * H * ((N + 127) / 128 + S - 1), pieces = (long long)B * Hk * (M / 256 + 2 * S + 1);
-    if (tiles >= (1 << 24) - 1024 || pieces >= (1 << 24) - 1024) return fail(MOC_ERR_SHAPE, "too many tiles: B * H * (N / 128 + S) or B * Hk * (M / 256 + 2 S)");
+    // (a launch has fewer than 2^32 threads, 256 a workgroup; dQ's has one more a sample)
+    const long long tiles = (long long)B * H * ((N + 127) / 128 + S - 1) + B;
+    const long long pieces = (long long)B * Hk * std::max(M / 256 + 2 * S + 1, (M + 127) / 128), most = (1 << 24) - 1024;
+    if (tiles >= most || pieces >= most)
+        return fail(MOC_ERR_SHAPE, "too many tiles: B * H * (N / 128 + S) + B, B * Hk * (M / 256 + 2 S) or B * Hk * M / 128");
     return MOC_OK;
 }
 

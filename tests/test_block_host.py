@@ -125,6 +125,14 @@ def test_workspace_sizes():
         assert size(*shape, 1, 1) <= stats + (600 << 20), shape
 
 
+@pytest.mark.parametrize("B,N,M", [(65535, 32640, 1), (1000, 1, 2147400)])
+def test_more_workgroups_than_a_launch_has(B, N, M):
+    """255 tiles of queries a sample and one workgroup more of each; 16,777 tiles of 128 states of 1,000 heads."""
+    n = C.c_size_t()
+    assert mb.lib().moc_cross_attn_workspace_bytes(B, 1, 1, N, M, 128, 1, 0, 1, C.byref(n)) == -2
+    assert mb.lib().moc_cross_attn_workspace_bytes(B // 2, 1, 1, N, M, 128, 1, 0, 1, C.byref(n)) == 0
+
+
 def test_binding_refuses_on_the_host():
     x = torch.zeros(1, 4, 2, 128)
     with pytest.raises(ValueError):
