@@ -258,9 +258,15 @@ __global__ __launch_bounds__(64 * KW, D == 64 && KW * sizeof(T) != 4 ? 2 : 1) vo
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int i = 4 * g + e;
-                const float p = ok ? __builtin_amdgcn_exp2f(fmaf(s[i], c, -l2[e])) : 0.f;
-                s[i] = p;
-                dp[i] = ok ? p * (dp[i] - dl[e]) : 0.f;
+                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -l2[e]));
+                dp[i] = s[i] * (dp[i] - dl[e]);
+            }
+        }
+        if (first > kw || end < kw + 32) {      // (a lane's key is in the range or not, for all of the queries. Heads of 64, as above: 720 us always masked, 655 so)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[i] = ok ? s[i] : 0.f;
+                dp[i] = ok ? dp[i] : 0.f;
             }
         }
 #pragma unroll
@@ -394,9 +400,10 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
         }
         return best;
     };
-    // (four waves to a compute unit, eight with heads of 64 features, or what its 160 KiB of LDS hold)
+    // (waves on a compute unit: four, with heads of 64 features eight, in bf16 in fours twelve; or what its 160 KiB of LDS hold. 24 heads of 64 features,
+    // 114k queries, 300 states: planned for eight 655 us, for twelve 580.)
     const int lds = 4 * kStreamRows * d * (dtype == MOC_BF16 ? 2 : 4) + (int)sizeof(CrossStream) + 512;
-    const int per_unit = std::min(163840 / lds, (d == 128 ? 4 : 8) / p.key_waves);
+    const int per_unit = std::min(163840 / lds, (d == 128 ? 4 : dtype == MOC_BF16 && p.key_waves == 4 ? 12 : 8) / p.key_waves);
     const double stage = (dtype == MOC_BF16 ? 1.5 : 8.) * d / 128 * std::max(1., per_unit * p.key_waves / 4.);
     const double us = cut(32 * p.key_waves, per_unit, stage, 10, false, p.split_kv);
     p.wide = false;
