@@ -363,13 +363,27 @@ hipError_t launch_cross_bwd(CrossArgs a, const CrossPlan &p, int d, int dtype, h
 CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype, bool with_bwd) {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     CrossPlan p;
-    auto split = [](long long n, long long want, long long most) { return n >= want ? 1 : (int)std::max(1LL, std::min((want - 1 + n) / n, most)); };
-    // Parts of the ranges of states, so that there are workgroups for all compute units, two where the states are many and the tiles certain;
-    // 128 states each at least. (Segments of one range are joined, so their number says little about that of the tiles.) 4 samples, 12 heads on 4,
-    // one query, 8,192 states: 32 parts 14 us, 16 parts 17. Three fp32 heads of 48 queries in eight segments, 1,707 states: 14 parts 23, four 63.
-    const long long items = S == 1 ? (long long)B * Hk * (((long long)N * (H / Hk) + kCrossRows - 1) / kCrossRows)
-                                   : (long long)B * H * ((N + kCrossRows - 1) / kCrossRows);
-    p.split_q = split(items, S == 1 && M >= 2048 ? 512 : 256, (M + 127) / 128);
+    const bool bf16 = dtype == MOC_BF16;
+    // Forward and dQ: parts of the ranges of states, of 128 states at least. Workgroups spread over the compute units in whole numbers; one takes 6 us
+    // and `one` for 32 states, two on a unit take `two` (float: twice as long, one fills the matrix pipes), and parts cost their sums. Forward, join,
+    // dQ and sum together, for at least 256 workgroups / this way: 24 heads of bf16, 309 queries, 300 states 46 / 33 us, 1,000 states 60 / 58, 16,000
+    // states 270 / 229; 1,000 queries, 1,000 states 86 / 72; twelve fp32 heads, 311 queries, 2,800 states 262 / 207 (36 tiles in eight
+    // parts are 32 units with two workgroups). Ranges of segments are all the states or each its own, as for dK and dV below.
+    {
+        const long long heads = (long long)B * (S == 1 ? Hk : H), len = S == 1 ? (long long)N * (H / Hk) : N;
+        const long long tiles = heads * ((len + kCrossRows - 1) / kCrossRows), own_tiles = tiles + heads * (S - 1);
+        const double one = (bf16 ? 0.7 : 3.5) * d / 128, two = (bf16 ? 1.1 : 7.) * d / 128, sums = (double)B * H * N * d * 8 / 6e6, stages = M / 32.;
+        auto time = [&](long long s, long long n, double work) {
+            const long long w = (n * s + kComputeUnits - 1) / kComputeUnits;
+            return (w / 2 * two + w % 2 * one) * std::max(1., work / s) + (w + 1) / 2 * 6 + (s > 1 ? s * sums + 6 : 0);
+        };
+        double best = 0;
+        const long long most = std::min({256LL, (M + 127LL) / 128, 4 * kComputeUnits / tiles + 1});
+        for (long long s = 1; s <= std::max(1LL, most); ++s) {
+            const double us = time(s, tiles, stages) + (S > 1 ? time(s, own_tiles, stages / S) : 0);
+            if (s == 1 || us < best) { best = us; p.split_q = (int)s; }
+        }
+    }
     const long long rows = (long long)B * H * N, states = (long long)B * Hk * M, per_head = (long long)N * (H / Hk);
     p.max_items = M / kWideTile + 2 * S + 1;
     p.key_waves = M <= 32 ? 1 : M <= 64 ? 2 : 4;
@@ -402,12 +416,12 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
     };
     // (waves on a compute unit: four, with heads of 64 features eight, in bf16 in fours twelve; or what its 160 KiB of LDS hold. 24 heads of 64 features,
     // 114k queries, 300 states: planned for eight 655 us, for twelve 580.)
-    const int lds = 4 * kStreamRows * d * (dtype == MOC_BF16 ? 2 : 4) + (int)sizeof(CrossStream) + 512;
-    const int per_unit = std::min(163840 / lds, (d == 128 ? 4 : dtype == MOC_BF16 && p.key_waves == 4 ? 12 : 8) / p.key_waves);
-    const double stage = (dtype == MOC_BF16 ? 1.5 : 8.) * d / 128 * std::max(1., per_unit * p.key_waves / 4.);
+    const int lds = 4 * kStreamRows * d * (bf16 ? 2 : 4) + (int)sizeof(CrossStream) + 512;
+    const int per_unit = std::min(163840 / lds, (d == 128 ? 4 : bf16 && p.key_waves == 4 ? 12 : 8) / p.key_waves);
+    const double stage = (bf16 ? 1.5 : 8.) * d / 128 * std::max(1., per_unit * p.key_waves / 4.);
     const double us = cut(32 * p.key_waves, per_unit, stage, 10, false, p.split_kv);
     p.wide = false;
-    if (d == 128 && dtype == MOC_BF16) {
+    if (d == 128 && bf16) {
         int parts;
         p.wide = cut(kWideTile, 1, 1.5, 25, true, parts) < us;
         if (p.wide) p.split_kv = parts;
