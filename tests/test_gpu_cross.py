@@ -345,3 +345,80 @@ def test_captured_passes_and_another_stream(N, M, S):
         got = both()
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def ran_wide(fn):
+    """fn()'s result; the call took the wide tiles of states."""
+    mb.prof_enable(True)
+    try:
+        out = fn()
+        ran = mb.prof_read()
+    finally:
+        mb.prof_enable(False)
+    assert "cross_dkdv_wide" in ran, ran
+    return out
+
+
+@pytest.mark.parametrize("junk", [float("nan"), float("inf"), -3e38])
+def test_wide_tiles_do_not_use_what_is_masked(junk):
+    """States outside every range, and the queries (and their dO) of segments whose range is empty."""
+    B, H, N, M, d = 2, 12, 4000, 700, 128
+    q, k, v, d_o = inputs(B, H, H, N, M, d, torch.bfloat16)
+    offs, ranges = [0, 1900, 2000, 4000], [[(3, 300), (0, 0), (333, 690)], [(0, 0), (70, 71), (64, 640)]]
+    kw = dict(kv_ranges=device_ranges(ranges), q_offsets=offs)
+
+    def run():
+        o, lse = mb.cross_attn_fwd(q, k, v, **kw)
+        return (o, lse, *mb.cross_attn_bwd(q, k, v, o, lse, d_o, **kw))
+
+    want = ran_wide(run)
+    for b in range(B):
+        used = torch.zeros(M, dtype=torch.bool, device="cuda")
+        for s, (a, e) in enumerate(ranges[b]):
+            used[a:e] = True
+            if e <= a:
+                q[b, :, offs[s]:offs[s + 1]] = junk
+                d_o[b, :, offs[s]:offs[s + 1]] = junk
+        k[b, :, ~used] = junk
+        v[b, :, ~used] = junk
+    got = run()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+def test_wide_tiles_captured():
+    B, H, Hk, N, M, S, d = 1, 12, 6, 5000, 900, 3, 128
+    q, k, v, d_o = inputs(B, H, Hk, N, M, d, torch.bfloat16)
+    offs = [N * s // S for s in range(S + 1)]
+    ranges = device_ranges([[(0, 900), (10, 20), (300, 900)]])
+    ws = mb.cross_attn_workspace(B, H, Hk, N, M, d, torch.bfloat16, True, S)
+
+    def both(ws=None):
+        o, lse = mb.cross_attn_fwd(q, k, v, ranges, offs, workspace=ws)
+        return (o, lse, *mb.cross_attn_bwd(q, k, v, o, lse, d_o, ranges, offs, workspace=ws))
+
+    ran_wide(lambda: both(ws))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = both(ws)
+    for r in ([[(0, 900), (10, 20), (300, 900)]], [[(5, 5), (0, 899), (0, 899)]], [[(0, 256), (256, 512), (512, 900)]], [[(0, 0)] * 3]):
+        ranges.copy_(device_ranges(r))
+        want = [t.clone() for t in both()]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want)), r
+
+
+def test_wide_tiles_of_a_key_head_of_more_than_4_gib_of_queries():
+    """Eight query heads on one key head, 17.6 million queries of it: the last of them."""
+    d, H, N, M = 128, 8, 2_200_000, 300
+    q = torch.zeros(1, H, N, d, dtype=torch.bfloat16, device="cuda")
+    k, v = inputs(1, H, 1, 1, M, d, torch.bfloat16)[1:3]
+    q[:, 7:, -100:] = mi.randn((1, 1, 100, d), 3, "cuda").to(torch.bfloat16)
+    o, lse = mb.cross_attn_fwd(q, k, v)
+    ref = reference(q[:, 7:, -100:], k, v, q[:, 7:, -100:], [[(0, M)]], [0, 100], d ** -0.5)
+    near("o", o[:, 7:, -100:], ref["o"])
+    dq, dk, dv = ran_wide(lambda: mb.cross_attn_bwd(q, k, v, o, lse, q))
+    near("dq", dq[:, 7:, -100:], ref["dq"])
+    near("dk", dk, ref["dk"])                # (the other queries and their dO are zero)
+    near("dv", dv, ref["dv"])
