@@ -398,7 +398,8 @@ int moc_rope(int32_t B, int32_t N, int32_t H, int32_t d, int dtype, const moc_ro
  *              padded batch are ranges (0, length), captions of shots one range a shot; ranges may
  *              overlap. NULL: all M states. Where a range is empty (end <= first) o = 0,
  *              lse = -infinity and no gradient arises. States outside every range are never
- *              used, whatever they hold; their dk and dv are 0.
+ *              used, whatever they hold; their dk and dv are 0. Nor does a query reach states that its
+ *              segment does not attend: a NaN or an infinity in it, or in its d_o, stays with those it attends.
  *   o DEVICE out [B,H,N,d];  lse DEVICE out [B,H,N] float.
  * MOC_BF16: products on bf16 matrix cores, softmax and sums in float, probabilities and dS rounded to
  * bf16 for the second products. MOC_F32: everything in float, the products on float matrix cores (unlike

@@ -179,7 +179,7 @@ __device__ __forceinline__ void make_stream(const CrossArgs &a, int b, int key0,
 
 // KW: waves of a workgroup, 32 states each
 template <int D, typename T, int KW>
-__global__ __launch_bounds__(64 * KW, D == 64 && KW * sizeof(T) != 4 ? 2 : 1) void cross_dkdv_kernel(CrossArgs a) {
+__global__ __launch_bounds__(64 * KW, D == 128 || KW * sizeof(T) == 4 ? 1 : KW * sizeof(T) == 8 && KW == 4 ? 3 : 2) void cross_dkdv_kernel(CrossArgs a) {
     typedef Ops<D, T> O;
     constexpr int DB = D / 32, TB = kStreamRows * O::RB, KEYS = 32 * KW;
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB];          // Q, dO, twice
@@ -213,6 +213,7 @@ __global__ __launch_bounds__(64 * KW, D == 64 && KW * sizeof(T) != 4 ? 2 : 1) vo
     O ops;
     ops.init(lane);
     const float c = a.scale_log2;
+    unsigned long long poisoned = 0;                // lanes whose results are NaN
     // the next tile to copy: query head `copy` of the group, entry si of the stream, tile u of the copy
     int copy = 0, u = 0, si = 0;
     if (t0 < t1) {
@@ -263,10 +264,18 @@ __global__ __launch_bounds__(64 * KW, D == 64 && KW * sizeof(T) != 4 ? 2 : 1) vo
             }
         }
         if (first > kw || end < kw + 32) {      // (a lane's key is in the range or not, for all of the queries. Heads of 64, as above: 720 us always masked, 655 so)
+            float all = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 s[i] = ok ? s[i] : 0.f;
                 dp[i] = ok ? dp[i] : 0.f;
+                all = fmaf(dp[i], 0.f, all);
+            }
+            // Zero times a NaN or an infinity of a query is not zero: its products would reach the lanes of states that it does not attend. Those that
+            // attend it come out as NaN, whatever the tile's other queries add, and the others have nothing of this tile.
+            if (__any(!(all == 0.f))) {
+                poisoned |= __ballot(ok);
+                return;
             }
         }
 #pragma unroll
@@ -284,6 +293,14 @@ __global__ __launch_bounds__(64 * KW, D == 64 && KW * sizeof(T) != 4 ? 2 : 1) vo
         if (t + 1 < t1) tile(IC<1>{}, t + 1);
     }
     if (key >= a.M) return;
+    if (poisoned) {
+        const float poison = poisoned >> lane & 1 ? NAN : 0.f;
+#pragma unroll
+        for (int b = 0; b < DB; ++b) {
+            dk[b] += poison;
+            dv[b] += poison;
+        }
+    }
     const size_t krow = (size_t)bhk * a.M + key;
     if (a.split > 1) {
         float *p = a.kpart + (((size_t)z * a.BHk * a.M) + krow) * 2 * D;

@@ -89,3 +89,34 @@ def test_block_forward_and_backward():
             assert float((axis_w.double() - want_w).norm() / want_w.norm()) < 1e-5
     assert torch.equal(grad[:, :, 2 * H:], dv.transpose(1, 2)) and torch.equal(dcv0, dcv.transpose(1, 2))
     meta.close()
+
+
+def test_two_streams_at_once():
+    """The same operators on two streams that are not ordered, each with its own workspace, against one after the other."""
+    B, N, H, d, M = 1, 3000, 6, 128, 300
+    bf16 = torch.bfloat16
+    plan = mb.rope_plan(torch.randint(0, 50, (N, 3), dtype=torch.int32, device="cuda"), [22, 21, 21])
+    sets = []
+    for s in range(2):
+        x = mi.randn((B, N, 3 * H, d), 7 + s, "cuda").to(bf16)
+        k, v = (mi.randn((B, H, M, d), 17 + s + 2 * i, "cuda").to(bf16) for i in range(2))
+        sets.append((x, k, v, mb.cross_attn_workspace(B, H, H, N, M, d, bf16, True), mb.qk_norm_rope_workspace(B, N, H, H, d, bf16)))
+
+    def block(x, k, v, ws, ws_norm):
+        q, kk, vv = mb.qk_norm_rope(*x.split(H, 2), rope=plan)
+        o, lse = mb.cross_attn_fwd(q, k, v, workspace=ws)
+        dq, dk, dv = mb.cross_attn_bwd(q, k, v, o, lse, q, workspace=ws)
+        return (o, lse, dq, dk, dv, *mb.qk_norm_rope_bwd(*x.split(H, 2)[:2], dq, kk, vv, rope=plan, workspace=ws_norm))
+
+    want = [block(*s) for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    got = [[], []]
+    for _ in range(4):
+        for i, (stream, s) in enumerate(zip(streams, sets)):
+            with torch.cuda.stream(stream):
+                got[i].append(block(*s))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for g in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(g, want[i]))

@@ -422,3 +422,35 @@ def test_wide_tiles_of_a_key_head_of_more_than_4_gib_of_queries():
     near("dq", dq[:, 7:, -100:], ref["dq"])
     near("dk", dk, ref["dk"])                # (the other queries and their dO are zero)
     near("dv", dv, ref["dv"])
+
+
+@pytest.mark.parametrize("junk", [float("nan"), float("inf")])
+@pytest.mark.parametrize("d,dtype,N,M", [(64, torch.bfloat16, 130, 100), (128, torch.bfloat16, 130, 100), (64, torch.float32, 130, 100),
+                                         (128, torch.float32, 130, 100), (128, torch.bfloat16, 130, 30), (64, torch.float32, 130, 60),
+                                         (128, torch.bfloat16, 9000, 900)])
+def test_a_bad_query_reaches_its_own_states_alone(junk, d, dtype, N, M):
+    """NaN or infinity in one query and its dO: the gradients of states that its segment does not attend, and the other queries, keep their bits."""
+    H, Hk = (24, 12) if N > 1000 else (2, 1)
+    q, k, v, d_o = inputs(1, H, Hk, N, M, d, dtype)
+    offs = [0, N // 3, 2 * N // 3, N]
+    ranges = [[(0, M * 37 // 100), (M * 37 // 100, M * 7 // 10), (M // 2, M)]]
+    kw = dict(kv_ranges=device_ranges(ranges), q_offsets=offs)
+
+    def run():
+        o, lse = mb.cross_attn_fwd(q, k, v, **kw)
+        return (o, lse, *mb.cross_attn_bwd(q, k, v, o, lse, d_o, **kw))
+
+    want = run()
+    bad = N // 2
+    q[:, 0, bad] = junk
+    d_o[:, 0, bad] = junk
+    got = run()
+    a, e = ranges[0][1]
+    other = torch.ones(M, dtype=torch.bool, device="cuda")
+    other[a:e] = False
+    for x, y in zip(got[3:], want[3:]):
+        assert torch.equal(x[:, :, other], y[:, :, other]) and not torch.isfinite(x[:, 0, ~other]).all(-1).any()
+        assert torch.equal(x[:, 1:], y[:, 1:])
+    for x, y in zip(got[:3], want[:3]):
+        x[:, 0, bad] = y[:, 0, bad] = 0
+        assert torch.equal(x, y)
