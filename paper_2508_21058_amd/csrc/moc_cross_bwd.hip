@@ -3,14 +3,16 @@
 //   dQ_i = scale sum_t dS_it k_t,  dV_t = sum_i P_it dO_i,  dK_t = scale sum_i dS_it q_i
 //
 // Two passes without atomics: dQ over the queries, as the forward goes (it forms delta on its way in and leaves the
-// statistics), then dK and dV over the states: a workgroup owns 128 states of a key head and streams the queries of every segment whose
-// range meets them, 32 at a time, of all the query heads that share the key head (bf16 heads of 128 features: 256 states, moc_cross_dkdv.hip).
-// The states are few and the queries many, so the queries of a tile of states are split over workgroups, whose sums a last launch adds
-// in a fixed order.
+// statistics), then dK and dV over the states: a workgroup owns 32 to 128 states of a key head, 32 a wave, and streams the queries of every
+// segment whose range meets them, 32 at a time, of all the query heads that share the key head (bf16 heads of 128 features in larger calls:
+// 256 states, moc_cross_dkdv.hip). The states are few and the queries many, so the queries of a tile of states are split over workgroups, whose
+// sums a last launch adds in a fixed order.
 //
-// What bounds it: at long ranges the products (33k queries, 4,357 states, 24 heads: dQ 2.4 ms, 1,080 TFLOP/s with the scores it forms again; a
+// What bounds it: at long ranges the products (33k queries, 4,357 states, 24 heads: dQ 2.35 ms, 1,140 TFLOP/s with the scores it forms again; a
 // library product of 8,192 x 8,192 matrices reaches 1,170 on this chip, which then holds less than its clock); at short ones the rows of
-// q, o, dO and dQ and what an item costs besides its products (114k queries, 256 states: 718 us, 2.8 GB, 750 TFLOP/s).
+// q, o, dO and dQ and what an item costs besides its products (114k queries, 256 states: 718 us, 2.8 GB, 750 TFLOP/s). dK and dV in small
+// tiles: 24 heads of 64 features, 114k queries, 1,024 states 1,495 us, 963 TFLOP/s; twelve fp32 heads, 33k queries, 512 states 1,575 us, 133
+// TFLOP/s of the card's 157; four states, where all there is to do is to read q and dO, 160 us for 0.74 GB.
 #include "moc_cross.h"
 
 namespace moc {
