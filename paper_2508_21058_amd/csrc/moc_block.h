@@ -59,6 +59,7 @@ struct CrossArgs {
     int copies;                        // query heads of a key head that are walked one by one
     int Hk, BHk, tiles;                // tiles: query tiles of one copy
     int split;                         // parts of a range of states (forward, dQ) or of the queries (dK / dV)
+    bool joined;                       // neighbouring segments with one range are one run of queries (a segment is short)
     int cut_at;                        // dQ: workgroups from here on cut the states, a sample each
     float scale, scale_log2;
     int32_t q_off[MOC_MAX_CROSS_SEGMENTS + 1];

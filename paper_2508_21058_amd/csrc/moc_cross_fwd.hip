@@ -190,9 +190,12 @@ hipError_t launch_cross_fwd(CrossArgs a, int d, int dtype, hipStream_t st) {
 // ---- how the queries are cut ----------------------------------------------------------------------
 void cross_tiles(CrossArgs &a) {
     a.tiles = 0;
+    a.joined = false;
     for (int s = 0; s < a.n_seg; ++s) {
+        const int rows = a.q_off[s + 1] - a.q_off[s];
         a.tile_at[s] = a.tiles;
-        a.tiles += (a.q_off[s + 1] - a.q_off[s] + kCrossRows - 1) / kCrossRows;
+        a.tiles += (rows + kCrossRows - 1) / kCrossRows;
+        a.joined |= a.n_seg > 1 && rows < kCrossJoin;
     }
     a.tile_at[a.n_seg] = a.tiles;
 }

@@ -180,6 +180,7 @@ LARGE = {
     "long overlapping": dict(B=2, H=12, Hk=4, N=8201, M=900, offs=[0, 1, 130, 130, 6700, 8201],
                              ranges=[[(0, 7), (5, 640), (0, 900), (640, 641), (100, 900)], [(250, 260), (30, 30), (0, 900), (200, 100), (-50, 1 << 30)]]),
     "long equal": dict(B=1, H=24, Hk=12, N=8900, M=1024, offs=[0, 7, 3000, 3001, 5055, 8900], ranges=[[(3, 1001)] * 5]),
+    "long segments": dict(B=2, H=6, Hk=3, N=6210, M=500, offs=[0, 2001, 4100, 4100 + 1025, 6210], ranges=[[(3, 400)] * 4, [(0, 90), (0, 90), (90, 500), (0, 0)]]),
     "none": dict(B=1, H=12, Hk=12, N=3900, M=700, offs=[0, 450, 3900], ranges=[[(5, 5), (700, 0)]]),
 }
 
