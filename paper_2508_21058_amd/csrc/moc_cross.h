@@ -151,13 +151,22 @@ __device__ __forceinline__ SegmentBits same_as_before(const CrossArgs &a, int b)
     }
     return m;
 }
+// The i-th key head of all samples in the order in which items are dealt out: sample after sample for each head, so that the slices of the XCDs
+// have items of every sample. (In a padded batch ranges differ, and the XCDs of the short ones would idle: three samples of 11k queries, 36 heads on
+// twelve, ranges of 539, 0 and 816 states, forward 486 us, this way 325, dQ 716 and 539.)
+__device__ __forceinline__ int dealt_head(const CrossArgs &a, int i) {
+    if (a.BHk == a.Hk) return i;
+    const int B = a.BHk / a.Hk, hk = i / B;
+    return (i - hk * B) * a.Hk + hk;
+}
 // Neighbouring segments with one range are one run of queries, cut into whole tiles; the tiles that are then too many have no queries.
 __device__ __forceinline__ CrossItem cross_item(const CrossArgs &a, int logical) {
     CrossItem it;
     const int per_head = a.tiles * a.copies;
-    it.bhk = logical / per_head;
+    const int i = logical / per_head;
+    it.bhk = dealt_head(a, i);
     const int b = it.bhk / a.Hk;
-    const int rest = logical - it.bhk * per_head, copy = rest / a.tiles, t = rest - copy * a.tiles;
+    const int rest = logical - i * per_head, copy = rest / a.tiles, t = rest - copy * a.tiles;
     int s = 0, e = 0;
     if (a.n_seg > 1) {
         int hi = a.n_seg;                                      // the last segment with tile_at <= t

@@ -191,7 +191,7 @@ __global__ __launch_bounds__(64 * KW, D == 128 || KW * sizeof(T) == 4 ? 1 : KW *
     const int ktiles = (a.M + KEYS - 1) / KEYS;
     int logical;
     if (!xcd_remap((long long)ktiles * a.BHk * a.split, logical)) return;
-    const int bhk = logical / (ktiles * a.split), rest = logical - bhk * ktiles * a.split;      // tiles of states that stream the
+    const int i = logical / (ktiles * a.split), bhk = dealt_head(a, i), rest = logical - i * ktiles * a.split;      // tiles of states that stream the
     const int z = rest / ktiles, key0 = (rest - z * ktiles) * KEYS;                             // same queries are neighbours
     if (wave == 0) make_stream(a, bhk / a.Hk, key0, min(key0 + KEYS, a.M), cs, lane);
     __syncthreads();
