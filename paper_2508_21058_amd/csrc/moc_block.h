@@ -60,6 +60,7 @@ struct CrossArgs {
     int Hk, BHk, tiles;                // tiles: query tiles of one copy
     int split;                         // parts of a range of states (forward, dQ) or of the queries (dK / dV)
     bool joined;                       // neighbouring segments with one range are one run of queries (a segment is short)
+    bool dealt;                        // items are dealt to the XCDs one by one
     int cut_at;                        // dQ: workgroups from here on cut the states, a sample each
     float scale, scale_log2;
     int32_t q_off[MOC_MAX_CROSS_SEGMENTS + 1];

@@ -159,6 +159,17 @@ __device__ __forceinline__ int dealt_head(const CrossArgs &a, int i) {
     const int B = a.BHk / a.Hk, hk = i / B;
     return (i - hk * B) * a.Hk + hk;
 }
+// Items of the query-stationary passes in slices of the XCDs, whose L2 then holds the states of a few heads. Samples of fewer heads than XCDs fill whole
+// slices all the same: where their ranges may differ and a head has queries enough, items are dealt one by one (four samples of 30k queries, two
+// heads, ranges of 498, 0, 81 and 380 states: forward 73 us, this way 52, dQ 112 and 83; one query a sample, where the order of reading decides, 13 and 16).
+__device__ __forceinline__ bool cross_logical(const CrossArgs &a, int &logical) {
+    const long long total = (long long)a.tiles * a.copies * a.BHk * a.split;
+    if (a.dealt) {
+        logical = blockIdx.x;
+        return logical < total;
+    }
+    return xcd_remap(total, logical);
+}
 // Neighbouring segments with one range are one run of queries, cut into whole tiles; the tiles that are then too many have no queries.
 __device__ __forceinline__ CrossItem cross_item(const CrossArgs &a, int logical) {
     CrossItem it;

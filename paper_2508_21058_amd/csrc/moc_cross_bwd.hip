@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256, D == 64 && sizeof(T) == 2 ? 3 : 2) void cross_
     if constexpr (D == 128 && sizeof(T) == 2)
         if ((int)blockIdx.x >= a.cut_at) { cross_cut(a, blockIdx.x - a.cut_at, *reinterpret_cast<CutLds *>(smem)); return; }
     int logical;
-    if (!xcd_remap((long long)a.tiles * a.copies * a.BHk * a.split, logical)) return;
+    if (!cross_logical(a, logical)) return;
     const int z = logical % a.split;
     CrossItem it = cross_item(a, logical / a.split);
     if (it.count <= 0) return;

@@ -22,7 +22,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cross_fwd_kernel(
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB > PATCH ? 4 * TB : PATCH];      // K, V, twice
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
     int logical;
-    if (!xcd_remap((long long)a.tiles * a.copies * a.BHk * a.split, logical)) return;
+    if (!cross_logical(a, logical)) return;
     const int z = logical % a.split;
     CrossItem it = cross_item(a, logical / a.split);
     if (it.count <= 0) return;
@@ -198,6 +198,7 @@ void cross_tiles(CrossArgs &a) {
         a.joined |= a.n_seg > 1 && rows < kCrossJoin;
     }
     a.tile_at[a.n_seg] = a.tiles;
+    a.dealt = a.ranges && a.BHk > a.Hk && a.Hk < kXcds && a.tiles >= kXcds;
 }
 
 }  // namespace moc

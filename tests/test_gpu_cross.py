@@ -455,3 +455,10 @@ def test_a_bad_query_reaches_its_own_states_alone(junk, d, dtype, N, M):
     for x, y in zip(got[:3], want[:3]):
         x[:, 0, bad] = y[:, 0, bad] = 0
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 128), (torch.float32, 64)])
+def test_padded_batch_of_few_heads(dtype, d):
+    """Items of the query passes are dealt out one by one, with and without segments, a last tile that is cut and parts of the ranges."""
+    check(5, 2, 1, 1030, 300, d, dtype, ranges=[[(0, 300)], [(0, 0)], [(0, 1)], [(0, 131)], [(7, 290)]])
+    check(2, 3, 3, 1100, 900, d, dtype, offs=[0, 500, 1100], ranges=[[(0, 900), (0, 900)], [(3, 20), (0, 0)]])
