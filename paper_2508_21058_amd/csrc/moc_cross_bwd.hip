@@ -13,6 +13,8 @@
 // q, o, dO and dQ and what an item costs besides its products (114k queries, 256 states: 718 us, 2.8 GB, 750 TFLOP/s). dK and dV in small
 // tiles: 24 heads of 64 features, 114k queries, 1,024 states 1,495 us, 963 TFLOP/s; twelve fp32 heads, 33k queries, 512 states 1,575 us, 133
 // TFLOP/s of the card's 157; four states, where all there is to do is to read q and dO, 160 us for 0.74 GB.
+#include <cmath>
+
 #include "moc_cross.h"
 
 namespace moc {
@@ -413,19 +415,22 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
     // 33k queries, 512 states (48 tiles) in 11 / 16 parts (2.06 / 3 rounds of the chip) 2,300 / 1,620. Wide tiles, 24 heads of 33k queries, 4,357 states
     // (432 tiles) in 1 / 2 / 3 / 4 / 8 parts 3,112 / 3,488 / 3,508 / 3,597 / 3,373. What the ranges of segments are is not known here: either all
     // of them are all the states or each has its own, and the sum of both times is made small. (The sums of the parts may take half a gigabyte.)
-    const double stages = per_head / 32., sums = (double)states * d * 16 / 6e6;
+    // (a copy's last 32 queries, or a segment's, are not whole ones: 36 fp32 heads on twelve, nine queries in two segments 57 us with one part, 22 with six and their sum)
+    const long long copies = S == 1 ? 1 : H / Hk, len = per_head / copies;
+    const double stages = (double)(copies * ((len + 31) / 32)), apart = (double)(copies * S * (((len + S - 1) / S + 31) / 32));
+    const double sums = (double)states * d * 16 / 6e6;
     const long long heads = (long long)B * Hk;
     auto cut = [&](int keys, int per_unit, double stage, double begin, bool pieces, int &parts) {
         const long long tiles = heads * ((M + keys - 1) / keys), units = (long long)kComputeUnits * per_unit;
         // with ranges of their own the wide tiles are cut at them; the others meet the queries of every range that reaches into them
         const long long own_tiles = pieces ? std::max(tiles, heads * S) : tiles;
-        const double own_stages = pieces ? stages / S : stages * std::min(1., (keys + M / S) / (double)M);
+        const double own_stages = pieces ? apart / S : apart * std::min(1., (keys + M / S) / (double)M);
         auto time = [&](long long s, long long n, double work) {
             // (a round with units to spare runs at a higher clock: full rounds of matrix instructions take 1.2 times as long per item)
             const double rounds = std::max((double)((n * s + units - 1) / units), pieces ? 1.2 * n * s / units : 0);
             return rounds * (stage * std::max(1., work / s) + begin) + (s > 1 ? s * sums + 5 : 0);
         };
-        const long long most = std::min({1024LL, (per_head + 63) / 64, 3 * units / tiles + 1});
+        const long long most = std::min({1024LL, (long long)std::ceil(std::max(stages, own_stages) / (bf16 ? 2 : 1)), 3 * units / tiles + 1});
         double best = 0;
         for (long long s = 1; s <= std::max(1LL, most) && (s == 1 || (s * states * d * 8 <= 512 << 20 && heads * p.max_items * s < 1 << 20)); s += 1 + s / 64) {
             const double us = time(s, tiles, stages) + (S > 1 ? time(s, own_tiles, own_stages) : 0);
