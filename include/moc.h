@@ -405,6 +405,10 @@ int moc_rope(int32_t B, int32_t N, int32_t H, int32_t d, int dtype, const moc_ro
  * bf16 for the second products. MOC_F32: everything in float, the products on float matrix cores (unlike
  * moc_attn_*). softmax_scale finite and > 0. B * H <= 65535, H / Hk * N and M < 2^26, B * H * N and B * Hk * M < 2^31,
  * B * H * (N / 128 + S) + B, B * Hk * (M / 256 + 2 S) and B * Hk * (M / 128 + 1) < 2^24 - 2048.
+ * No sum over states (o, lse, dq) or over the queries of a key head (dk, dv) adds more than 2^20 terms (MOC_F32: 2^15) in a row; longer ones
+ * are cut into parts, which are in the workspace. That is 2^16 (2^14) additions, whose error stays within 2^-8 (2^-10) of the terms' magnitudes. So
+ * with M beyond that the first of the three products above times the parts is bounded too, and B * H * N < 2^27 - 2^14, with H / Hk * N
+ * beyond it the others and B * Hk * M < 2^26 - 2^13 (MOC_ERR_SHAPE).
  *
  * moc_cross_attn_bwd: dq [B,H,N,d], dk, dv [B,Hk,M,d] (fully overwritten; dk and dv are summed over the
  * query heads of a key head) from the forward's o and lse and d_o [B,H,N,d]. Every sum has a fixed order: same

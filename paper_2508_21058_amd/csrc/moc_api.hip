@@ -966,6 +966,8 @@ int check_cross(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t 
     return MOC_OK;
 }
 
+int too_many_parts() { return fail(MOC_ERR_SHAPE, "too many tiles for the parts that sums over so many states or queries are cut into"); }
+
 // The parts of a call that both directions share.
 int cross_args(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t d, int32_t S, const int32_t *q_offsets,
                const int32_t *kv_ranges, float scale, moc::CrossArgs &a) {
@@ -1113,7 +1115,9 @@ int moc_cross_attn_workspace_bytes(int32_t B, int32_t H, int32_t Hk, int32_t N, 
     const int rc = check_cross(B, H, Hk, N, M, d, S, dtype);
     if (rc) return rc;
     // (calls without kv_ranges are planned as one segment)
-    *bytes = std::max(moc::cross_plan(B, H, Hk, N, M, d, S, dtype, with_bwd != 0).total, moc::cross_plan(B, H, Hk, N, M, d, 1, dtype, with_bwd != 0).total);
+    const moc::CrossPlan p = moc::cross_plan(B, H, Hk, N, M, d, S, dtype, with_bwd != 0), one = moc::cross_plan(B, H, Hk, N, M, d, 1, dtype, with_bwd != 0);
+    if (!p.fits || !one.fits) return too_many_parts();
+    *bytes = std::max(p.total, one.total);
     return MOC_OK;
 }
 
@@ -1129,6 +1133,7 @@ int moc_cross_attn_fwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, i
     rc = cross_args(B, H, Hk, N, M, d, S, q_offsets, kv_ranges, softmax_scale, a);
     if (rc) return rc;
     const moc::CrossPlan p = moc::cross_plan(B, H, Hk, N, M, d, a.n_seg, dtype, false);
+    if (!p.fits) return too_many_parts();
     if (p.total > 0 && (!workspace || workspace_bytes < p.total)) return fail(MOC_ERR_WORKSPACE, "cross attention workspace too small");
     if (misaligned(workspace)) return fail(MOC_ERR_ALIGN, "workspace must be 16-byte aligned");
     char *ws = static_cast<char *>(workspace);
@@ -1154,6 +1159,7 @@ int moc_cross_attn_bwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, i
     rc = cross_args(B, H, Hk, N, M, d, S, q_offsets, kv_ranges, softmax_scale, a);
     if (rc) return rc;
     const moc::CrossPlan p = moc::cross_plan(B, H, Hk, N, M, d, a.n_seg, dtype, true);
+    if (!p.fits) return too_many_parts();
     if (!workspace || workspace_bytes < p.total) return fail(MOC_ERR_WORKSPACE, "cross attention workspace too small (with_bwd)");
     if (misaligned(workspace)) return fail(MOC_ERR_ALIGN, "workspace must be 16-byte aligned");
     char *ws = static_cast<char *>(workspace);

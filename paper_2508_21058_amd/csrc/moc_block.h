@@ -67,11 +67,15 @@ struct CrossArgs {
     int32_t tile_at[MOC_MAX_CROSS_SEGMENTS + 1];      // first query tile of a segment
 };
 void cross_tiles(CrossArgs &a);        // cuts the segments into query tiles
+// Terms of a sum over states or queries that are added one after the other: 2^16 matrix additions of 16 products each in bf16, 2^14 of two in float.
+// n additions in a row are off by at most n 2^-24 of the terms' magnitudes, and by a quarter of that where all terms are alike (2^-10, 2^-12).
+constexpr int kChainTerms = 1 << 20, kChainTermsF32 = 1 << 15;
 // Sizes of a call that follow from its arguments alone, and the places in its workspace (byte offsets).
 struct CrossPlan {
     int split_q, split_kv;
     bool wide;                         // dK and dV in tiles of 256 states (moc_cross_dkdv.hip)
     int key_waves, max_items;          // else waves of 32 states of a workgroup
+    bool fits;                         // no launch is larger than launches can be
     size_t stats, part, part_lse, kpart, items, item_counts, total;
 };
 CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype, bool with_bwd);

@@ -385,6 +385,10 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     CrossPlan p;
     const bool bf16 = dtype == MOC_BF16;
+    const long long rows = (long long)B * H * N, states = (long long)B * Hk * M, per_head = (long long)N * (H / Hk);
+    // However well a call fills the chip, a sum is no longer than kChainTerms: a growing float sum rounds the same number the same way for a long time, so
+    // that its error is not a random walk's (4 million states of nearly equal probability in one chain: the softmax's sum 1.6 % off).
+    const long long chain = bf16 ? kChainTerms : kChainTermsF32, least_q = (M + chain - 1) / chain, least_kv = (per_head + chain - 1) / chain;
     // Forward and dQ: parts of the ranges of states, of 128 states at least. Workgroups spread over the compute units in whole numbers; one takes 6 us
     // and `one` for 32 states, two on a unit take `two` (float: twice as long, one fills the matrix pipes), and parts cost their sums. Forward, join,
     // dQ and sum together, for at least 256 workgroups / this way: 24 heads of bf16, 309 queries, 300 states 46 / 33 us, 1,000 states 60 / 58, 16,000
@@ -400,12 +404,11 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
         };
         double best = 0;
         const long long most = std::min({256LL, (M + 127LL) / 128, 4 * kComputeUnits / tiles + 1});
-        for (long long s = 1; s <= std::max(1LL, most); ++s) {
+        for (long long s = least_q; s <= std::max(least_q, most); ++s) {
             const double us = time(s, tiles, stages) + (S > 1 ? time(s, own_tiles, stages / S) : 0);
-            if (s == 1 || us < best) { best = us; p.split_q = (int)s; }
+            if (s == least_q || us < best) { best = us; p.split_q = (int)s; }
         }
     }
-    const long long rows = (long long)B * H * N, states = (long long)B * Hk * M, per_head = (long long)N * (H / Hk);
     p.max_items = M / kWideTile + 2 * S + 1;
     p.key_waves = M <= 32 ? 1 : M <= 64 ? 2 : 4;
     // dK and dV: parts of the queries that workgroups of one tile of states share, and (bf16, 128 features) which tiles. Rounds of workgroups on
@@ -414,7 +417,8 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
     // states 54 / 58; 1,000 queries, 512 states 45 / 50; 8,000 queries, 77 states 47 / 67; 2,000 queries, 512 states 88 / 60. Small tiles, 12 fp32 heads of
     // 33k queries, 512 states (48 tiles) in 11 / 16 parts (2.06 / 3 rounds of the chip) 2,300 / 1,620. Wide tiles, 24 heads of 33k queries, 4,357 states
     // (432 tiles) in 1 / 2 / 3 / 4 / 8 parts 3,112 / 3,488 / 3,508 / 3,597 / 3,373. What the ranges of segments are is not known here: either all
-    // of them are all the states or each has its own, and the sum of both times is made small. (The sums of the parts may take half a gigabyte.)
+    // of them are all the states or each has its own, and the sum of both times is made small. (The sums of the parts may take half a gigabyte, of parts that are
+    // there for the length of the sums more.)
     // (a copy's last 32 queries, or a segment's, are not whole ones: 36 fp32 heads on twelve, nine queries in two segments 57 us with one part, 22 with six and their sum)
     const long long copies = S == 1 ? 1 : H / Hk, len = per_head / copies;
     const double stages = (double)(copies * ((len + 31) / 32)), apart = (double)(copies * S * (((len + S - 1) / S + 31) / 32));
@@ -432,9 +436,10 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
         };
         const long long most = std::min({1024LL, (long long)std::ceil(std::max(stages, own_stages) / (bf16 ? 2 : 1)), 3 * units / tiles + 1});
         double best = 0;
-        for (long long s = 1; s <= std::max(1LL, most) && (s == 1 || (s * states * d * 8 <= 512 << 20 && heads * p.max_items * s < 1 << 20)); s += 1 + s / 64) {
+        for (long long s = least_kv; s <= std::max(least_kv, most) && (s == least_kv || (s * states * d * 8 <= 512 << 20 && heads * p.max_items * s < 1 << 20));
+             s += 1 + s / 64) {
             const double us = time(s, tiles, stages) + (S > 1 ? time(s, own_tiles, own_stages) : 0);
-            if (s == 1 || us < best) { best = us; parts = (int)s; }
+            if (s == least_kv || us < best) { best = us; parts = (int)s; }
         }
         return best;
     };
@@ -459,6 +464,13 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
     p.items = take(with_bwd && p.wide ? (size_t)B * p.max_items * sizeof(CrossKeys) : 0);
     p.item_counts = take(with_bwd && p.wide ? (size_t)B * sizeof(CrossCount) : 0);
     p.total = at;
+    // A launch has fewer than 2^32 threads. (The query passes take workgroups of 256 threads, one a tile of queries and part, dQ's one more a sample;
+    // the passes over the states one a tile and part, the wide one 16 more; joins and sums 256 / (d / 4) rows.)
+    const long long most = (1 << 24) - 1024, words = d / 4, keys = 32 * p.key_waves;
+    const long long q_wgs = ((long long)B * H * ((N + kCrossRows - 1) / kCrossRows + S - 1)) * p.split_q + B;
+    const long long kv_wgs = heads * (p.wide ? p.max_items : (M + keys - 1) / keys) * p.split_kv;
+    p.fits = q_wgs < most && (p.split_q == 1 || rows * words / 256 < most) &&
+             (!with_bwd || (kv_wgs < most && (p.split_kv == 1 || states * 2 * words / 256 < most)));
     return p;
 }
 

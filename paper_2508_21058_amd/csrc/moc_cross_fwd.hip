@@ -86,11 +86,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cross_fwd_kernel(
                 m_run = m_new;
             }
             const float mc = m_run * c;
+            float l_tile = 0.f;                // (on its own first: a long range adds few large numbers)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -mc));
-                l_run += s[i];
+                l_tile += s[i];
             }
+            l_run += l_tile;
 #pragma unroll
             for (int ks = 0; ks < O::RS; ++ks) {
                 const typename O::Frag pf = O::pack(s, ks);
@@ -119,8 +121,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cross_fwd_kernel(
 
 // Joins the results of split calls: lse = log sum_z exp(lse_z), o = sum_z exp(lse_z - lse) o_z; a split without states has lse_z = -inf and no o_z.
 // SL slices of threads share a row: slice j takes every SL-th split, four features a thread, and the slices are joined in their order. (48 rows of
-// 32 splits: one slice 21 us, eight 7; 51k rows of two splits: a workgroup of eight slices a row 43 us, of eight rows 15.)
-constexpr int kJoinThreads = 256, kJoinFew = 4;
+// 32 splits: one slice 21 us, eight 7; 51k rows of two splits: a workgroup of eight slices a row 43 us, of eight rows 15. Where
+// rows fill the chip by themselves, as in calls cut for the length of their sums, one slice: 131k rows of 64 features, nine splits, eight slices 158 us, one 70.)
+constexpr int kJoinThreads = 256, kJoinFew = 4, kJoinRows = 1 << 16;
 template <int D, typename T, int SL> __global__ __launch_bounds__(kJoinThreads) void cross_join_kernel(CrossArgs a) {
     constexpr int LPR = D / 4, ROWS = kJoinThreads / (LPR * SL);
     __shared__ __attribute__((aligned(16))) float part[ROWS * SL][D + 4];
@@ -174,7 +177,7 @@ template <int D, typename T> static void fwd_dispatch(CrossArgs &a, hipStream_t 
     if (a.split > 1) {
         MOC_PROF("cross_join", st);
         constexpr int SL = kJoinThreads / (D / 4);
-        if (a.split <= kJoinFew) cross_join_kernel<D, T, 1><<<(unsigned)((a.rows + SL - 1) / SL), kJoinThreads, 0, st>>>(a);
+        if (a.split <= kJoinFew || a.rows >= kJoinRows) cross_join_kernel<D, T, 1><<<(unsigned)((a.rows + SL - 1) / SL), kJoinThreads, 0, st>>>(a);
         else cross_join_kernel<D, T, SL><<<(unsigned)a.rows, kJoinThreads, 0, st>>>(a);
     }
 }

@@ -1,0 +1,40 @@
+"""Sizes at the edge of what cross attention and the head norms take: answered on the host, so no GPU is needed."""
+import ctypes as C
+
+import pytest
+
+from paper_2508_21058_amd import binding as mb
+
+
+def cross_bytes(B, H, Hk, N, M, d=128, S=1, dt=0, bwd=1):
+    """Workspace bytes, or the (negative) refusal."""
+    n = C.c_size_t()
+    rc = mb.lib().moc_cross_attn_workspace_bytes(B, H, Hk, N, M, d, S, dt, bwd, C.byref(n))
+    return n.value if rc == 0 else rc
+
+
+@pytest.mark.parametrize("dt,terms", [(0, 1 << 20), (1, 1 << 15)])
+def test_long_sums_are_cut_however_well_a_call_fills_the_chip(dt, terms):
+    """1,025 tiles of queries, or of states: without a limit of their length such sums are one part, without room for others."""
+    N = 131_200
+    assert cross_bytes(1, 1, 1, N, terms, dt=dt, bwd=0) == 0
+    for parts in (2, 5):
+        assert cross_bytes(1, 1, 1, N, (parts - 1) * terms + 1, dt=dt, bwd=0) >= parts * N * (128 + 1) * 4
+    M = 262_400
+    for parts in (1, 2, 5):
+        queries = max((parts - 1) * terms + 1, 1 << 14)
+        stats, sums = queries * 16, parts * M * 2 * 128 * 4 if parts > 1 else 0
+        assert cross_bytes(1, 1, 1, queries, M, dt=dt) - stats >= sums
+    # the queries of all heads of a key head count
+    assert cross_bytes(1, 8, 1, terms // 4, M, dt=dt) >= 2 * M * 2 * 128 * 4
+
+
+def test_parts_that_no_launch_has_room_for():
+    assert cross_bytes(1, 1024, 1, 65_000, 1 << 25, bwd=0) > 0              # 508 x 1,024 tiles in 32 parts
+    assert cross_bytes(1, 1024, 1, 65_000, (1 << 25) + 1, bwd=0) == -2      # ... in 33
+    assert cross_bytes(2, 65, 65, 1 << 20, 1 << 15, dt=1, bwd=0) >= 0
+    assert cross_bytes(2, 65, 65, 1 << 20, (1 << 15) + 1, dt=1, bwd=0) == -2     # more rows than a launch joins
+    assert cross_bytes(1, 16, 16, 1 << 15, 1 << 21, dt=1) > 0               # 2^18 tiles of states
+    assert cross_bytes(1, 16, 16, 1 << 21, 1 << 21, dt=1) == -2             # ... of which each has its queries in 64 parts
+    assert cross_bytes(1, 16, 16, 1 << 15, 1 << 22, dt=1) > 0
+    assert cross_bytes(1, 32, 16, (1 << 14) + 1, 1 << 22, dt=1) == -2       # 2^26 states in two parts, more than a launch adds
