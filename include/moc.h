@@ -356,7 +356,7 @@ typedef struct moc_rope_plan {
  *   q_weight, k_weight  DEVICE [d] float or NULL (ones); eps finite and >= 0.
  *   q_out, k_out, v_out DEVICE out, contiguous [B, heads, N, d], NULL where the input is NULL.
  * Rows are in float, sums too; results are rounded once, to `dtype`. N here is free of any
- * layout (an encoder's states have their own); B * N < 2^28, B * heads * N < 2^31. Outputs
+ * layout (an encoder's states have their own); B * N < 2^28 (<= 2^28 - 16 with 128 features), B * heads * N < 2^31. Outputs
  * must not overlap inputs.
  *
  * moc_qk_norm_rope_bwd: gradients of the same call. d_q_out, d_k_out, d_v_out (DEVICE in,

@@ -905,9 +905,10 @@ int check_heads(int32_t B, int32_t N, int32_t H, int32_t d, int dtype) {
     if (dtype != MOC_BF16 && dtype != MOC_F32) return fail(MOC_ERR_DTYPE, "dtype must be MOC_BF16 or MOC_F32");
     if (B <= 0 || N <= 0 || H <= 0) return fail(MOC_ERR_SHAPE, "B, N and the heads must be positive");
     if (d != 64 && d != 128) return fail(MOC_ERR_SHAPE, "d must be 64 or 128");
-    // (a launch has fewer than 2^32 threads: sixteen a token of 128 features)
     if ((long long)B * N >= (1LL << 28) || (long long)B * N * H >= (1LL << 31))
         return fail(MOC_ERR_SHAPE, "B * N must be < 2^28 and B * heads * N < 2^31");
+    // (a launch has fewer than 2^32 threads, 256 a workgroup; one takes 16 tokens of 128 features)
+    if (moc::row_grid(B, N, 1, d, false).blocks >= 1 << 24) return fail(MOC_ERR_SHAPE, "B * N must be <= 2^28 - 16 with 128 features");
     return MOC_OK;
 }
 

@@ -38,3 +38,43 @@ def test_parts_that_no_launch_has_room_for():
     assert cross_bytes(1, 16, 16, 1 << 21, 1 << 21, dt=1) == -2             # ... of which each has its queries in 64 parts
     assert cross_bytes(1, 16, 16, 1 << 15, 1 << 22, dt=1) > 0
     assert cross_bytes(1, 32, 16, (1 << 14) + 1, 1 << 22, dt=1) == -2       # 2^26 states in two parts, more than a launch adds
+
+
+P = 0x10000
+LAST_128 = (1 << 28) - 16       # tokens of 2^24 - 1 workgroups of sixteen
+
+
+def rows():
+    return mb._ROWS.pack(P, 128, 128, 128)
+
+
+def rope():
+    return C.byref(mb._RopePlan(P, P, 1, (C.c_int32 * 4)(10, 0, 0, 0), 0))
+
+
+def norm_bytes(B, N, d):
+    n = C.c_size_t()
+    return mb.lib().moc_qk_norm_rope_workspace_bytes(B, N, 1, 1, d, 0, C.byref(n))
+
+
+def norm_forward(B, N, d):
+    return mb.lib().moc_qk_norm_rope(B, N, 1, 1, d, 0, rows(), None, None, None, None, 1e-6, None, P, None, None, None)
+
+
+def norm_backward(B, N, d):
+    return mb.lib().moc_qk_norm_rope_bwd(B, N, 1, 1, d, 0, rows(), None, None, None, 1e-6, None, P, None, None, rows(), None, None, None, None,
+                                         P, 1 << 30, None)
+
+
+def turn(B, N, d):
+    return mb.lib().moc_rope(B, N, 1, d, 0, rows(), rope(), 0, rows(), None)
+
+
+@pytest.mark.parametrize("call", [norm_bytes, norm_forward, norm_backward, turn])
+@pytest.mark.parametrize("B,N,d", [(1, LAST_128 + 1, 128), (1, (1 << 28) - 1, 128), (3, (1 << 28) // 3, 128), (1, 1 << 28, 64)])
+def test_tokens_of_2_24_workgroups_are_refused(call, B, N, d):
+    assert call(B, N, d) == -2
+
+
+def test_tokens_that_a_launch_holds():
+    assert norm_bytes(1, LAST_128, 128) == 0 and norm_bytes(1, (1 << 28) - 1, 64) == 0
