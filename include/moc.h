@@ -412,7 +412,8 @@ int moc_rope(int32_t B, int32_t N, int32_t H, int32_t d, int dtype, const moc_ro
  *
  * moc_cross_attn_bwd: dq [B,H,N,d], dk, dv [B,Hk,M,d] (fully overwritten; dk and dv are summed over the
  * query heads of a key head) from the forward's o and lse and d_o [B,H,N,d]. Every sum has a fixed order: same
- * input, same bits. workspace: moc_cross_attn_workspace_bytes(..., with_bwd) bytes, which
+ * input, same bits. Outputs and the workspace must not overlap inputs or each other (MOC_ERR_SHAPE), but o may be q itself,
+ * dq may be o, dk k and dv v. workspace: moc_cross_attn_workspace_bytes(..., with_bwd) bytes, which
  * serve both calls; nothing is kept in it between calls, and calls that may run side by side need one
  * each. No call allocates or waits, so they can be captured into a HIP graph.
  */

@@ -967,6 +967,23 @@ int check_cross(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t 
     return MOC_OK;
 }
 
+// Outputs must not overlap inputs or each other, but output i < in_place may be input i itself.
+struct Span { const void *data; size_t bytes; };
+int check_overlap(const Span *out, int n_out, const Span *in, int n_in, int in_place) {
+    auto apart = [](const Span &x, const Span &y) {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(x.data), b = reinterpret_cast<uintptr_t>(y.data);
+        return !a || !b || !x.bytes || !y.bytes || (a < b ? b - a >= x.bytes : a - b >= y.bytes);
+    };
+    for (int i = 0; i < n_out; ++i) {
+        for (int j = 0; j < n_in; ++j)
+            if (!apart(out[i], in[j]) && !(i == j && i < in_place && out[i].data == in[j].data))
+                return fail(MOC_ERR_SHAPE, "an output or the workspace overlaps an input");
+        for (int j = 0; j < i; ++j)
+            if (!apart(out[i], out[j])) return fail(MOC_ERR_SHAPE, "outputs or the workspace overlap");
+    }
+    return MOC_OK;
+}
+
 int too_many_parts() { return fail(MOC_ERR_SHAPE, "too many tiles for the parts that sums over so many states or queries are cut into"); }
 
 // The parts of a call that both directions share.
@@ -1137,6 +1154,11 @@ int moc_cross_attn_fwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, i
     if (!p.fits) return too_many_parts();
     if (p.total > 0 && (!workspace || workspace_bytes < p.total)) return fail(MOC_ERR_WORKSPACE, "cross attention workspace too small");
     if (misaligned(workspace)) return fail(MOC_ERR_ALIGN, "workspace must be 16-byte aligned");
+    const size_t row = (size_t)d * (dtype == MOC_F32 ? 4 : 2), q_bytes = (size_t)a.rows * row, k_bytes = (size_t)B * Hk * M * row, l_bytes = (size_t)a.rows * 4;
+    const Span out[] = {{o, q_bytes}, {lse, l_bytes}, {workspace, p.total}};
+    const Span in[] = {{q, q_bytes}, {k, k_bytes}, {v, k_bytes}, {kv_ranges, (size_t)B * S * 8}};
+    rc = check_overlap(out, 3, in, 4, 1);
+    if (rc) return rc;
     char *ws = static_cast<char *>(workspace);
     a.q = q; a.k = k; a.v = v; a.o = o; a.lse = lse;
     a.split = p.split_q;
@@ -1163,6 +1185,11 @@ int moc_cross_attn_bwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, i
     if (!p.fits) return too_many_parts();
     if (!workspace || workspace_bytes < p.total) return fail(MOC_ERR_WORKSPACE, "cross attention workspace too small (with_bwd)");
     if (misaligned(workspace)) return fail(MOC_ERR_ALIGN, "workspace must be 16-byte aligned");
+    const size_t row = (size_t)d * (dtype == MOC_F32 ? 4 : 2), q_bytes = (size_t)a.rows * row, k_bytes = (size_t)B * Hk * M * row, l_bytes = (size_t)a.rows * 4;
+    const Span out[] = {{dq, q_bytes}, {dk, k_bytes}, {dv, k_bytes}, {workspace, p.total}};
+    const Span in[] = {{o, q_bytes}, {k, k_bytes}, {v, k_bytes}, {q, q_bytes}, {d_o, q_bytes}, {lse, l_bytes}, {kv_ranges, (size_t)B * S * 8}};
+    rc = check_overlap(out, 4, in, 7, 3);
+    if (rc) return rc;
     char *ws = static_cast<char *>(workspace);
     a.q = q; a.k = k; a.v = v; a.o_in = o; a.lse_in = lse; a.d_o = d_o;
     a.dq = dq; a.dk = dk; a.dv = dv;

@@ -78,3 +78,37 @@ def test_tokens_of_2_24_workgroups_are_refused(call, B, N, d):
 
 def test_tokens_that_a_launch_holds():
     assert norm_bytes(1, LAST_128, 128) == 0 and norm_bytes(1, (1 << 28) - 1, 64) == 0
+
+
+# ---- tensors on top of one another: made-up addresses, far apart unless a case says otherwise. B = 2, H = 4, Hk = 2, N = 10, M = 600, 128 features, bf16
+MIB = 1 << 20
+Q_BYTES, K_BYTES, LSE_BYTES = 2 * 4 * 10 * 128 * 2, 2 * 2 * 600 * 128 * 2, 2 * 4 * 10 * 4
+AT = {n: (i + 1) * 64 * MIB for i, n in enumerate(("q", "k", "v", "o", "lse", "d_o", "dq", "dk", "dv", "ranges", "ws"))}
+
+
+def cross_at(backward, **moved):
+    p = {**AT, **moved}
+    head, mid = (2, 4, 2, 10, 600, 128, 0, p["q"], p["k"], p["v"]), (1, None, p["ranges"], 0.1)
+    if backward:
+        return mb.lib().moc_cross_attn_bwd(*head, p["o"], p["lse"], p["d_o"], *mid, p["dq"], p["dk"], p["dv"], p["ws"], 32 * MIB, None)
+    return mb.lib().moc_cross_attn_fwd(*head, *mid, p["o"], p["lse"], p["ws"], 32 * MIB, None)
+
+
+@pytest.mark.parametrize("moved", [
+    dict(o=AT["q"] + 16), dict(o=AT["q"] + Q_BYTES - 16), dict(o=AT["q"] - Q_BYTES + 16), dict(o=AT["k"]), dict(o=AT["v"] + K_BYTES - 16), dict(lse=AT["q"]),
+    dict(lse=AT["o"] + Q_BYTES - 16), dict(lse=AT["k"] - LSE_BYTES + 16), dict(o=AT["ranges"]), dict(lse=AT["ranges"]), dict(ws=AT["q"]), dict(ws=AT["k"] + K_BYTES - 16),
+    dict(ws=AT["o"]), dict(ws=AT["ranges"]),
+])
+def test_cross_attention_refuses_overlaps(moved):
+    assert cross_at(False, **moved) == -2
+    assert b"overlap" in mb.lib().moc_last_error()
+
+
+@pytest.mark.parametrize("moved", [
+    dict(dq=AT["q"]), dict(dq=AT["d_o"]), dict(dq=AT["o"] + 32), dict(dq=AT["k"]), dict(dq=AT["lse"]), dict(dk=AT["q"]), dict(dk=AT["d_o"] - K_BYTES + 16), dict(dk=AT["v"]),
+    dict(dk=AT["k"] + 256), dict(dv=AT["k"]), dict(dv=AT["v"] - 256), dict(dv=AT["dk"] + K_BYTES - 16), dict(dk=AT["dq"]), dict(dv=AT["dq"] + 16), dict(dq=AT["ranges"]),
+    dict(ws=AT["lse"]), dict(ws=AT["dv"]), dict(ws=AT["d_o"] - 256), dict(dv=AT["ranges"]),
+])
+def test_cross_attention_backward_refuses_overlaps(moved):
+    assert cross_at(True, **moved) == -2
+    assert b"overlap" in mb.lib().moc_last_error()
