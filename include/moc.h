@@ -319,7 +319,8 @@ int moc_attn_bwd_after_fwd(const moc_meta *meta, int32_t B, int32_t H, int32_t d
  * moc_rows: a [B, heads, N, d] tensor in any order of memory. Element
  * (b, h, n, e) lies at data + b*stride_b + h*stride_h + n*stride_n + e; strides
  * count elements, the d features of a row are contiguous. data has to be
- * 16-byte aligned and the strides multiples of 16 bytes (MOC_ERR_ALIGN). A slice
+ * 16-byte aligned and the strides multiples of 16 bytes (MOC_ERR_ALIGN). An input may
+ * have strides of 0 (a broadcast one); rows of an output must not overlap (MOC_ERR_SHAPE). A slice
  * of a fused projection [B, N, 3H, d] is such a tensor, and so is a head-major one.
  *
  * moc_rope_plan: how tokens are turned. The d features of a head are d/2 pairs:

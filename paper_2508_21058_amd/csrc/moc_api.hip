@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cstdio>
+#include <cstdlib>
 #include <map>
 #include <mutex>
 #include <cstring>
@@ -924,6 +925,15 @@ int check_rows(const moc_rows *r, int32_t B, int32_t N, int32_t H, int dtype, lo
     return MOC_OK;
 }
 
+// ... that is written: neighbouring rows, heads or samples of it must not share elements.
+int check_rows_out(const moc_rows *r, int32_t B, int32_t N, int32_t H, int32_t d, int dtype, long long *sb, long long *sh, long long *sn) {
+    const int rc = check_rows(r, B, N, H, dtype, sb, sh, sn);
+    if (rc) return rc;
+    if ((B > 1 && std::abs(*sb) < d) || (H > 1 && std::abs(*sh) < d) || (N > 1 && std::abs(*sn) < d))
+        return fail(MOC_ERR_SHAPE, "rows of an output overlap: a stride is smaller than d");
+    return MOC_OK;
+}
+
 int check_rope(const moc_rope_plan *p, int32_t d, moc::RowArgs &a) {
     if (!p->positions || !p->freq) return fail(MOC_ERR_NULL, "positions or freq is NULL");
     if ((reinterpret_cast<uintptr_t>(p->positions) & 3u) || (reinterpret_cast<uintptr_t>(p->freq) & 7u))
@@ -1086,7 +1096,7 @@ int moc_qk_norm_rope_bwd(int32_t B, int32_t N, int32_t H, int32_t Hk, int32_t d,
             if (rc) return rc;
             hp.x = in[p]->data;
         }
-        rc = check_rows(out[p], B, N, hp.heads, dtype, &hp.o_b, &hp.o_h, &hp.o_n);
+        rc = check_rows_out(out[p], B, N, hp.heads, d, dtype, &hp.o_b, &hp.o_h, &hp.o_n);
         if (rc) return rc;
         if (misaligned(grad[p])) return fail(MOC_ERR_ALIGN, "device pointers must be 16-byte aligned");
         hp.g = grad[p];
@@ -1114,7 +1124,7 @@ int moc_rope(int32_t B, int32_t N, int32_t H, int32_t d, int dtype, const moc_ro
     moc::RowArgs a{};
     moc::HeadPart &hp = a.part[0];
     rc = check_rows(x, B, N, H, dtype, &hp.x_b, &hp.x_h, &hp.x_n);
-    if (!rc) rc = check_rows(out, B, N, H, dtype, &hp.o_b, &hp.o_h, &hp.o_n);
+    if (!rc) rc = check_rows_out(out, B, N, H, d, dtype, &hp.o_b, &hp.o_h, &hp.o_n);
     if (!rc) rc = check_rope(rope, d, a);
     if (rc) return rc;
     hp.x = x->data;

@@ -112,3 +112,27 @@ def test_cross_attention_refuses_overlaps(moved):
 def test_cross_attention_backward_refuses_overlaps(moved):
     assert cross_at(True, **moved) == -2
     assert b"overlap" in mb.lib().moc_last_error()
+
+
+# ---- outputs whose rows lie on top of one another: B = 2, N = 8, H = 2 and Hk = 2 heads of 128 features
+def turn_into(out):
+    return mb.lib().moc_rope(2, 8, 2, 128, 0, mb._ROWS.pack(P, 2048, 128, 256), rope(), 0, out, None)
+
+
+def norm_backward_into(dq=None, dk=None, dv=None):
+    far = [mb._ROWS.pack((i + 1) << 24, 2048, 128, 256) for i in range(3)]
+    x = mb._ROWS.pack(P, 2048, 128, 256)
+    return mb.lib().moc_qk_norm_rope_bwd(2, 8, 2, 2, 128, 0, x, x, None, None, 1e-6, None, P, P, P, dq or far[0], dk or far[1], dv or far[2], None, None,
+                                         P, 1 << 30, None)
+
+
+OVERLAID = [(0, 128, 256), (2048, 0, 256), (2048, 128, 0), (2048, 64, 256), (2048, 2048, 120), (-64, 128, 256)]       # strides of samples, heads, tokens
+
+
+@pytest.mark.parametrize("strides", OVERLAID)
+def test_output_rows_on_top_of_one_another_are_refused(strides):
+    out = mb._ROWS.pack(1 << 24, *strides)
+    assert turn_into(out) == -2
+    for name in ("dq", "dk", "dv"):
+        assert norm_backward_into(**{name: out}) == -2
+    assert b"overlap" in mb.lib().moc_last_error()
