@@ -490,6 +490,13 @@ def _weight(w: Optional[torch.Tensor], d: int):
     return w.data_ptr()
 
 
+def _scratch(ws: torch.Tensor):
+    """Address and bytes of a workspace: what a strided or expanded tensor counts is not what lies behind its address."""
+    if not ws.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 def _need_like(t: torch.Tensor, shape, like: torch.Tensor):
     """A contiguous tensor of a shape, of `like`'s dtype and device."""
     if t.shape != shape or t.dtype != like.dtype or t.device != like.device or not t.is_contiguous():
@@ -573,7 +580,7 @@ def qk_norm_rope_bwd(q, k, d_q_out, d_k_out, d_v_out=None, q_weight=None, k_weig
     dqw, dkw = None if q is None else dw[0], None if k is None else dw[1]
     ws = workspace if workspace is not None else qk_norm_rope_workspace(B, N, H, Hk, d, some.dtype, some.device)
     _call(l.moc_qk_norm_rope_bwd, device, B, N, H, Hk, d, dt, _rows(q, True), _rows(k, True), _weight(q_weight, d), _weight(k_weight, d), eps,
-          _plan(rope, N, some.device), *_ptrs(*grads), *[_rows(o, True) for o in out], *_ptrs(dqw, dkw), ws.data_ptr(), ws.numel(), stream)
+          _plan(rope, N, some.device), *_ptrs(*grads), *[_rows(o, True) for o in out], *_ptrs(dqw, dkw), *_scratch(ws), stream)
     return (*out, dqw, dkw)
 
 
@@ -639,7 +646,7 @@ def cross_attn_fwd(q, k, v, kv_ranges: Optional[torch.Tensor] = None, q_offsets=
         _need_lse(lse, q)
     _call(l.moc_cross_attn_fwd, device, B, H, Hk, N, M, d, dt, q.data_ptr(), k.data_ptr(), v.data_ptr(), S,
           None if off is None else off.ctypes.data, None if kv_ranges is None else kv_ranges.data_ptr(),
-          d ** -0.5 if scale is None else scale, o.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(), stream)
+          d ** -0.5 if scale is None else scale, o.data_ptr(), lse.data_ptr(), *_scratch(ws), stream)
     return o, lse
 
 
@@ -664,5 +671,5 @@ def cross_attn_bwd(q, k, v, o, lse, d_o, kv_ranges: Optional[torch.Tensor] = Non
     _call(l.moc_cross_attn_bwd, device, B, H, Hk, N, M, d, dt, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
           lse.data_ptr(), d_o.data_ptr(), S, None if off is None else off.ctypes.data,
           None if kv_ranges is None else kv_ranges.data_ptr(), d ** -0.5 if scale is None else scale, dq.data_ptr(),
-          dk.data_ptr(), dv.data_ptr(), ws.data_ptr(), ws.numel(), stream)
+          dk.data_ptr(), dv.data_ptr(), *_scratch(ws), stream)
     return dq, dk, dv

@@ -2,6 +2,7 @@
 import ctypes as C
 
 import pytest
+import torch
 
 from paper_2508_21058_amd import binding as mb
 
@@ -136,3 +137,11 @@ def test_output_rows_on_top_of_one_another_are_refused(strides):
     for name in ("dq", "dk", "dv"):
         assert norm_backward_into(**{name: out}) == -2
     assert b"overlap" in mb.lib().moc_last_error()
+
+
+def test_workspaces_count_what_lies_behind_their_address():
+    whole = torch.empty(64, dtype=torch.uint8)
+    assert mb._scratch(whole) == (whole.data_ptr(), 64) and mb._scratch(whole.view(torch.float32))[1] == 64
+    for ws in (whole[:1].expand(1 << 20), whole[::2], whole.view(8, 8)[:, :4]):
+        with pytest.raises(ValueError):
+            mb._scratch(ws)
