@@ -5,10 +5,11 @@
 // product from the registers they are in. Calls of few query tiles split the range over workgroups, whose results a second launch joins.
 //
 // In bf16 three workgroups share a compute unit (168 registers, tiles of 32 states): 114k queries of 24 heads, eight shots of captions of 100 to 512
-// states 569 -> 506 us against two of 64-state tiles (of 32: 594), 33k queries against 4,357 states 1,886 -> 1,835.
+// states 569 -> 506 us against two of 64-state tiles (of 32: 594), 33k queries against 4,357 states 1,886 -> 1,835
+// (cards differ by 7 %: on another one tile buffers as constants took the latter from 1,790 to 1,723).
 //
-// What bounds it: at long ranges the products (the latter 1,640 us with tile buffers as constants, 1,090 TFLOP/s, near what the chip's power allows);
-// at short ones products and vector work, which share a SIMD's issue (39 % of the cycles each), and the rows of q and o, 130 of the 506 us.
+// What bounds it: at long ranges the products (the latter stands at 1,640 to 1,650 us, 1,080 TFLOP/s, near what the chip's power allows); at short ones
+// products and vector work, which share a SIMD's issue (39 % of the cycles each), and the rows of q and o, 130 of the 506 us.
 #include "moc_cross.h"
 
 namespace moc {

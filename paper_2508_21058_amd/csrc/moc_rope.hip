@@ -17,9 +17,10 @@ constexpr int kRowThreads = 256;
 // Workgroups wanted. The forward takes many short ones, so that the last round of the chip is short, but at least eight heads each where there are
 // enough tokens, since each forms the angles anew: 33k tokens of 24 heads 91 us with a workgroup per 16 tokens (2,080 of them, 2,048 at a time),
 // 85 with three, 83 with eight; 6k tokens (q, k and v) 41.5 with three, 43.5 with 18, 55.5 with 36. The backward's, of
-// which two fit a compute unit (174 registers), take several blocks of tokens one after the other, all of them in one round, so that the weights'
+// which two fit a compute unit (174 to 181 registers), take several blocks of tokens one after the other, all of them in one round, so that the weights'
 // partial sums are few: 512, 1,024, 1,536 of them 53.5, 60.5, 66 us (two samples of 16k tokens, twelve and four heads of 64), 351, 357, 353
-// (33k tokens of 24 heads of 128).
+// (33k tokens of 24 heads of 128). Whole blocks of tokens each: calls of a few blocks more than a round's take a round more for them (24 heads of
+// 128: 4,096 / 4,099 tokens 42 / 56 us, 8,192 / 8,200 88 / 110, 12,288 / 12,300 129 / 138; 6,256 tokens 73, 4.2 TB/s).
 constexpr int kRowWgs = 6144, kRowWgsFew = 512, kRowHeadsMin = 8, kRowWgsBwd = 512;
 
 RowGrid row_grid(int B, int N, int heads_total, int d, bool bwd) {
