@@ -404,8 +404,8 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
             return (w / 2 * two + w % 2 * one) * std::max(1., work / s) + (w + 1) / 2 * 6 + (s > 1 ? s * sums + 6 : 0);
         };
         double best = 0;
-        const long long most = std::min({256LL, (M + 127LL) / 128, 4 * kComputeUnits / tiles + 1});
-        for (long long s = least_q; s <= std::max(least_q, most); ++s) {
+        const long long most = std::max(std::min({256LL, (M + 127LL) / 128, 4 * kComputeUnits / tiles + 1}), least_q > 1 && tiles <= 4 * kComputeUnits ? least_q + 3 : least_q);
+        for (long long s = least_q; s <= most; ++s) {
             const double us = time(s, tiles, stages) + (S > 1 ? time(s, own_tiles, stages / S) : 0);
             if (s == least_q || us < best) { best = us; p.split_q = (int)s; }
         }
@@ -435,9 +435,11 @@ CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype
             const double rounds = std::max((double)((n * s + units - 1) / units), pieces ? 1.2 * n * s / units : 0);
             return rounds * (stage * std::max(1., work / s) + begin) + (s > 1 ? s * sums + 5 : 0);
         };
-        const long long most = std::min({1024LL, (long long)std::ceil(std::max(stages, own_stages) / (bf16 ? 2 : 1)), 3 * units / tiles + 1});
+        // (from the least number of parts on, since that one may be a bad number of rounds: 24 heads in fp32, 46k queries each of two, 1,827 states in 2 / 3 / 7
+        // parts 34.3 / 37.7 / 32.7 ms)
+        const long long most = std::max(std::min({1024LL, (long long)std::ceil(std::max(stages, own_stages) / (bf16 ? 2 : 1)), 3 * units / tiles + 1}), least_kv > 1 ? 3 * least_kv : 1);
         double best = 0;
-        for (long long s = least_kv; s <= std::max(least_kv, most) && (s == least_kv || (s * states * d * 8 <= 512 << 20 && heads * p.max_items * s < 1 << 20));
+        for (long long s = least_kv; s <= most && (s == least_kv || (s * states * d * 8 <= 512 << 20 && heads * p.max_items * s < 1 << 20));
              s += 1 + s / 64) {
             const double us = time(s, tiles, stages) + (S > 1 ? time(s, own_tiles, own_stages) : 0);
             if (s == least_kv || us < best) { best = us; parts = (int)s; }
