@@ -430,6 +430,60 @@ int moc_cross_attn_bwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, i
                        void *dv, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * A key / value cache held in 8 bits, for sampling that attends what was made before: frames of a rollout, tokens of an
+ * autoregressive one, or an encoder's states that every sampling step reads again. One call writes it, one reads
+ * it back (for moc_route and moc_attn_*, say), one attends it.
+ *
+ * moc_cache: a pool of pages of MOC_CACHE_PAGE tokens, and a table that says where the tokens of a sample are.
+ *   k, v          DEVICE [pages][Hk][MOC_CACHE_PAGE][d] codes in e4m3 (OCP: no infinities), 16-byte aligned
+ *   k_exp, v_exp  DEVICE [pages][Hk] int8: the value of a code is code * 2^exponent. Exponents are -110 .. 120 (others are taken
+ *                 for the nearest of these), so that every value is a normal number of bf16, exactly.
+ *   table         DEVICE [B][blocks] int32: tokens [64 i, 64 i + 64) of sample b are on page table[b][i]. A number that is
+ *                 no page (-1, say) is never followed: those tokens are not there. Rows may share pages that are only read.
+ * A pool filled with zeros holds zeros. Keep 64 * blocks < 2^26 and B * Hk <= 65535.
+ *
+ * moc_cache_write: token n of sample b goes to position starts[b] + n, for n < counts[b].
+ *   k, v          DEVICE in, moc_rows of Hk heads, e.g. slices of a fused projection or what moc_qk_norm_rope left
+ *   starts, counts  DEVICE [B] int32 or NULL (0; N); counts are clipped to [0, N].
+ * A head's exponent on a page is the least one with |x| <= 448 * 2^exponent for every finite x that is written to it now, and not
+ * less than before where tokens in front of starts[b] share the page; these keep their values as long as they are not
+ * subnormal codes (below 2^(exponent - 6)), which are rounded again. Values are rounded to nearest, ties to even; NaN and
+ * infinities become NaN (and do not touch other tokens). Positions behind starts[b] + counts[b] on a page that is written to hold nothing
+ * afterwards (their codes stay, under another exponent): a write ends its sample there. Positions below 0 or without a page are
+ * dropped. Pages that one call writes must differ: two samples that append to one page race.
+ *
+ * moc_cache_read: k_out, v_out (DEVICE out, contiguous [B,Hk,N,d], either may be NULL) from the positions starts[b] + n; rows
+ * n >= counts[b], and positions that are not there, are 0. MOC_BF16 and MOC_F32 both hold the values exactly.
+ *
+ * moc_cache_attn: moc_cross_attn_fwd with cached states: q [B,H,N,d], Hk divides H, segments of the queries with a range of positions
+ * each ([first, end), clipped to [0, 64 * blocks); kv_ranges NULL: everything that the table names), o [B,H,N,d], lse [B,H,N] float. Positions
+ * that are not there are left out, so an evicted page, or one that a selection skips, is a -1 in the table. A query that attends nothing
+ * has o = 0, lse = -infinity. Positions outside of a range are never used, whatever their pages hold.
+ * MOC_BF16: products on bf16 matrix cores, softmax and sums in float, probabilities rounded to bf16. MOC_F32: queries and probabilities as
+ * three bf16 terms each, which is as exact as products of floats. Sums over more than 2^20 positions (MOC_F32: 2^18) are
+ * cut into parts. B * H <= 65535, H / Hk * N < 2^26, B * H * N < 2^31; a call of more tiles than a launch has workgroups is MOC_ERR_SHAPE.
+ * workspace: moc_cache_attn_workspace_bytes bytes; calls that may run side by side need one each. o may be q itself; other outputs and the
+ * workspace must not overlap inputs, the cache or each other.
+ *
+ * None of these calls allocates or waits, so they can be captured into a HIP graph: starts, counts, the table and the ranges
+ * are read on the device. Same input, same bits.
+ */
+#define MOC_CACHE_PAGE 64
+typedef struct moc_cache {
+    void *k, *v;
+    int8_t *k_exp, *v_exp;
+    const int32_t *table;
+    int32_t pages, blocks, Hk, d;
+} moc_cache;
+int moc_cache_write(const moc_cache *cache, int32_t B, int32_t N, int dtype, const moc_rows *k, const moc_rows *v, const int32_t *starts,
+                    const int32_t *counts, void *stream);
+int moc_cache_read(const moc_cache *cache, int32_t B, int32_t N, int dtype, const int32_t *starts, const int32_t *counts, void *k_out,
+                   void *v_out, void *stream);
+int moc_cache_attn_workspace_bytes(const moc_cache *cache, int32_t B, int32_t H, int32_t N, int32_t S, int dtype, size_t *bytes);
+int moc_cache_attn(const moc_cache *cache, int32_t B, int32_t H, int32_t N, int dtype, const void *q, int32_t S, const int32_t *q_offsets,
+                   const int32_t *kv_ranges, float softmax_scale, void *o, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Per-kernel timing (measurement aid, not part of the layer). While enabled,
  * every kernel launch of the library is bracketed by HIP events recorded on the
  * launch stream. moc_prof_enable(on) clears the records. moc_prof_read(-1, ...)

@@ -29,6 +29,7 @@ SYMBOLS = ["moc_status_string", "moc_last_error", "moc_chunk_meta", "moc_meta_de
            "moc_attn_bwd", "moc_attn_bwd_after_fwd",
            "moc_qk_norm_rope", "moc_qk_norm_rope_workspace_bytes", "moc_qk_norm_rope_bwd", "moc_rope",
            "moc_cross_attn_workspace_bytes", "moc_cross_attn_fwd", "moc_cross_attn_bwd",
+           "moc_cache_write", "moc_cache_read", "moc_cache_attn_workspace_bytes", "moc_cache_attn",
            "moc_prof_enable", "moc_prof_read", "moc_probe"]
 
 
@@ -87,6 +88,10 @@ def lib():
                                      vp, sz, vp]
     l.moc_cross_attn_bwd.argtypes = [i32, i32, i32, i32, i32, i32, C.c_int, vp, vp, vp, vp, vp, vp, i32, vp, vp,
                                      C.c_float, vp, vp, vp, vp, sz, vp]
+    l.moc_cache_write.argtypes = [vp, i32, i32, C.c_int, vp, vp, vp, vp, vp]
+    l.moc_cache_read.argtypes = [vp, i32, i32, C.c_int, vp, vp, vp, vp, vp]
+    l.moc_cache_attn_workspace_bytes.argtypes = [vp, i32, i32, i32, i32, C.c_int, C.POINTER(sz)]
+    l.moc_cache_attn.argtypes = [vp, i32, i32, i32, C.c_int, vp, i32, vp, vp, C.c_float, vp, vp, vp, sz, vp]
     l.moc_probe.argtypes = [i32, vp, sz, i32, vp, C.POINTER(C.c_float), C.POINTER(C.c_double)]
     l.moc_prof_enable.argtypes = [C.c_int]
     l.moc_prof_read.argtypes = [i32, C.c_char_p, sz, C.POINTER(i32), C.POINTER(C.c_float)]
@@ -673,3 +678,127 @@ def cross_attn_bwd(q, k, v, o, lse, d_o, kv_ranges: Optional[torch.Tensor] = Non
           None if kv_ranges is None else kv_ranges.data_ptr(), d ** -0.5 if scale is None else scale, dq.data_ptr(),
           dk.data_ptr(), dv.data_ptr(), *_scratch(ws), stream)
     return dq, dk, dv
+
+
+# ---- a key / value cache in 8 bits ------------------------------------------------------------------------------------
+
+MOC_CACHE_PAGE = 64
+
+
+class _Cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p), ("table", C.c_void_p),
+                ("pages", C.c_int32), ("blocks", C.c_int32), ("Hk", C.c_int32), ("d", C.c_int32)]
+
+
+class KVCache:
+    """A cache (moc_cache) over tensors of the caller: k, v [pages, Hk, 64, d] float8_e4m3fn codes, k_exp, v_exp [pages, Hk] int8
+    (a value is code * 2^exponent) and table [B, blocks] int32, the page of each 64 tokens of a sample (no page: -1). The
+    table may be written between calls, on the device; its tensor stays the same."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor, table: torch.Tensor):
+        if k.dim() != 4 or k.shape[2] != MOC_CACHE_PAGE or k.shape != v.shape or k_exp.shape != k.shape[:2] or v_exp.shape != k.shape[:2]:
+            raise ValueError("need k, v [pages, Hk, 64, d] and k_exp, v_exp [pages, Hk]")
+        if k.dtype != torch.float8_e4m3fn or v.dtype != k.dtype or k_exp.dtype != torch.int8 or v_exp.dtype != torch.int8:
+            raise TypeError("need float8_e4m3fn pages and int8 exponents")
+        if table.dim() != 2 or table.dtype != torch.int32:
+            raise TypeError("the table must be an int32 tensor [B, blocks]")
+        if not all(t.is_contiguous() for t in (k, v, k_exp, v_exp, table)):
+            raise ValueError("tensors must be contiguous")
+        if any(t.device != k.device for t in (v, k_exp, v_exp, table)):
+            raise ValueError("tensors must be on one device")
+        self.k, self.v, self.k_exp, self.v_exp, self.table = k, v, k_exp, v_exp, table
+        self.B, self.blocks = table.shape
+        self.pages, self.Hk, _, self.d = k.shape
+        self.struct = _Cache(*_ptrs(k, v, k_exp, v_exp, table), self.pages, self.blocks, self.Hk, self.d)
+
+
+def kv_cache(B: int, tokens: int, Hk: int, d: int, pages: Optional[int] = None, device="cuda") -> KVCache:
+    """An empty cache (zeros) with room for `tokens` a sample; without `pages` every sample has its own pages, one behind
+    the other, else a pool of so many and a table of -1 that the caller fills."""
+    blocks = -(-int(tokens) // MOC_CACHE_PAGE)
+    own = pages is None
+    pages = B * blocks if own else int(pages)
+    if B <= 0 or blocks <= 0 or Hk <= 0 or pages <= 0:
+        raise ValueError("B, tokens, Hk and pages must be positive")
+    table = torch.arange(B * blocks, dtype=torch.int32, device=device).view(B, blocks) if own else \
+        torch.full((B, blocks), -1, dtype=torch.int32, device=device)
+    k, v = (torch.zeros((pages, Hk, MOC_CACHE_PAGE, d), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2))
+    ke, ve = (torch.full((pages, Hk), -110, dtype=torch.int8, device=device) for _ in range(2))
+    return KVCache(k, v, ke, ve, table)
+
+
+def _per_sample(t: Optional[torch.Tensor], B: int, name: str):
+    if t is not None and (t.dtype != torch.int32 or t.shape != (B,) or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous int32 tensor [{B}]")
+
+
+def cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None):
+    """Writes k, v [B, Hk, N, d] (any strides, contiguous features) to the positions starts[b] + n of every sample, n < counts[b]
+    (int32 tensors [B] on the device; None: 0 and N). What a sample held behind them is gone."""
+    if k.dim() != 4 or k.shape != v.shape or k.shape[0] != cache.B or k.shape[1] != cache.Hk or k.shape[3] != cache.d:
+        raise ValueError("need k and v [B, Hk, N, d] of the cache's B, Hk and d")
+    B, _, N, _ = k.shape
+    _per_sample(starts, B, "starts")
+    _per_sample(counts, B, "counts")
+    l = lib()
+    dt = _same_dtype(k, v)
+    device, stream = _on(k, v, cache.k, starts, counts)
+    _call(l.moc_cache_write, device, C.byref(cache.struct), B, N, dt, _rows(k, False), _rows(v, False), *_ptrs(starts, counts), stream)
+
+
+def cache_read(cache: KVCache, N: int, starts: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None,
+               dtype: torch.dtype = torch.bfloat16, out=None):
+    """-> k, v [B, Hk, N, d] from the positions starts[b] + n; 0 for n >= counts[b] and where the cache has no page. `out`: the two
+    tensors to fill, one of which may be None."""
+    B = cache.B
+    _per_sample(starts, B, "starts")
+    _per_sample(counts, B, "counts")
+    if out is None:
+        out = [torch.empty((B, cache.Hk, N, cache.d), dtype=dtype, device=cache.k.device) for _ in range(2)]
+    k, v = out
+    some = k if k is not None else v
+    if some is None:
+        raise ValueError("out holds no tensor")
+    for t in (k, v):
+        if t is not None:
+            _need_like(t, (B, cache.Hk, N, cache.d), some)
+    l = lib()
+    device, stream = _on(some, cache.k, starts, counts)
+    _call(l.moc_cache_read, device, C.byref(cache.struct), B, N, _dtype_code(some), *_ptrs(starts, counts), *_ptrs(k, v), stream)
+    return k, v
+
+
+def cache_attn_workspace(cache: KVCache, H: int, N: int, dtype: torch.dtype, segments: int = 1) -> torch.Tensor:
+    nbytes = C.c_size_t()
+    _check(lib().moc_cache_attn_workspace_bytes(C.byref(cache.struct), cache.B, H, N, segments, MOC_BF16 if dtype == torch.bfloat16 else MOC_F32,
+                                                C.byref(nbytes)), "moc_cache_attn_workspace_bytes")
+    return torch.empty(max(nbytes.value, 16), dtype=torch.uint8, device=cache.k.device)
+
+
+def cache_attn(q, cache: KVCache, kv_ranges: Optional[torch.Tensor] = None, q_offsets=None, scale: Optional[float] = None,
+               workspace: Optional[torch.Tensor] = None, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
+    """Attention of q [B, H, N, d] to the cache -> o [B, H, N, d], lse [B, H, N] fp32. q_offsets and kv_ranges [B, S, 2] as for
+    cross_attn_fwd: the positions [first, end) that a segment of a sample attends, of those that have a page; None: all."""
+    if q.dim() != 4 or q.shape[0] != cache.B or q.shape[3] != cache.d or not q.is_contiguous():
+        raise ValueError("need a contiguous q [B, H, N, d] of the cache's B and d")
+    B, H, N, d = q.shape
+    off, S = None, 1
+    if q_offsets is not None:
+        off = _i32(q_offsets)
+        S = off.shape[0] - 1
+    if kv_ranges is not None and (kv_ranges.dtype != torch.int32 or kv_ranges.shape != (B, S, 2) or not kv_ranges.is_contiguous()):
+        raise ValueError(f"kv_ranges must be a contiguous int32 tensor {(B, S, 2)}")
+    l = lib()
+    dt = _dtype_code(q)
+    device, stream = _on(q, cache.k, kv_ranges, workspace)
+    ws = workspace if workspace is not None else cache_attn_workspace(cache, H, N, q.dtype, S)
+    if out is None:
+        o, lse = torch.empty_like(q), torch.empty((B, H, N), dtype=torch.float32, device=q.device)
+    else:
+        o, lse = out
+        _need_like(o, q.shape, q)
+        _need_lse(lse, q)
+    _call(l.moc_cache_attn, device, C.byref(cache.struct), B, H, N, dt, q.data_ptr(), S, None if off is None else off.ctypes.data,
+          None if kv_ranges is None else kv_ranges.data_ptr(), d ** -0.5 if scale is None else scale, o.data_ptr(), lse.data_ptr(),
+          *_scratch(ws), stream)
+    return o, lse

@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "moc_block.h"
+#include "moc_cache.h"
 #include "moc_internal.h"
 
 namespace {
@@ -996,10 +997,8 @@ int check_overlap(const Span *out, int n_out, const Span *in, int n_in, int in_p
 
 int too_many_parts() { return fail(MOC_ERR_SHAPE, "too many tiles for the parts that sums over so many states or queries are cut into"); }
 
-// The parts of a call that both directions share.
-int cross_args(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t d, int32_t S, const int32_t *q_offsets,
-               const int32_t *kv_ranges, float scale, moc::CrossArgs &a) {
-    if (bad_scale(scale)) return fail(MOC_ERR_SHAPE, "softmax_scale must be finite and positive");
+// The cut of the queries into segments and the ranges that they attend.
+int check_segments(int32_t N, int32_t S, const int32_t *q_offsets, const int32_t *kv_ranges) {
     if (!q_offsets && S != 1) return fail(MOC_ERR_NULL, "q_offsets is NULL with S > 1");
     if (q_offsets) {
         if (q_offsets[0] != 0 || q_offsets[S] != N) return fail(MOC_ERR_OFFSETS, "q_offsets must run from 0 to N");
@@ -1007,6 +1006,15 @@ int cross_args(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t d
             if (q_offsets[s + 1] < q_offsets[s]) return fail(MOC_ERR_OFFSETS, "q_offsets must not decrease");
     }
     if (reinterpret_cast<uintptr_t>(kv_ranges) & 7u) return fail(MOC_ERR_ALIGN, "kv_ranges must be 8-byte aligned");
+    return MOC_OK;
+}
+
+// The parts of a call that both directions share.
+int cross_args(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, int32_t d, int32_t S, const int32_t *q_offsets,
+               const int32_t *kv_ranges, float scale, moc::CrossArgs &a) {
+    if (bad_scale(scale)) return fail(MOC_ERR_SHAPE, "softmax_scale must be finite and positive");
+    const int rc = check_segments(N, S, q_offsets, kv_ranges);
+    if (rc) return rc;
     a.ranges = reinterpret_cast<const moc::CrossRange *>(kv_ranges);
     if (!kv_ranges) S = 1;              // every query attends all states: segments do not matter
     a.rows = (long long)B * H * N;
@@ -1211,6 +1219,156 @@ int moc_cross_attn_bwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, i
     a.max_items = p.max_items;
     const hipError_t e = moc::launch_cross_bwd(a, p, d, dtype, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? MOC_OK : hip_fail(e, "cross attention backward kernels");
+}
+
+namespace {
+
+int check_cache(const moc_cache *c, int32_t B, int32_t N, int dtype, moc::CachePool &p) {
+    if (!c) return fail(MOC_ERR_NULL, "cache is NULL");
+    if (dtype != MOC_BF16 && dtype != MOC_F32) return fail(MOC_ERR_DTYPE, "dtype must be MOC_BF16 or MOC_F32");
+    if (B <= 0 || N <= 0 || c->Hk <= 0 || c->pages <= 0 || c->blocks <= 0) return fail(MOC_ERR_SHAPE, "B, N, Hk, pages and blocks must be positive");
+    if (c->d != 64 && c->d != 128) return fail(MOC_ERR_SHAPE, "d must be 64 or 128");
+    if ((long long)c->blocks * MOC_CACHE_PAGE >= (1 << 26) || N >= (1 << 26)) return fail(MOC_ERR_SHAPE, "64 * blocks and N must be < 2^26");
+    if ((long long)B * c->Hk > 65535) return fail(MOC_ERR_SHAPE, "B * Hk must be <= 65535");
+    if (!c->k || !c->v || !c->k_exp || !c->v_exp || !c->table) return fail(MOC_ERR_NULL, "a pointer of the cache is NULL");
+    if (misaligned(c->k) || misaligned(c->v)) return fail(MOC_ERR_ALIGN, "the pages must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(c->table) & 3u) return fail(MOC_ERR_ALIGN, "the table must be 4-byte aligned");
+    p = moc::CachePool{static_cast<uint8_t *>(c->k), static_cast<uint8_t *>(c->v), c->k_exp, c->v_exp, c->table, c->pages, c->blocks, c->Hk};
+    return MOC_OK;
+}
+
+struct CacheSpans { Span k, v, k_exp, v_exp, table; };
+CacheSpans cache_spans(const moc_cache *c, int32_t B) {
+    const size_t heads = (size_t)c->pages * c->Hk, codes = heads * MOC_CACHE_PAGE * c->d;
+    return {{c->k, codes}, {c->v, codes}, {c->k_exp, heads}, {c->v_exp, heads}, {c->table, (size_t)B * c->blocks * 4}};
+}
+
+// What lies between the first and the last element of a strided tensor.
+Span rows_span(const moc_rows *r, int32_t B, int32_t N, int32_t H, int32_t d, int dtype, long long sb, long long sh, long long sn) {
+    const long long s[3] = {sb * (B - 1), sh * (H - 1), sn * (N - 1)};
+    long long lo = 0, hi = d;
+    for (long long x : s) (x < 0 ? lo : hi) += x;
+    const int e = dtype == MOC_F32 ? 4 : 2;
+    return {static_cast<const char *>(r->data) + lo * e, (size_t)(hi - lo) * e};
+}
+
+// The parts of a call that the write and the read share.
+int cache_copy_args(const moc_cache *c, int32_t B, int32_t N, int dtype, const int32_t *starts, const int32_t *counts, moc::CacheCopyArgs &a) {
+    const int rc = check_cache(c, B, N, dtype, a.pool);
+    if (rc) return rc;
+    if ((reinterpret_cast<uintptr_t>(starts) | reinterpret_cast<uintptr_t>(counts)) & 3u)
+        return fail(MOC_ERR_ALIGN, "starts and counts must be 4-byte aligned");
+    a.starts = starts;
+    a.counts = counts;
+    a.B = B;
+    a.N = N;
+    a.touched = (N + MOC_CACHE_PAGE - 2) / MOC_CACHE_PAGE + 1;
+    // (a launch has fewer than 2^32 threads, 256 a workgroup)
+    if ((long long)B * a.touched * c->Hk * 2 >= 1 << 24) return fail(MOC_ERR_SHAPE, "too many pages: B * Hk * (N / 64 + 2) must be < 2^23");
+    return MOC_OK;
+}
+
+int check_cache_attn(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t S) {
+    if (H <= 0 || H % Hk != 0) return fail(MOC_ERR_SHAPE, "Hk must divide H");
+    if (S < 1 || S > MOC_MAX_CROSS_SEGMENTS) return fail(MOC_ERR_SHAPE, "need 1 <= S <= MOC_MAX_CROSS_SEGMENTS");
+    if ((long long)B * H > 65535) return fail(MOC_ERR_SHAPE, "B * H must be <= 65535");
+    if ((long long)N * (H / Hk) >= (1 << 26) || (long long)B * H * N >= (1LL << 31)) return fail(MOC_ERR_SHAPE, "H / Hk * N must be < 2^26 and B * H * N < 2^31");
+    return MOC_OK;
+}
+
+}  // namespace
+
+int moc_cache_write(const moc_cache *cache, int32_t B, int32_t N, int dtype, const moc_rows *k, const moc_rows *v, const int32_t *starts,
+                    const int32_t *counts, void *stream) {
+    moc::CacheCopyArgs a{};
+    int rc = cache_copy_args(cache, B, N, dtype, starts, counts, a);
+    if (rc) return rc;
+    const moc_rows *in[2] = {k, v};
+    const CacheSpans c = cache_spans(cache, B);
+    const Span out[] = {c.k, c.v, c.k_exp, c.v_exp};
+    Span from[5] = {{}, {}, c.table, {starts, (size_t)B * 4}, {counts, (size_t)B * 4}};
+    for (int i = 0; i < 2; ++i) {
+        if (!in[i]) return fail(MOC_ERR_NULL, "k or v is NULL");
+        rc = check_rows(in[i], B, N, cache->Hk, dtype, &a.x_b[i], &a.x_h[i], &a.x_n[i]);
+        if (rc) return rc;
+        a.x[i] = in[i]->data;
+        from[i] = rows_span(in[i], B, N, cache->Hk, cache->d, dtype, a.x_b[i], a.x_h[i], a.x_n[i]);
+    }
+    rc = check_overlap(out, 4, from, 5, 0);
+    if (rc) return rc;
+    const hipError_t e = moc::launch_cache_write(a, cache->d, dtype, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? MOC_OK : hip_fail(e, "cache write kernel");
+}
+
+int moc_cache_read(const moc_cache *cache, int32_t B, int32_t N, int dtype, const int32_t *starts, const int32_t *counts, void *k_out,
+                   void *v_out, void *stream) {
+    moc::CacheCopyArgs a{};
+    int rc = cache_copy_args(cache, B, N, dtype, starts, counts, a);
+    if (rc) return rc;
+    if (!k_out && !v_out) return fail(MOC_ERR_NULL, "k_out and v_out are both NULL");
+    if (misaligned(k_out) || misaligned(v_out)) return fail(MOC_ERR_ALIGN, "device pointers must be 16-byte aligned");
+    const size_t bytes = (size_t)B * cache->Hk * N * cache->d * (dtype == MOC_F32 ? 4 : 2);
+    const CacheSpans c = cache_spans(cache, B);
+    const Span out[] = {{k_out, bytes}, {v_out, bytes}};
+    const Span in[] = {c.k, c.v, c.k_exp, c.v_exp, c.table, {starts, (size_t)B * 4}, {counts, (size_t)B * 4}};
+    rc = check_overlap(out, 2, in, 7, 0);
+    if (rc) return rc;
+    a.out[0] = k_out;
+    a.out[1] = v_out;
+    const hipError_t e = moc::launch_cache_read(a, cache->d, dtype, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? MOC_OK : hip_fail(e, "cache read kernel");
+}
+
+int moc_cache_attn_workspace_bytes(const moc_cache *cache, int32_t B, int32_t H, int32_t N, int32_t S, int dtype, size_t *bytes) {
+    if (!bytes) return fail(MOC_ERR_NULL, "bytes is NULL");
+    moc::CachePool pool;
+    int rc = check_cache(cache, B, N, dtype, pool);
+    if (!rc) rc = check_cache_attn(B, H, cache->Hk, N, S);
+    if (rc) return rc;
+    const int M = cache->blocks * MOC_CACHE_PAGE;
+    // (calls without kv_ranges are planned as one segment)
+    const moc::CachePlan p = moc::cache_attn_plan(B, H, cache->Hk, N, M, cache->d, S, dtype), one = moc::cache_attn_plan(B, H, cache->Hk, N, M, cache->d, 1, dtype);
+    if (!p.fits || !one.fits) return too_many_parts();
+    *bytes = std::max(p.total, one.total);
+    return MOC_OK;
+}
+
+int moc_cache_attn(const moc_cache *cache, int32_t B, int32_t H, int32_t N, int dtype, const void *q, int32_t S, const int32_t *q_offsets,
+                   const int32_t *kv_ranges, float softmax_scale, void *o, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    moc::CacheAttnArgs a{};
+    int rc = check_cache(cache, B, N, dtype, a.pool);
+    if (!rc) rc = check_cache_attn(B, H, cache->Hk, N, S);
+    if (rc) return rc;
+    if (!q || !o || !lse) return fail(MOC_ERR_NULL, "a tensor pointer is NULL");
+    if (misaligned(q) || misaligned(o) || misaligned(lse)) return fail(MOC_ERR_ALIGN, "device pointers must be 16-byte aligned");
+    if (bad_scale(softmax_scale)) return fail(MOC_ERR_SHAPE, "softmax_scale must be finite and positive");
+    rc = check_segments(N, S, q_offsets, kv_ranges);
+    if (rc) return rc;
+    if (!kv_ranges) S = 1;              // every query attends everything: segments do not matter
+    const int M = cache->blocks * MOC_CACHE_PAGE, d = cache->d;
+    const moc::CachePlan p = moc::cache_attn_plan(B, H, cache->Hk, N, M, d, S, dtype);
+    if (!p.fits) return too_many_parts();
+    if (p.total > 0 && (!workspace || workspace_bytes < p.total)) return fail(MOC_ERR_WORKSPACE, "cache attention workspace too small");
+    if (misaligned(workspace)) return fail(MOC_ERR_ALIGN, "workspace must be 16-byte aligned");
+    const size_t rows = (size_t)B * H * N, q_bytes = rows * d * (dtype == MOC_F32 ? 4 : 2);
+    const CacheSpans c = cache_spans(cache, B);
+    const Span out[] = {{o, q_bytes}, {lse, rows * 4}, {workspace, p.total}};
+    const Span in[] = {{q, q_bytes}, c.k, c.v, c.k_exp, c.v_exp, c.table, {kv_ranges, (size_t)B * S * 8}};
+    rc = check_overlap(out, 3, in, 7, 1);
+    if (rc) return rc;
+    char *ws = static_cast<char *>(workspace);
+    a.q = q; a.o = o; a.lse = lse;
+    a.part = reinterpret_cast<float *>(ws + p.part);
+    a.part_lse = reinterpret_cast<float *>(ws + p.part_lse);
+    a.ranges = reinterpret_cast<const moc::CrossRange *>(kv_ranges);
+    a.rows = (long long)rows;
+    a.N = N; a.M = M; a.n_seg = S; a.H = H; a.G = H / cache->Hk; a.BHk = B * cache->Hk;
+    a.split = p.split;
+    a.scale = softmax_scale;
+    a.scale_log2 = softmax_scale * 1.4426950408889634f;
+    for (int s = 0; s <= S; ++s) a.q_off[s] = S == 1 ? s * N : q_offsets[s];
+    const hipError_t e = moc::launch_cache_attn(a, d, dtype, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? MOC_OK : hip_fail(e, "cache attention kernels");
 }
 
 }  // extern "C"

@@ -1,0 +1,51 @@
+// Arguments and launchers of the key / value cache held in 8 bits (moc_cache.hip, moc_cache_attn.hip).
+#pragma once
+#include "moc_block.h"
+
+namespace moc {
+
+constexpr int kPage = MOC_CACHE_PAGE;          // tokens of a page
+// Exponents that values and codes can be multiplied by without leaving the normal numbers of bf16 and float: a code is 2^-9 at least.
+constexpr int kLeastExp = -110, kMostExp = 120;
+
+struct CachePool {
+    uint8_t *k, *v;                            // [pages][Hk][kPage][d] codes
+    int8_t *k_exp, *v_exp;                     // [pages][Hk]
+    const int32_t *table;                      // [B][blocks]
+    int pages, blocks, Hk;
+};
+// What goes into the cache or comes out of it.
+struct CacheCopyArgs {
+    CachePool pool;
+    const void *x[2];                          // write: keys, values
+    long long x_b[2], x_h[2], x_n[2];          // strides, in elements
+    void *out[2];                              // read: contiguous [B, Hk, N, d], nullptr: left out
+    const int32_t *starts, *counts;            // [B] or nullptr: 0, N
+    int B, N, touched;                         // blocks that N tokens of a sample can lie in
+};
+hipError_t launch_cache_write(const CacheCopyArgs &a, int d, int dtype, hipStream_t st);
+hipError_t launch_cache_read(const CacheCopyArgs &a, int d, int dtype, hipStream_t st);
+
+struct CacheAttnArgs {
+    CachePool pool;
+    const void *q;
+    void *o;
+    float *lse;
+    float *part, *part_lse;                    // split calls: [split][B * H * N][d], [split][B * H * N]
+    const CrossRange *ranges;                  // [B][n_seg] or nullptr
+    long long rows;                            // B * H * N
+    int N, M, n_seg, H, G, BHk;                // G query heads on a key head
+    int tiles, split;                          // query tiles of a key head, parts of a range
+    float scale, scale_log2;
+    int32_t q_off[MOC_MAX_CROSS_SEGMENTS + 1];
+    int32_t tile_at[MOC_MAX_CROSS_SEGMENTS + 1];      // first query tile of a segment
+};
+struct CachePlan {
+    int split;
+    bool fits;
+    size_t part, part_lse, total;              // workspace, byte offsets
+};
+CachePlan cache_attn_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype);
+hipError_t launch_cache_attn(CacheAttnArgs a, int d, int dtype, hipStream_t st);
+
+}  // namespace moc

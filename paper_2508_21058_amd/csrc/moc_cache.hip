@@ -1,0 +1,169 @@
+// Writing a key / value cache in 8 bits and reading it back.
+//
+// A page holds 64 tokens of every key head: codes in e4m3 (three bits behind the leading one, 2^-9 to 448) and one exponent a head, value = code * 2^e.
+// A power of two as the scale costs a float format nothing (one of its 17 binades), and the value of a code is then exact in bf16: it comes
+// back without a rounding, goes to the matrix cores as it is, and codes follow a growing exponent without loss until they reach the
+// subnormals. One workgroup takes a page of one head; both passes are bound by HBM.
+#include "moc_cache.h"
+#include "moc_device.h"
+
+namespace moc {
+
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+// An exponent in memory; others than those that the write leaves are taken for the nearest of them.
+__device__ __forceinline__ int stored_exp(const int8_t *p) { return min(max((int)*p, kLeastExp), kMostExp); }
+
+// The least e with amax <= 448 * 2^e, from the bits of amax (finite, >= 0): 448 is 1.75 * 2^8.
+__device__ __forceinline__ int needed_exp(uint32_t amax) {
+    const int e = (int)(amax >> 23) - 127 - 8 + ((amax & 0x7fffffu) > 0x600000u);
+    return min(max((amax >> 23) ? e : kLeastExp, kLeastExp), kMostExp);
+}
+
+// Four floats to four codes, to the nearest, ties to even; what is not finite becomes NaN (the format has no infinity).
+__device__ __forceinline__ uint32_t to_codes(const float *x, float inv) {
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = __builtin_isfinite(x[i]) ? x[i] * inv : __builtin_nanf("");
+    int u = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], u, true);
+}
+__device__ __forceinline__ void from_codes(uint32_t u, float scale, float *x) {
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)u, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)u, true);
+    x[0] = a[0] * scale; x[1] = a[1] * scale; x[2] = b[0] * scale; x[3] = b[1] * scale;
+}
+
+// The page of a head that a workgroup has, and the positions of its rows.
+struct PageItem {
+    int b, h, kv, page;                // page -1: not there
+    long long first;                   // token of the call (n) that the page's first row stands for
+    int count;                         // tokens of the sample
+};
+__device__ __forceinline__ PageItem page_item(const CacheCopyArgs &a) {
+    PageItem it;
+    int i = blockIdx.x;
+    it.kv = i % 2; i /= 2;
+    it.h = i % a.pool.Hk; i /= a.pool.Hk;
+    const int j = i % a.touched;
+    it.b = i / a.touched;
+    const int start = a.starts ? a.starts[it.b] : 0;
+    const long long block = (long long)(start >> 6) + j;
+    it.count = a.counts ? min(max(a.counts[it.b], 0), a.N) : a.N;
+    it.first = block * kPage - start;
+    it.page = block >= 0 && block < a.pool.blocks ? a.pool.table[(size_t)it.b * a.pool.blocks + block] : -1;
+    if (it.page >= a.pool.pages) it.page = -1;
+    return it;
+}
+static_assert(kPage == 64, "page_item() shifts by six");
+
+template <typename T> __device__ __forceinline__ void load16(const T *p, float *f) {
+    Io<T>::load8f(p, f);
+    Io<T>::load8f(p + 8, f + 8);
+}
+
+template <int D, typename T> __global__ __launch_bounds__(256) void cache_write_kernel(CacheCopyArgs a) {
+    constexpr int LPR = D / 16, PASS = 256 / LPR, NP = kPage / PASS;          // lanes a row of 16 features each, rows a pass
+    __shared__ uint32_t most[4];
+    __shared__ int prior;
+    const PageItem it = page_item(a);
+    if (it.page < 0 || it.first >= it.count || it.first + kPage <= 0) return;
+    const int tid = threadIdx.x, row = tid / LPR, c = tid % LPR * 16;
+    const size_t slot = (size_t)it.page * a.pool.Hk + it.h;
+    uint8_t *codes = (it.kv ? a.pool.v : a.pool.k) + slot * (kPage * D) + c;
+    int8_t *exps = (it.kv ? a.pool.v_exp : a.pool.k_exp) + slot;
+    const int kept = it.first < 0 ? (int)-it.first : 0;                       // rows in front of the new tokens
+    if (tid == 0) prior = stored_exp(exps);
+    const T *x = static_cast<const T *>(a.x[it.kv]) + it.b * a.x_b[it.kv] + it.h * a.x_h[it.kv] + c;
+    float f[NP][16];
+    uint32_t amax = 0;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        const long long n = it.first + p * PASS + row;
+        if (n < 0 || n >= it.count) continue;
+        load16<T>(x + n * a.x_n[it.kv], f[p]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t u = __float_as_uint(f[p][i]) & 0x7fffffffu;
+            amax = max(amax, u < 0x7f800000u ? u : 0u);
+        }
+    }
+#pragma unroll
+    for (int i = 32; i > 0; i >>= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, i, 64));
+    if ((tid & 63) == 0) most[tid >> 6] = amax;
+    __syncthreads();
+    const int old = prior;
+    int e = needed_exp(max(max(most[0], most[1]), max(most[2], most[3])));
+    if (kept > 0) e = max(e, old);
+    if (tid == 0) *exps = (int8_t)e;
+    const float inv = pow2(-e);
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        const int r = p * PASS + row;
+        const long long n = it.first + r;
+        u32x4 u;
+        if (r < kept) {
+            if (e == old) continue;
+            const float shrink = pow2(max(old - e, -126));
+            u = *reinterpret_cast<const u32x4 *>(codes + r * D);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float y[4];
+                from_codes(u[i], 1.f, y);
+                u[i] = to_codes(y, shrink);
+            }
+        } else {
+            if (n >= it.count) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[i] = to_codes(f[p] + 4 * i, inv);
+        }
+        *reinterpret_cast<u32x4 *>(codes + r * D) = u;
+    }
+}
+
+template <int D, typename T> __global__ __launch_bounds__(256) void cache_read_kernel(CacheCopyArgs a) {
+    constexpr int LPR = D / 16, PASS = 256 / LPR, NP = kPage / PASS;
+    const PageItem it = page_item(a);
+    T *out = static_cast<T *>(a.out[it.kv]);
+    if (!out || it.first >= a.N) return;
+    const int row = threadIdx.x / LPR, c = threadIdx.x % LPR * 16;
+    const size_t slot = (size_t)max(it.page, 0) * a.pool.Hk + it.h;
+    const uint8_t *codes = (it.kv ? a.pool.v : a.pool.k) + slot * (kPage * D) + c;
+    const float scale = pow2(stored_exp((it.kv ? a.pool.v_exp : a.pool.k_exp) + slot));
+    out += ((size_t)it.b * a.pool.Hk + it.h) * a.N * D + c;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        const int r = p * PASS + row;
+        const long long n = it.first + r;
+        if (n < 0 || n >= a.N) continue;
+        float f[16];
+        u32x4 u = {0, 0, 0, 0};
+        if (it.page >= 0 && n < it.count) u = *reinterpret_cast<const u32x4 *>(codes + r * D);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) from_codes(u[i], scale, f + 4 * i);
+        Io<T>::store8(out + n * D, f);
+        Io<T>::store8(out + n * D + 8, f + 8);
+    }
+}
+
+static unsigned copy_grid(const CacheCopyArgs &a) { return (unsigned)((long long)a.B * a.touched * a.pool.Hk * 2); }
+
+hipError_t launch_cache_write(const CacheCopyArgs &a, int d, int dtype, hipStream_t st) {
+    MOC_PROF("cache_write", st);
+    const unsigned grid = copy_grid(a);
+    if (d == 128 && dtype == MOC_BF16) cache_write_kernel<128, bf16_t><<<grid, 256, 0, st>>>(a);
+    else if (d == 128) cache_write_kernel<128, float><<<grid, 256, 0, st>>>(a);
+    else if (dtype == MOC_BF16) cache_write_kernel<64, bf16_t><<<grid, 256, 0, st>>>(a);
+    else cache_write_kernel<64, float><<<grid, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_read(const CacheCopyArgs &a, int d, int dtype, hipStream_t st) {
+    MOC_PROF("cache_read", st);
+    const unsigned grid = copy_grid(a);
+    if (d == 128 && dtype == MOC_BF16) cache_read_kernel<128, bf16_t><<<grid, 256, 0, st>>>(a);
+    else if (d == 128) cache_read_kernel<128, float><<<grid, 256, 0, st>>>(a);
+    else if (dtype == MOC_BF16) cache_read_kernel<64, bf16_t><<<grid, 256, 0, st>>>(a);
+    else cache_read_kernel<64, float><<<grid, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace moc

@@ -1,0 +1,311 @@
+// Attention over a key / value cache held in 8 bits: o = softmax(q K^T scale) V over the range of cached tokens that a query's segment attends.
+//
+// One pass with a running maximum and sum, as in cross attention's forward: S^T = K Q^T and O^T = V^T P^T, so that a lane owns a query and the scores feed
+// the second product from the registers they are in. The queries of a segment, of all query heads on a key head, are one list of rows: a workgroup
+// owns 128 of them, four waves of 32, and streams the range's pages through LDS in double-buffered tiles of 32 tokens. Codes come through
+// registers and are written to LDS as bf16, which has every value code * 2^e exactly, by an instruction that takes the exponent along: once for the
+// four waves. Calls of few rows split the range over workgroups, whose results a second launch joins.
+//
+// fp32 queries are three bf16 terms that add up to them exactly, and so are the probabilities: since the cached values have four bits, three products on bf16
+// matrix cores are as exact as one on float cores, at a fifth of the time.
+#include "moc_cache.h"
+#include "moc_attn_common.h"
+#include "moc_cross.h"
+
+namespace moc {
+
+// 16 codes as bf16 times 2^e (scale), eight to a word of 16 bytes.
+__device__ __forceinline__ void widen16(u32x4 u, float scale, u32x4 &lo, u32x4 &hi) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[i], scale, false));
+        w[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[i], scale, true));
+    }
+    lo = u32x4{w[0], w[1], w[2], w[3]};
+    hi = u32x4{w[4], w[5], w[6], w[7]};
+}
+__device__ __forceinline__ float exp_scale(const int8_t *p) {
+    return __uint_as_float((uint32_t)(min(max((int)*p, kLeastExp), kMostExp) + 127) << 23);
+}
+
+// Operands of T = bf16: one term; of T = float: three bf16 terms, the largest first, whose sum is the value.
+template <typename T> constexpr int kTerms = sizeof(T) == 2 ? 1 : 3;
+__device__ __forceinline__ void three_terms(const float *x, bf16x8 *out) {
+    uint32_t w[3][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a = x[2 * i], b = x[2 * i + 1];
+#pragma unroll
+        for (int t = 0; t < 3; ++t) {
+            w[t][i] = pack_bf16(a, b);
+            a -= bf16_lo(w[t][i]);
+            b -= bf16_hi(w[t][i]);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < 3; ++t) out[t] = __builtin_bit_cast(bf16x8, u32x4{w[t][0], w[t][1], w[t][2], w[t][3]});
+}
+__device__ __forceinline__ void query_terms(const bf16_t *p, bf16x8 *out) { out[0] = Io<bf16_t>::load8(p); }
+__device__ __forceinline__ void query_terms(const float *p, bf16x8 *out) {
+    float x[8];
+    Io<float>::load8f(p, x);
+    three_terms(x, out);
+}
+// Probabilities of 8 tokens (registers 8 s ..) as the second product's operand. In bf16 they are rounded, half a step 2^-8: that product runs on
+// bf16 matrix cores, sixteen times the rate of the float ones.
+template <typename T> __device__ __forceinline__ void score_terms(const f32x16 &acc, int s, bf16x8 *out) {
+    if constexpr (sizeof(T) == 2) {
+        out[0] = acc_to_frag(acc, s);
+    } else {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = acc[8 * s + i];
+        three_terms(x, out);
+    }
+}
+
+// Rows [first, first + count) of the list of a segment's queries: query i of head g is row g * n + i.
+struct CacheItem {
+    int b, hk, z;
+    int first, count, n;             // n: queries of the segment
+    int begin, end;                  // tokens that are attended
+    long long row0;                  // query 0 of the segment and of the first head in [B * H * N]
+};
+__device__ __forceinline__ bool cache_item(const CacheAttnArgs &a, int rows, CacheItem &it) {
+    int logical;
+    if (!xcd_remap((long long)a.tiles * a.BHk * a.split, logical)) return false;
+    it.z = logical % a.split;
+    int i = logical / a.split;
+    const int bhk = i / a.tiles, t = i - bhk * a.tiles;
+    it.b = bhk / a.pool.Hk;
+    it.hk = bhk - it.b * a.pool.Hk;
+    int s = 0, hi = a.n_seg;                                      // the last segment with tile_at <= t
+    while (hi - s > 1) {
+        const int mid = (s + hi) >> 1;
+        if (a.tile_at[mid] <= t) s = mid; else hi = mid;
+    }
+    it.n = a.q_off[s + 1] - a.q_off[s];
+    it.first = (t - a.tile_at[s]) * rows;
+    it.count = min(rows, it.n * a.G - it.first);
+    it.row0 = ((long long)it.b * a.H + it.hk * a.G) * a.N + a.q_off[s];
+    CrossRange r = {0, a.M};
+    if (a.ranges) {
+        r = a.ranges[(size_t)it.b * a.n_seg + s];
+        r.first = max(r.first, 0);
+        r.end = min(r.end, a.M);
+        if (r.end <= r.first) r.first = r.end = 0;               // (a tile begins in front of the range)
+    }
+    it.begin = __builtin_amdgcn_readfirstlane(r.first);
+    it.end = __builtin_amdgcn_readfirstlane(r.end);
+    return it.count > 0;
+}
+// Part z of a range, whole tiles of 32 tokens that begin at multiples of 32.
+__device__ __forceinline__ void cache_slice(CacheItem &it, int n) {
+    if (n == 1 || it.end <= it.begin) return;
+    const int t0 = it.begin >> 5, tiles = ((it.end + 31) >> 5) - t0, begin = it.begin, end = it.end;
+    it.begin = max(begin, (t0 + (int)((long long)tiles * it.z / n)) << 5);
+    it.end = min(end, (t0 + (int)((long long)tiles * (it.z + 1) / n)) << 5);
+}
+
+// Walks the tiles of 32 tokens of a range whose pages are there; the next page's number is asked for a tile ahead.
+struct TileWalk {
+    const int32_t *table;
+    int pages, end, next, ahead;       // next: where to look on, ahead: its page
+    __device__ __forceinline__ TileWalk(const CacheAttnArgs &a, const CacheItem &it, int from)
+        : table(a.pool.table + (size_t)it.b * a.pool.blocks), pages(a.pool.pages), end(it.end), next(from & ~31), ahead(-1) {
+        if (next < end) ahead = look(next);
+    }
+    __device__ __forceinline__ int look(int pos) const { return (int)uniform_load_u32(reinterpret_cast<const uint32_t *>(table), pos >> 6); }
+    // -> the next tile's first token and its page; false: none is left
+    __device__ __forceinline__ bool step(int &pos, int &page, int stride) {
+        page = ahead;
+        while (next < end && (unsigned)page >= (unsigned)pages) {
+            next = (next | 63) + 1;                             // (a multiple of 32 behind the missing page)
+            if (next < end) page = look(next);
+        }
+        if (next >= end) return false;
+        pos = next;
+        next += stride;
+        if (next < end) ahead = look(next);
+        return true;
+    }
+};
+
+template <int D, typename T>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel(CacheAttnArgs a) {
+    constexpr int BN = 32, DB = D / 32, KS = D / 16, RB = D * 2, TB = BN * RB, NT = kTerms<T>;
+    constexpr int PATCH = sizeof(T) == 2 ? 4 * (32 * (D + 4) + 64) * 2 : 0;      // what store_rows_bf16 takes
+    __shared__ __attribute__((aligned(1024))) char smem[4 * TB > PATCH ? 4 * TB : PATCH];      // K, V, twice
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
+    CacheItem it;
+    if (!cache_item(a, kCrossRows, it)) return;
+    cache_slice(it, a.split);
+    const int r = wave * 32 + l32, rc = it.first + min(r, it.count - 1), g = rc / it.n;
+    const bool row_valid = r < it.count;
+    const int local = g * a.N + (rc - g * it.n);               // row behind row0
+    const size_t row = (size_t)it.row0 + local;
+    float *pout = a.split > 1 ? a.part + ((size_t)it.z * a.rows + row) * D : nullptr;
+    float *lout = a.split > 1 ? a.part_lse + (size_t)it.z * a.rows + row : a.lse + row;
+    f32x16 oacc[DB];
+#pragma unroll
+    for (int b = 0; b < DB; ++b) oacc[b] = zero16();
+    float m_run = -INFINITY, l_run = 0.f;
+    TileWalk walk(a, it, it.begin);
+    int pos, page;
+    if (walk.step(pos, page, BN)) {
+        // A thread's share of a tile: 16 codes of a row of K and of V (64 features: of one of the two).
+        constexpr int LPR = D / 16, NL = D / 64;
+        const int lr = (tid % (BN * LPR)) / LPR, lc = tid % LPR, which = NL == 1 ? tid / (BN * LPR) : 0;
+        u32x4 raw[NL];
+        float scale[NL];
+        auto load = [&](int pos, int page) {
+            const size_t slot = (size_t)page * a.pool.Hk + it.hk;
+            const int at = min(max(pos + lr, it.begin), it.end - 1) & (kPage - 1);      // rows outside the range repeat one inside
+#pragma unroll
+            for (int j = 0; j < NL; ++j) {
+                const bool v = (NL == 1 ? which : j) != 0;
+                raw[j] = *reinterpret_cast<const u32x4 *>((v ? a.pool.v : a.pool.k) + slot * (kPage * D) + at * D + lc * 16);
+                scale[j] = exp_scale((v ? a.pool.v_exp : a.pool.k_exp) + slot);
+            }
+        };
+        load(pos, page);
+        Ops<D, bf16_t> ops;
+        ops.init(lane);
+        bf16x8 qf[KS][NT];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) query_terms(static_cast<const T *>(a.q) + row * D + 16 * s + 8 * half, qf[s]);
+        const float c = a.scale_log2;
+        bool first = true, more = true;
+        // One tile; the buffers take turns in a loop unrolled by two, so that LDS addresses are constants beside the lane's offsets.
+        auto tile = [&](auto which_buf) {
+            constexpr int BUF = decltype(which_buf)::value;
+            char *kt = smem + BUF * 2 * TB, *vt = kt + TB;
+#pragma unroll
+            for (int j = 0; j < NL; ++j) {
+                u32x4 lo, hi;
+                widen16(raw[j], scale[j], lo, hi);
+                char *t = (NL == 1 ? which : j) ? vt : kt;
+                *reinterpret_cast<u32x4 *>(t + SwTile<D>::off(lr, 2 * lc) * 2) = lo;
+                *reinterpret_cast<u32x4 *>(t + SwTile<D>::off(lr, 2 * lc + 1) * 2) = hi;
+            }
+            const int lo = it.begin - pos, hi = it.end - pos;
+            more = walk.step(pos, page, BN);
+            if (more) load(pos, page);
+            __syncthreads();
+            if (wave * 32 >= it.count) return;
+            ops.pin();
+            f32x16 s = zero16();
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                const bf16x8 kf = ops.frag(kt, 0, i);
+#pragma unroll
+                for (int t = NT - 1; t >= 0; --t) s = mfma32(kf, qf[i][t], s);
+            }
+            if (lo > 0 || hi < BN) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int n = (i >> 2) * 8 + half * 4 + (i & 3);
+                    if (n < lo || n >= hi) s[i] = -INFINITY;
+                }
+            }
+            float mx = s[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+            const float m_new = fmaxf(m_run, xhalf_max(mx));
+            if (first) {
+                m_run = m_new;
+                first = false;
+            } else if (__any((m_new - m_run) * c > 8.f)) {      // moved, and the sums rescaled, only when it has grown by 2^8
+                const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * c);
+                l_run *= alpha;
+#pragma unroll
+                for (int b = 0; b < DB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) oacc[b][i] *= alpha;
+                m_run = m_new;
+            }
+            const float mc = m_run * c;
+            float l_tile = 0.f;                // (on its own first: a long range adds few large numbers)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -mc));
+                l_tile += s[i];
+            }
+            l_run += l_tile;
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                bf16x8 pf[NT];
+                score_terms<T>(s, ks, pf);
+#pragma unroll
+                for (int b = 0; b < DB; ++b) {
+                    const bf16x8 vf = ops.tfrag(vt, 0, b, ks);
+#pragma unroll
+                    for (int t = NT - 1; t >= 0; --t) oacc[b] = mfma32(vf, pf[t], oacc[b]);
+                }
+            }
+        };
+        while (true) {
+            tile(IC<0>{});
+            if (!more) break;
+            tile(IC<1>{});
+            if (!more) break;
+        }
+    }
+    const float l = xhalf_sum(l_run);
+    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;      // nothing attended: o = 0, lse = -inf
+    const float lse = l > 0.f || l != l ? m_run * a.scale + logf(l) : -INFINITY;
+    if (row_valid && half == 0) *lout = lse;
+    if (a.split > 1) {
+        if (row_valid && lse != -INFINITY) store_rows_f32<D>(oacc, inv, pout, half);
+    } else if constexpr (sizeof(T) == 4) {
+        if (row_valid) store_rows_f32<D>(oacc, inv, static_cast<float *>(a.o) + row * D, half);
+    } else {
+        __syncthreads();
+        store_rows_bf16<D>(smem, wave, lane, oacc, inv, row_valid ? local : -1, static_cast<bf16_t *>(a.o) + (size_t)it.row0 * D);
+    }
+}
+
+template <int D, typename T> static void attn_dispatch(CacheAttnArgs &a, hipStream_t st) {
+    a.tiles = 0;
+    for (int s = 0; s < a.n_seg; ++s) {
+        a.tile_at[s] = a.tiles;
+        a.tiles += ((a.q_off[s + 1] - a.q_off[s]) * a.G + kCrossRows - 1) / kCrossRows;
+    }
+    a.tile_at[a.n_seg] = a.tiles;
+    {
+        MOC_PROF("cache_attn", st);
+        cache_attn_kernel<D, T><<<xcd_grid((long long)a.tiles * a.BHk * a.split), 256, 0, st>>>(a);
+    }
+    if (a.split > 1) launch_join(a.part, a.part_lse, a.split, a.rows, D, sizeof(T) == 2 ? MOC_BF16 : MOC_F32, a.o, a.lse, st);
+}
+
+hipError_t launch_cache_attn(CacheAttnArgs a, int d, int dtype, hipStream_t st) {
+    if (d == 128 && dtype == MOC_BF16) attn_dispatch<128, bf16_t>(a, st);
+    else if (d == 128) attn_dispatch<128, float>(a, st);
+    else if (dtype == MOC_BF16) attn_dispatch<64, bf16_t>(a, st);
+    else attn_dispatch<64, float>(a, st);
+    return hipGetLastError();
+}
+
+// Parts of the ranges: as many as give every compute unit two workgroups, of 256 tokens at least; more where a sum would otherwise be longer than sums may be.
+CachePlan cache_attn_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype) {
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    CachePlan p;
+    const long long rows = (long long)B * H * N, chain = dtype == MOC_BF16 ? kChainTerms : kChainTerms / 4, least = (M + chain - 1) / chain;
+    const long long per_head = ((long long)N * (H / Hk) + kCrossRows - 1) / kCrossRows, tiles = (long long)B * Hk * (per_head + S - 1);
+    long long split = std::min<long long>((M + 255) / 256, (2 * kComputeUnits + (long long)B * Hk * per_head - 1) / ((long long)B * Hk * per_head));
+    split = std::max(split, least);
+    p.split = (int)split;
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t x = at; at += up(bytes); return x; };
+    p.part = take(split > 1 ? (size_t)split * rows * d * 4 : 0);
+    p.part_lse = take(split > 1 ? (size_t)split * rows * 4 : 0);
+    p.total = at;
+    // (a launch has fewer than 2^32 threads)
+    const long long most = (1 << 24) - 1024;
+    p.fits = tiles * split < most && (split == 1 || rows * (d / 4) / 256 < most);
+    return p;
+}
+
+}  // namespace moc
