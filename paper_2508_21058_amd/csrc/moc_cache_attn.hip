@@ -72,9 +72,7 @@ struct CacheItem {
     int begin, end;                  // tokens that are attended
     long long row0;                  // query 0 of the segment and of the first head in [B * H * N]
 };
-__device__ __forceinline__ bool cache_item(const CacheAttnArgs &a, int rows, CacheItem &it) {
-    int logical;
-    if (!xcd_remap((long long)a.tiles * a.BHk * a.split, logical)) return false;
+__device__ __forceinline__ bool cache_item(const CacheAttnArgs &a, int logical, int rows, CacheItem &it) {
     it.z = logical % a.split;
     int i = logical / a.split;
     const int bhk = i / a.tiles, t = i - bhk * a.tiles;
@@ -108,8 +106,8 @@ __device__ __forceinline__ void cache_slice(CacheItem &it, int n) {
     it.end = min(end, (t0 + (int)((long long)tiles * (it.z + 1) / n)) << 5);
 }
 
-// Walks the tiles of 32 tokens of a range whose pages are there; the next page's number is asked for a tile ahead.
-struct TileWalk {
+// Walks the tiles of 32 tokens of a range whose pages are there, every STRIDE tokens; the next page's number is asked for a tile ahead.
+template <int STRIDE> struct TileWalk {
     const int32_t *table;
     int pages, end, next, ahead;       // next: where to look on, ahead: its page
     __device__ __forceinline__ TileWalk(const CacheAttnArgs &a, const CacheItem &it, int from)
@@ -118,15 +116,15 @@ struct TileWalk {
     }
     __device__ __forceinline__ int look(int pos) const { return (int)uniform_load_u32(reinterpret_cast<const uint32_t *>(table), pos >> 6); }
     // -> the next tile's first token and its page; false: none is left
-    __device__ __forceinline__ bool step(int &pos, int &page, int stride) {
+    __device__ __forceinline__ bool step(int &pos, int &page) {
         page = ahead;
         while (next < end && (unsigned)page >= (unsigned)pages) {
-            next = (next | 63) + 1;                             // (a multiple of 32 behind the missing page)
+            next = STRIDE < kPage ? (next | (kPage - 1)) + 1 : next + STRIDE;
             if (next < end) page = look(next);
         }
         if (next >= end) return false;
         pos = next;
-        next += stride;
+        next += STRIDE;
         if (next < end) ahead = look(next);
         return true;
     }
@@ -139,7 +137,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB > PATCH ? 4 * TB : PATCH];      // K, V, twice
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
     CacheItem it;
-    if (!cache_item(a, kCrossRows, it)) return;
+    int logical;
+    if (!xcd_remap((long long)a.tiles * a.BHk * a.split, logical) || !cache_item(a, logical, kCrossRows, it)) return;
     cache_slice(it, a.split);
     const int r = wave * 32 + l32, rc = it.first + min(r, it.count - 1), g = rc / it.n;
     const bool row_valid = r < it.count;
@@ -151,9 +150,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
 #pragma unroll
     for (int b = 0; b < DB; ++b) oacc[b] = zero16();
     float m_run = -INFINITY, l_run = 0.f;
-    TileWalk walk(a, it, it.begin);
+    TileWalk<BN> walk(a, it, it.begin);
     int pos, page;
-    if (walk.step(pos, page, BN)) {
+    if (walk.step(pos, page)) {
         // A thread's share of a tile: 16 codes of a row of K and of V (64 features: of one of the two).
         constexpr int LPR = D / 16, NL = D / 64;
         const int lr = (tid % (BN * LPR)) / LPR, lc = tid % LPR, which = NL == 1 ? tid / (BN * LPR) : 0;
@@ -190,7 +189,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
                 *reinterpret_cast<u32x4 *>(t + SwTile<D>::off(lr, 2 * lc + 1) * 2) = hi;
             }
             const int lo = it.begin - pos, hi = it.end - pos;
-            more = walk.step(pos, page, BN);
+            more = walk.step(pos, page);
             if (more) load(pos, page);
             __syncthreads();
             if (wave * 32 >= it.count) return;
@@ -266,16 +265,195 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
     }
 }
 
+// The same for few rows, which is bound by HBM: a workgroup has up to 32 of them, and its four waves take the tiles of its part of the range in turn,
+// each with statistics and sums of its own, joined through LDS at the end. K goes from memory to the matrix cores through registers (a lane's half
+// of a row are the features of all its steps: 64 bytes in a row), V through LDS, since the second product wants it transposed. Nothing is shared
+// between workgroups, and ranges differ in length, so items go out in plain order: every XCD has some of every sample.
+//
+// Probabilities are two bf16 terms here (three for fp32): matrix cores wait for memory anyway, and results are then as exact as products of floats.
+constexpr int kFewRows = 32, kFewWaves = 4;
+template <int D, typename T>
+__global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(CacheAttnArgs a) {
+    constexpr int BN = 32, DB = D / 32, KS = D / 16, RB = D * 2, TB = BN * RB, NT = kTerms<T>, NP = NT + (NT == 1), NL = D / 32;
+    constexpr int JOIN = 2 * DB * 4096;                        // the sums of two waves
+    __shared__ __attribute__((aligned(1024))) char smem[kFewWaves * TB > JOIN ? kFewWaves * TB : JOIN];
+    __shared__ float stat[kFewWaves][2][32];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
+    CacheItem it;
+    if (!cache_item(a, blockIdx.x, kFewRows, it)) return;
+    cache_slice(it, a.split);
+    const int rc = it.first + min(l32, it.count - 1), g = rc / it.n;
+    const bool row_valid = l32 < it.count;
+    const size_t row = (size_t)it.row0 + (g * a.N + (rc - g * it.n));
+    f32x16 oacc[DB];
+#pragma unroll
+    for (int b = 0; b < DB; ++b) oacc[b] = zero16();
+    float m_run = -INFINITY, l_run = 0.f;
+    TileWalk<BN * kFewWaves> walk(a, it, (it.begin & ~31) + wave * BN);
+    int pos, page;
+    if (walk.step(pos, page)) {
+        constexpr int LPR = D / 16, RPL = 64 / LPR;            // V: lanes a row, rows a load
+        char *vt = smem + wave * TB;
+        u32x4 kraw[NL], vraw[NL];
+        float kscale, vscale;
+        auto load = [&](int pos, int page) {
+            const size_t slot = (size_t)page * a.pool.Hk + it.hk;
+            auto at = [&](int r) { return (min(max(pos + r, it.begin), it.end - 1) & (kPage - 1)) * D; };      // rows outside the range repeat one inside
+            const uint8_t *kp = a.pool.k + slot * (kPage * D) + at(l32) + half * (D / 2), *vp = a.pool.v + slot * (kPage * D) + lane % LPR * 16;
+#pragma unroll
+            for (int j = 0; j < NL; ++j) kraw[j] = *reinterpret_cast<const u32x4 *>(kp + 16 * j);
+#pragma unroll
+            for (int j = 0; j < NL; ++j) vraw[j] = *reinterpret_cast<const u32x4 *>(vp + at(j * RPL + lane / LPR));
+            kscale = exp_scale(a.pool.k_exp + slot);
+            vscale = exp_scale(a.pool.v_exp + slot);
+        };
+        load(pos, page);
+        Ops<D, bf16_t> ops;
+        ops.init(lane);
+        bf16x8 qf[KS][NT];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) query_terms(static_cast<const T *>(a.q) + row * D + half * (D / 2) + 8 * s, qf[s]);
+        const float c = a.scale_log2;
+        bool more = true;
+        while (more) {
+            u32x4 kw[KS];
+#pragma unroll
+            for (int j = 0; j < NL; ++j) {
+                widen16(kraw[j], kscale, kw[2 * j], kw[2 * j + 1]);
+                u32x4 lo, hi;
+                widen16(vraw[j], vscale, lo, hi);
+                const int r = j * RPL + lane / LPR;
+                *reinterpret_cast<u32x4 *>(vt + SwTile<D>::off(r, 2 * (lane % LPR)) * 2) = lo;
+                *reinterpret_cast<u32x4 *>(vt + SwTile<D>::off(r, 2 * (lane % LPR) + 1) * 2) = hi;
+            }
+            const int lo = it.begin - pos, hi = it.end - pos;
+            more = walk.step(pos, page);
+            if (more) load(pos, page);
+            f32x16 s = zero16();
+#pragma unroll
+            for (int i = 0; i < KS; ++i)
+#pragma unroll
+                for (int t = NT - 1; t >= 0; --t) s = mfma32(__builtin_bit_cast(bf16x8, kw[i]), qf[i][t], s);
+            if (lo > 0 || hi < BN) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int n = (i >> 2) * 8 + half * 4 + (i & 3);
+                    if (n < lo || n >= hi) s[i] = -INFINITY;
+                }
+            }
+            float mx = s[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+            const float m_new = fmaxf(m_run, xhalf_max(mx));
+            if (__any((m_new - m_run) * c > 8.f)) {              // moved, and the sums rescaled, only when it has grown by 2^8
+                const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * c);
+                l_run *= alpha;
+#pragma unroll
+                for (int b = 0; b < DB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) oacc[b][i] *= alpha;
+                m_run = m_new;
+            }
+            const float mc = m_run * c;
+            float l_tile = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -mc));
+                l_tile += s[i];
+            }
+            l_run += l_tile;
+            __builtin_amdgcn_wave_barrier();                     // (a wave reads only what it wrote itself, and LDS serves it in order)
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                bf16x8 pf[3];
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = s[8 * ks + i];
+                three_terms(x, pf);
+#pragma unroll
+                for (int b = 0; b < DB; ++b) {
+                    const bf16x8 vf = ops.tfrag(vt, 0, b, ks);
+#pragma unroll
+                    for (int t = NP - 1; t >= 0; --t) oacc[b] = mfma32(vf, pf[t], oacc[b]);
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+    // Joins the waves: everything relative to the largest maximum, then 2 + 3 to 0 + 1, 1 to 0.
+    float l = xhalf_sum(l_run);
+    if (half == 0) {
+        stat[wave][0][l32] = m_run;
+        stat[wave][1][l32] = l;
+    }
+    __syncthreads();
+    float m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) m = fmaxf(m, stat[w][0][l32]);
+    auto weight = [&](float x) { return x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x - m) * a.scale_log2); };
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) l += stat[w][1][l32] * weight(stat[w][0][l32]);
+    const float mine = weight(m_run);
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) oacc[b][i] *= mine;
+#pragma unroll
+    for (int from = 2; from > 0; from >>= 1) {
+        char *buf = smem + (wave - from) * (DB * 4096) + lane * 16;
+        if (wave >= from && wave < 2 * from) {
+#pragma unroll
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<f32x4 *>(buf + (b * 4 + j) * 1024) = f32x4{oacc[b][4 * j], oacc[b][4 * j + 1], oacc[b][4 * j + 2], oacc[b][4 * j + 3]};
+        }
+        __syncthreads();
+        if (wave < from) {
+            buf = smem + wave * (DB * 4096) + lane * 16;
+#pragma unroll
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const f32x4 x = *reinterpret_cast<const f32x4 *>(buf + (b * 4 + j) * 1024);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) oacc[b][4 * j + i] += x[i];
+                }
+        }
+        __syncthreads();
+    }
+    if (wave > 0 || !row_valid) return;
+    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;      // nothing attended: o = 0, lse = -inf
+    const float lse = l > 0.f || l != l ? m * a.scale + logf(l) : -INFINITY;
+    if (half == 0) *(a.split > 1 ? a.part_lse + (size_t)it.z * a.rows + row : a.lse + row) = lse;
+    if (a.split > 1) {
+        if (lse != -INFINITY) store_rows_f32<D>(oacc, inv, a.part + ((size_t)it.z * a.rows + row) * D, half);
+    } else {
+        T *out = static_cast<T *>(a.o) + row * D;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                Io<T>::store4(out + b * 32 + j * 8 + half * 4, oacc[b][4 * j] * inv, oacc[b][4 * j + 1] * inv, oacc[b][4 * j + 2] * inv, oacc[b][4 * j + 3] * inv);
+    }
+}
+
 template <int D, typename T> static void attn_dispatch(CacheAttnArgs &a, hipStream_t st) {
+    const int per = a.few ? kFewRows : kCrossRows;
     a.tiles = 0;
     for (int s = 0; s < a.n_seg; ++s) {
         a.tile_at[s] = a.tiles;
-        a.tiles += ((a.q_off[s + 1] - a.q_off[s]) * a.G + kCrossRows - 1) / kCrossRows;
+        a.tiles += ((a.q_off[s + 1] - a.q_off[s]) * a.G + per - 1) / per;
     }
     a.tile_at[a.n_seg] = a.tiles;
-    {
+    const long long items = (long long)a.tiles * a.BHk * a.split;
+    if (a.few) {
+        MOC_PROF("cache_attn_few", st);
+        cache_attn_few_kernel<D, T><<<(unsigned)items, 256, 0, st>>>(a);
+    } else {
         MOC_PROF("cache_attn", st);
-        cache_attn_kernel<D, T><<<xcd_grid((long long)a.tiles * a.BHk * a.split), 256, 0, st>>>(a);
+        cache_attn_kernel<D, T><<<xcd_grid(items), 256, 0, st>>>(a);
     }
     if (a.split > 1) launch_join(a.part, a.part_lse, a.split, a.rows, D, sizeof(T) == 2 ? MOC_BF16 : MOC_F32, a.o, a.lse, st);
 }
@@ -288,14 +466,19 @@ hipError_t launch_cache_attn(CacheAttnArgs a, int d, int dtype, hipStream_t st) 
     return hipGetLastError();
 }
 
-// Parts of the ranges: as many as give every compute unit two workgroups, of 256 tokens at least; more where a sum would otherwise be longer than sums may be.
+// Which kernel a call takes, and the parts of the ranges: as many as give every compute unit two workgroups (few rows: eight, so that ranges of different
+// lengths even out, of 512 tokens at least), of 256 tokens at least; more where a sum would otherwise be longer than sums may be. Rows are
+// those of a segment on average, so that the answer is known from the sizes alone.
 CachePlan cache_attn_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype) {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     CachePlan p;
     const long long rows = (long long)B * H * N, chain = dtype == MOC_BF16 ? kChainTerms : kChainTerms / 4, least = (M + chain - 1) / chain;
-    const long long per_head = ((long long)N * (H / Hk) + kCrossRows - 1) / kCrossRows, tiles = (long long)B * Hk * (per_head + S - 1);
-    long long split = std::min<long long>((M + 255) / 256, (2 * kComputeUnits + (long long)B * Hk * per_head - 1) / ((long long)B * Hk * per_head));
-    split = std::max(split, least);
+    const long long group = (long long)N * (H / Hk), heads = (long long)B * Hk;
+    p.few = (group + S - 1) / S <= kFewRows;
+    const long long per = p.few ? kFewRows : kCrossRows, per_head = (group + per - 1) / per, tiles = heads * (per_head + S - 1);
+    const long long aim = kComputeUnits * (p.few ? 8 : 2), shortest = p.few ? 512 : 256;
+    const long long busy = heads * std::max<long long>(per_head, std::min<long long>(S, N));          // items that have rows, about
+    const long long split = std::max(std::min((M + shortest - 1) / shortest, (aim + busy - 1) / busy), least);
     p.split = (int)split;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t x = at; at += up(bytes); return x; };
