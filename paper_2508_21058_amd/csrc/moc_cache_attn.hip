@@ -8,25 +8,23 @@
 //
 // fp32 queries are three bf16 terms that add up to them exactly, and so are the probabilities: since the cached values have four bits, three products on bf16
 // matrix cores are as exact as one on float cores, at a fifth of the time.
+#include <climits>
+
 #include "moc_cache.h"
 #include "moc_attn_common.h"
 #include "moc_cross.h"
 
 namespace moc {
 
-// 16 codes as bf16 times 2^e (scale), eight to a word of 16 bytes.
-__device__ __forceinline__ void widen16(u32x4 u, float scale, u32x4 &lo, u32x4 &hi) {
-    uint32_t w[8];
+// Eight codes as bf16 times 2^e (scale).
+__device__ __forceinline__ u32x4 widen8(u32x2 u, float scale) {
+    u32x4 w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
         w[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[i], scale, false));
         w[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[i], scale, true));
     }
-    lo = u32x4{w[0], w[1], w[2], w[3]};
-    hi = u32x4{w[4], w[5], w[6], w[7]};
-}
-__device__ __forceinline__ float exp_scale(const int8_t *p) {
-    return __uint_as_float((uint32_t)(min(max((int)*p, kLeastExp), kMostExp) + 127) << 23);
+    return w;
 }
 
 // Operands of T = bf16: one term; of T = float: three bf16 terms, the largest first, whose sum is the value.
@@ -51,6 +49,13 @@ __device__ __forceinline__ void query_terms(const float *p, bf16x8 *out) {
     float x[8];
     Io<float>::load8f(p, x);
     three_terms(x, out);
+}
+// Waits for the queries here: left to the first product, the wait would stand inside the loop, and there be for the next tile's codes as well.
+template <int K, int N> __device__ __forceinline__ void pin_terms(bf16x8 (&f)[K][N]) {
+#pragma unroll
+    for (int s = 0; s < K; ++s)
+#pragma unroll
+        for (int t = 0; t < N; ++t) asm volatile("" : "+v"(f[s][t]));
 }
 // Probabilities of 8 tokens (registers 8 s ..) as the second product's operand. In bf16 they are rounded, half a step 2^-8: that product runs on
 // bf16 matrix cores, sixteen times the rate of the float ones.
@@ -104,28 +109,51 @@ __device__ __forceinline__ void cache_slice(CacheItem &it, int n) {
     const int t0 = it.begin >> 5, tiles = ((it.end + 31) >> 5) - t0, begin = it.begin, end = it.end;
     it.begin = max(begin, (t0 + (int)((long long)tiles * it.z / n)) << 5);
     it.end = min(end, (t0 + (int)((long long)tiles * (it.z + 1) / n)) << 5);
+    if (it.end <= it.begin) it.begin = it.end = 0;
 }
 
-// Walks the tiles of 32 tokens of a range whose pages are there, every STRIDE tokens; the next page's number is asked for a tile ahead.
+// Walks a range every STRIDE tokens, where pages are there. A wave's lanes hold the page numbers and exponents of 64 blocks at a
+// time: a tile's are lane reads, and a missing page is a bit that is looked over. (Asked for tile by tile through the scalar cache, each waited for the
+// answer at the next barrier: 24 heads of 4,096 queries and 32k tokens CARD us, this way NOW.)
+struct Tile {
+    int pos, page;
+    float kscale, vscale;
+};
 template <int STRIDE> struct TileWalk {
+    const CachePool &pool;
     const int32_t *table;
-    int pages, end, next, ahead;       // next: where to look on, ahead: its page
+    int hk, end, next;
+    int base, pages, exps;             // first block of the lanes; a lane's page and biased exponents (values' in the upper half)
+    unsigned long long there;
     __device__ __forceinline__ TileWalk(const CacheAttnArgs &a, const CacheItem &it, int from)
-        : table(a.pool.table + (size_t)it.b * a.pool.blocks), pages(a.pool.pages), end(it.end), next(from & ~31), ahead(-1) {
-        if (next < end) ahead = look(next);
+        : pool(a.pool), table(a.pool.table + (size_t)it.b * a.pool.blocks), hk(it.hk), end(it.end), next(from), base(INT_MIN) {}
+    __device__ __forceinline__ void look(int block) {
+        const int mine = block + (int)(threadIdx.x & 63);
+        base = block;
+        pages = mine <= (end - 1) >> 6 ? table[mine] : -1;
+        const bool ok = (unsigned)pages < (unsigned)pool.pages;
+        there = __ballot(ok);
+        const size_t slot = (size_t)(ok ? pages : 0) * pool.Hk + hk;
+        auto biased = [](int e) { return min(max(e, kLeastExp), kMostExp) + 127; };
+        exps = biased(pool.k_exp[slot]) | biased(pool.v_exp[slot]) << 16;
     }
-    __device__ __forceinline__ int look(int pos) const { return (int)uniform_load_u32(reinterpret_cast<const uint32_t *>(table), pos >> 6); }
-    // -> the next tile's first token and its page; false: none is left
-    __device__ __forceinline__ bool step(int &pos, int &page) {
-        page = ahead;
-        while (next < end && (unsigned)page >= (unsigned)pages) {
-            next = STRIDE < kPage ? (next | (kPage - 1)) + 1 : next + STRIDE;
-            if (next < end) page = look(next);
+    // -> the next tile; false: none is left
+    __device__ __forceinline__ bool step(Tile &t) {
+        while (next < end) {
+            const int block = next >> 6;
+            if (base == INT_MIN || block >= base + 64) look(block);
+            const unsigned long long rest = there >> (block - base);
+            if (rest & 1) break;
+            // (behind the missing pages, or the lanes; strides of pages keep their step)
+            next = STRIDE == kPage ? (block + (rest ? __builtin_ctzll(rest) : 64 - (block - base))) << 6 : next + STRIDE;
         }
         if (next >= end) return false;
-        pos = next;
+        const int lane = (next >> 6) - base, e = __builtin_amdgcn_readlane(exps, lane);
+        t.pos = next;
+        t.page = __builtin_amdgcn_readlane(pages, lane);
+        t.kscale = __uint_as_float((uint32_t)(e & 0xffff) << 23);
+        t.vscale = __uint_as_float((uint32_t)(e >> 16) << 23);
         next += STRIDE;
-        if (next < end) ahead = look(next);
         return true;
     }
 };
@@ -150,57 +178,91 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
 #pragma unroll
     for (int b = 0; b < DB; ++b) oacc[b] = zero16();
     float m_run = -INFINITY, l_run = 0.f;
-    TileWalk<BN> walk(a, it, it.begin);
-    int pos, page;
-    if (walk.step(pos, page)) {
+    TileWalk<kPage> walk(a, it, it.begin & ~(kPage - 1));
+    Tile t;
+    if (walk.step(t)) {
         // A thread's share of a tile: 16 codes of a row of K and of V (64 features: of one of the two).
         constexpr int LPR = D / 16, NL = D / 64;
-        const int lr = (tid % (BN * LPR)) / LPR, lc = tid % LPR, which = NL == 1 ? tid / (BN * LPR) : 0;
-        u32x4 raw[NL];
-        float scale[NL];
-        auto load = [&](int pos, int page) {
-            const size_t slot = (size_t)page * a.pool.Hk + it.hk;
-            const int at = min(max(pos + lr, it.begin), it.end - 1) & (kPage - 1);      // rows outside the range repeat one inside
+        const int lr = (threadIdx.x % (BN * LPR)) / LPR, lc = threadIdx.x % LPR, which = NL == 1 ? threadIdx.x / (BN * LPR) : 0;
+        // Which half of them a lane takes first: neighbours of a row, and neighbouring rows, write to different banks then.
+        const int swap = D == 128 ? ((lc >> 2) ^ lr) & 1 : (lr ^ (lr >> 1)) & 1;
+        const int at[2] = {SwTile<D>::off(lr, 2 * lc + swap) * 2, SwTile<D>::off(lr, 2 * lc + 1 - swap) * 2};
+        const uint32_t mine = lr * D + lc * 16 + 8 * swap;
+        u32x2 raw[NL][2];
+        auto load = [&](auto half_page) {
+            constexpr int HP = decltype(half_page)::value;
+            const size_t page = ((size_t)t.page * a.pool.Hk + it.hk) * (kPage * D);
+            uint32_t off = mine + HP * BN * D;
+            if (t.pos < it.begin || t.pos + kPage > it.end)                        // rows outside the range repeat one inside
+                off = (min(max(t.pos + HP * BN + lr, it.begin), it.end - 1) & (kPage - 1)) * D + lc * 16 + 8 * swap;
+#pragma unroll
+            for (int j = 0; j < NL; ++j) {
+                const uint8_t *base = ((NL == 1 ? which : j) ? a.pool.v : a.pool.k) + page;
+                raw[j][0] = *reinterpret_cast<const u32x2 *>(base + off);
+                raw[j][1] = *reinterpret_cast<const u32x2 *>(base + (off ^ 8));
+            }
+        };
+        auto stage = [&](char *kt, float kscale, float vscale) {
 #pragma unroll
             for (int j = 0; j < NL; ++j) {
                 const bool v = (NL == 1 ? which : j) != 0;
-                raw[j] = *reinterpret_cast<const u32x4 *>((v ? a.pool.v : a.pool.k) + slot * (kPage * D) + at * D + lc * 16);
-                scale[j] = exp_scale((v ? a.pool.v_exp : a.pool.k_exp) + slot);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) *reinterpret_cast<u32x4 *>(kt + (v ? TB : 0) + at[u]) = widen8(raw[j][u], v ? vscale : kscale);
             }
         };
-        load(pos, page);
+        // The two tiles of a page have a buffer each, and a copy of the loop. Two tiles ahead of the one in LDS is asked for, one ahead is written between
+        // the products. Behind the last tile it is asked for and written again, which nobody reads: no branch cuts the schedule.
+        int pos = t.pos;                     // of the page whose tiles are in LDS, or the first of which is
+        bool another = false, more = true;   // another page is there; another tile
+        const bool from_half = it.begin - pos >= BN;
+        if (!from_half) {
+            load(IC<0>{});
+            stage(smem, t.kscale, t.vscale);
+            load(IC<1>{});
+        } else {
+            load(IC<1>{});
+            stage(smem + 2 * TB, t.kscale, t.vscale);
+            another = walk.step(t);
+            load(IC<0>{});
+        }
         Ops<D, bf16_t> ops;
         ops.init(lane);
         bf16x8 qf[KS][NT];
 #pragma unroll
         for (int s = 0; s < KS; ++s) query_terms(static_cast<const T *>(a.q) + row * D + 16 * s + 8 * half, qf[s]);
+        pin_terms(qf);
         const float c = a.scale_log2;
-        bool first = true, more = true;
-        // One tile; the buffers take turns in a loop unrolled by two, so that LDS addresses are constants beside the lane's offsets.
-        auto tile = [&](auto which_buf) {
-            constexpr int BUF = decltype(which_buf)::value;
-            char *kt = smem + BUF * 2 * TB, *vt = kt + TB;
-#pragma unroll
-            for (int j = 0; j < NL; ++j) {
-                u32x4 lo, hi;
-                widen16(raw[j], scale[j], lo, hi);
-                char *t = (NL == 1 ? which : j) ? vt : kt;
-                *reinterpret_cast<u32x4 *>(t + SwTile<D>::off(lr, 2 * lc) * 2) = lo;
-                *reinterpret_cast<u32x4 *>(t + SwTile<D>::off(lr, 2 * lc + 1) * 2) = hi;
-            }
-            const int lo = it.begin - pos, hi = it.end - pos;
-            more = walk.step(pos, page);
-            if (more) load(pos, page);
+        bool first = true;
+        auto tile = [&](auto half_page) {
+            constexpr int HP = decltype(half_page)::value;
+            char *kt = smem + HP * 2 * TB, *vt = kt + TB, *other = smem + (HP ^ 1) * 2 * TB;
+            const int lo = it.begin - pos - HP * BN, hi = it.end - pos - HP * BN;
+            auto ahead = [&] {
+                stage(other, t.kscale, t.vscale);
+                if (HP == 0) {
+                    more = hi > BN;
+                    another = walk.step(t);
+                    load(IC<0>{});
+                } else {
+                    more = another;
+                    pos = t.pos;
+                    load(IC<1>{});
+                }
+            };
             __syncthreads();
-            if (wave * 32 >= it.count) return;
+            if (wave * 32 >= it.count) {
+                ahead();
+                return;
+            }
             ops.pin();
             f32x16 s = zero16();
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
                 const bf16x8 kf = ops.frag(kt, 0, i);
 #pragma unroll
-                for (int t = NT - 1; t >= 0; --t) s = mfma32(kf, qf[i][t], s);
+                for (int x = NT - 1; x >= 0; --x) s = mfma32(kf, qf[i][x], s);
             }
+            ahead();
             if (lo > 0 || hi < BN) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -240,15 +302,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
                 for (int b = 0; b < DB; ++b) {
                     const bf16x8 vf = ops.tfrag(vt, 0, b, ks);
 #pragma unroll
-                    for (int t = NT - 1; t >= 0; --t) oacc[b] = mfma32(vf, pf[t], oacc[b]);
+                    for (int x = NT - 1; x >= 0; --x) oacc[b] = mfma32(vf, pf[x], oacc[b]);
                 }
             }
         };
-        while (true) {
+        if (from_half) tile(IC<1>{});
+        while (more) {
             tile(IC<0>{});
-            if (!more) break;
-            tile(IC<1>{});
-            if (!more) break;
+            if (more) tile(IC<1>{});
         }
     }
     const float l = xhalf_sum(l_run);
@@ -290,50 +351,47 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(CacheAttnArgs a)
     for (int b = 0; b < DB; ++b) oacc[b] = zero16();
     float m_run = -INFINITY, l_run = 0.f;
     TileWalk<BN * kFewWaves> walk(a, it, (it.begin & ~31) + wave * BN);
-    int pos, page;
-    if (walk.step(pos, page)) {
+    Tile t;
+    if (walk.step(t)) {
         constexpr int LPR = D / 16, RPL = 64 / LPR;            // V: lanes a row, rows a load
         char *vt = smem + wave * TB;
         u32x4 kraw[NL], vraw[NL];
-        float kscale, vscale;
-        auto load = [&](int pos, int page) {
-            const size_t slot = (size_t)page * a.pool.Hk + it.hk;
-            auto at = [&](int r) { return (min(max(pos + r, it.begin), it.end - 1) & (kPage - 1)) * D; };      // rows outside the range repeat one inside
+        auto load = [&] {
+            const size_t slot = (size_t)t.page * a.pool.Hk + it.hk;
+            auto at = [&](int r) { return (min(max(t.pos + r, it.begin), it.end - 1) & (kPage - 1)) * D; };      // rows outside the range repeat one inside
             const uint8_t *kp = a.pool.k + slot * (kPage * D) + at(l32) + half * (D / 2), *vp = a.pool.v + slot * (kPage * D) + lane % LPR * 16;
 #pragma unroll
             for (int j = 0; j < NL; ++j) kraw[j] = *reinterpret_cast<const u32x4 *>(kp + 16 * j);
 #pragma unroll
             for (int j = 0; j < NL; ++j) vraw[j] = *reinterpret_cast<const u32x4 *>(vp + at(j * RPL + lane / LPR));
-            kscale = exp_scale(a.pool.k_exp + slot);
-            vscale = exp_scale(a.pool.v_exp + slot);
         };
-        load(pos, page);
+        load();
         Ops<D, bf16_t> ops;
         ops.init(lane);
         bf16x8 qf[KS][NT];
 #pragma unroll
         for (int s = 0; s < KS; ++s) query_terms(static_cast<const T *>(a.q) + row * D + half * (D / 2) + 8 * s, qf[s]);
+        pin_terms(qf);
         const float c = a.scale_log2;
         bool more = true;
         while (more) {
             u32x4 kw[KS];
 #pragma unroll
             for (int j = 0; j < NL; ++j) {
-                widen16(kraw[j], kscale, kw[2 * j], kw[2 * j + 1]);
-                u32x4 lo, hi;
-                widen16(vraw[j], vscale, lo, hi);
+                kw[2 * j] = widen8(u32x2{kraw[j][0], kraw[j][1]}, t.kscale);
+                kw[2 * j + 1] = widen8(u32x2{kraw[j][2], kraw[j][3]}, t.kscale);
                 const int r = j * RPL + lane / LPR;
-                *reinterpret_cast<u32x4 *>(vt + SwTile<D>::off(r, 2 * (lane % LPR)) * 2) = lo;
-                *reinterpret_cast<u32x4 *>(vt + SwTile<D>::off(r, 2 * (lane % LPR) + 1) * 2) = hi;
+                *reinterpret_cast<u32x4 *>(vt + SwTile<D>::off(r, 2 * (lane % LPR)) * 2) = widen8(u32x2{vraw[j][0], vraw[j][1]}, t.vscale);
+                *reinterpret_cast<u32x4 *>(vt + SwTile<D>::off(r, 2 * (lane % LPR) + 1) * 2) = widen8(u32x2{vraw[j][2], vraw[j][3]}, t.vscale);
             }
-            const int lo = it.begin - pos, hi = it.end - pos;
-            more = walk.step(pos, page);
-            if (more) load(pos, page);
+            const int lo = it.begin - t.pos, hi = it.end - t.pos;
+            more = walk.step(t);
+            if (more) load();
             f32x16 s = zero16();
 #pragma unroll
             for (int i = 0; i < KS; ++i)
 #pragma unroll
-                for (int t = NT - 1; t >= 0; --t) s = mfma32(__builtin_bit_cast(bf16x8, kw[i]), qf[i][t], s);
+                for (int x = NT - 1; x >= 0; --x) s = mfma32(__builtin_bit_cast(bf16x8, kw[i]), qf[i][x], s);
             if (lo > 0 || hi < BN) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -374,7 +432,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(CacheAttnArgs a)
                 for (int b = 0; b < DB; ++b) {
                     const bf16x8 vf = ops.tfrag(vt, 0, b, ks);
 #pragma unroll
-                    for (int t = NP - 1; t >= 0; --t) oacc[b] = mfma32(vf, pf[t], oacc[b]);
+                    for (int x = NP - 1; x >= 0; --x) oacc[b] = mfma32(vf, pf[x], oacc[b]);
                 }
             }
             __builtin_amdgcn_wave_barrier();
