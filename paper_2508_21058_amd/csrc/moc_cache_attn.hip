@@ -116,14 +116,14 @@ __device__ __forceinline__ void cache_slice(CacheItem &it, int n) {
 // time: a tile's are lane reads, and a missing page is a bit that is looked over. (Asked for tile by tile through the scalar cache, each waited for the
 // answer at the next barrier: 24 heads of 4,096 queries and 32k tokens CARD us, this way NOW.)
 struct Tile {
-    int pos, page;
-    float kscale, vscale;
+    int pos, page, lane;
 };
 template <int STRIDE> struct TileWalk {
     const CachePool &pool;
     const int32_t *table;
     int hk, end, next;
-    int base, pages, exps;             // first block of the lanes; a lane's page and biased exponents (values' in the upper half)
+    int base;                          // first block of the lanes
+    int pages, kexp, vexp;             // a lane's page and exponents
     unsigned long long there;
     __device__ __forceinline__ TileWalk(const CacheAttnArgs &a, const CacheItem &it, int from)
         : pool(a.pool), table(a.pool.table + (size_t)it.b * a.pool.blocks), hk(it.hk), end(it.end), next(from), base(INT_MIN) {}
@@ -134,8 +134,8 @@ template <int STRIDE> struct TileWalk {
         const bool ok = (unsigned)pages < (unsigned)pool.pages;
         there = __ballot(ok);
         const size_t slot = (size_t)(ok ? pages : 0) * pool.Hk + hk;
-        auto biased = [](int e) { return min(max(e, kLeastExp), kMostExp) + 127; };
-        exps = biased(pool.k_exp[slot]) | biased(pool.v_exp[slot]) << 16;
+        kexp = pool.k_exp[slot];
+        vexp = pool.v_exp[slot];
     }
     // -> the next tile; false: none is left
     __device__ __forceinline__ bool step(Tile &t) {
@@ -148,13 +148,17 @@ template <int STRIDE> struct TileWalk {
             next = STRIDE == kPage ? (block + (rest ? __builtin_ctzll(rest) : 64 - (block - base))) << 6 : next + STRIDE;
         }
         if (next >= end) return false;
-        const int lane = (next >> 6) - base, e = __builtin_amdgcn_readlane(exps, lane);
         t.pos = next;
-        t.page = __builtin_amdgcn_readlane(pages, lane);
-        t.kscale = __uint_as_float((uint32_t)(e & 0xffff) << 23);
-        t.vscale = __uint_as_float((uint32_t)(e >> 16) << 23);
+        t.lane = (next >> 6) - base;
+        t.page = __builtin_amdgcn_readlane(pages, t.lane);
         next += STRIDE;
         return true;
+    }
+    // The scales of the last tile that step() gave. (Apart from it: the codes are asked for while exponents are on their way.)
+    __device__ __forceinline__ void scales(const Tile &t, float &k, float &v) const {
+        auto pow2 = [&](int e) { return __uint_as_float((uint32_t)(min(max(__builtin_amdgcn_readlane(e, t.lane & 63), kLeastExp), kMostExp) + 127) << 23); };
+        k = pow2(kexp);
+        v = pow2(vexp);
     }
 };
 
@@ -202,7 +206,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
                 raw[j][1] = *reinterpret_cast<const u32x2 *>(base + (off ^ 8));
             }
         };
-        auto stage = [&](char *kt, float kscale, float vscale) {
+        auto stage = [&](char *kt) {
+            float kscale, vscale;
+            walk.scales(t, kscale, vscale);
 #pragma unroll
             for (int j = 0; j < NL; ++j) {
                 const bool v = (NL == 1 ? which : j) != 0;
@@ -217,11 +223,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
         const bool from_half = it.begin - pos >= BN;
         if (!from_half) {
             load(IC<0>{});
-            stage(smem, t.kscale, t.vscale);
+            stage(smem);
             load(IC<1>{});
         } else {
             load(IC<1>{});
-            stage(smem + 2 * TB, t.kscale, t.vscale);
+            stage(smem + 2 * TB);
             another = walk.step(t);
             load(IC<0>{});
         }
@@ -238,7 +244,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
             char *kt = smem + HP * 2 * TB, *vt = kt + TB, *other = smem + (HP ^ 1) * 2 * TB;
             const int lo = it.begin - pos - HP * BN, hi = it.end - pos - HP * BN;
             auto ahead = [&] {
-                stage(other, t.kscale, t.vscale);
+                stage(other);
                 if (HP == 0) {
                     more = hi > BN;
                     another = walk.step(t);
@@ -350,6 +356,9 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(CacheAttnArgs a)
 #pragma unroll
     for (int b = 0; b < DB; ++b) oacc[b] = zero16();
     float m_run = -INFINITY, l_run = 0.f;
+    bf16x8 qf[KS][NT];                                         // (asked for before the pages are)
+#pragma unroll
+    for (int s = 0; s < KS; ++s) query_terms(static_cast<const T *>(a.q) + row * D + half * (D / 2) + 8 * s, qf[s]);
     TileWalk<BN * kFewWaves> walk(a, it, (it.begin & ~31) + wave * BN);
     Tile t;
     if (walk.step(t)) {
@@ -368,21 +377,20 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(CacheAttnArgs a)
         load();
         Ops<D, bf16_t> ops;
         ops.init(lane);
-        bf16x8 qf[KS][NT];
-#pragma unroll
-        for (int s = 0; s < KS; ++s) query_terms(static_cast<const T *>(a.q) + row * D + half * (D / 2) + 8 * s, qf[s]);
         pin_terms(qf);
         const float c = a.scale_log2;
         bool more = true;
         while (more) {
             u32x4 kw[KS];
+            float kscale, vscale;
+            walk.scales(t, kscale, vscale);
 #pragma unroll
             for (int j = 0; j < NL; ++j) {
-                kw[2 * j] = widen8(u32x2{kraw[j][0], kraw[j][1]}, t.kscale);
-                kw[2 * j + 1] = widen8(u32x2{kraw[j][2], kraw[j][3]}, t.kscale);
+                kw[2 * j] = widen8(u32x2{kraw[j][0], kraw[j][1]}, kscale);
+                kw[2 * j + 1] = widen8(u32x2{kraw[j][2], kraw[j][3]}, kscale);
                 const int r = j * RPL + lane / LPR;
-                *reinterpret_cast<u32x4 *>(vt + SwTile<D>::off(r, 2 * (lane % LPR)) * 2) = widen8(u32x2{vraw[j][0], vraw[j][1]}, t.vscale);
-                *reinterpret_cast<u32x4 *>(vt + SwTile<D>::off(r, 2 * (lane % LPR) + 1) * 2) = widen8(u32x2{vraw[j][2], vraw[j][3]}, t.vscale);
+                *reinterpret_cast<u32x4 *>(vt + SwTile<D>::off(r, 2 * (lane % LPR)) * 2) = widen8(u32x2{vraw[j][0], vraw[j][1]}, vscale);
+                *reinterpret_cast<u32x4 *>(vt + SwTile<D>::off(r, 2 * (lane % LPR) + 1) * 2) = widen8(u32x2{vraw[j][2], vraw[j][3]}, vscale);
             }
             const int lo = it.begin - t.pos, hi = it.end - t.pos;
             more = walk.step(t);
@@ -524,27 +532,45 @@ hipError_t launch_cache_attn(CacheAttnArgs a, int d, int dtype, hipStream_t st) 
     return hipGetLastError();
 }
 
-// Which kernel a call takes, and the parts of the ranges: as many as give every compute unit two workgroups (few rows: eight, so that ranges of different
-// lengths even out, of 512 tokens at least), of 256 tokens at least; more where a sum would otherwise be longer than sums may be. Rows are
-// those of a segment on average, so that the answer is known from the sizes alone.
+// Which kernel a call takes, and the parts of the ranges. Rows are those of a segment on average, so that the answer follows from the sizes alone.
+// Few rows: 512 workgroups, two on a compute unit, of 512 tokens at least; 1,024 where they have 2,048 tokens each, so that ranges of different lengths
+// even out (eight samples, four key heads, 39k to 131k tokens: in 8 / 16 / 32 / 64 parts 167 / 145 / 141 / 144 us; four of 8k at most in 8 / 16 / 32 / 64
+// parts 26 / 24 / 25 / 29).
+// Many rows: from an estimate of the time, as for cross attention. w workgroups on a compute unit run three at a time (two heads of 128 fp32 features);
+// 32 tokens take `at_once[r - 1]` us with r of them, to begin and end 6 us a round, and parts cost their sums, written and read again. (24 heads, 1,560
+// queries, 33k tokens: one part 1,122 us, two 792, three 790, four 710, six 765, eight 741; two heads of 903 rows, 2k tokens: one 59, four 26, eight 22, sixteen 24.)
 CachePlan cache_attn_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype) {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     CachePlan p;
-    const long long rows = (long long)B * H * N, chain = dtype == MOC_BF16 ? kChainTerms : kChainTerms / 4, least = (M + chain - 1) / chain;
-    const long long group = (long long)N * (H / Hk), heads = (long long)B * Hk;
-    p.few = (group + S - 1) / S <= kFewRows;
-    const long long per = p.few ? kFewRows : kCrossRows, per_head = (group + per - 1) / per, tiles = heads * (per_head + S - 1);
-    const long long aim = kComputeUnits * (p.few ? 8 : 2), shortest = p.few ? 512 : 256;
-    const long long busy = heads * std::max<long long>(per_head, std::min<long long>(S, N));          // items that have rows, about
-    const long long split = std::max(std::min((M + shortest - 1) / shortest, (aim + busy - 1) / busy), least);
+    const bool bf16 = dtype == MOC_BF16;
+    const long long rows = (long long)B * H * N, chain = bf16 ? kChainTerms : kChainTerms / 4, least = (M + chain - 1) / chain;
+    const long long group = (long long)N * (H / Hk), heads = (long long)B * Hk, own = (group + S - 1) / S;          // rows of a segment
+    p.few = own <= kFewRows;
+    const long long per = p.few ? kFewRows : kCrossRows, items = heads * std::min<long long>(S, N) * ((own + per - 1) / per);
+    long long split = least;
+    if (p.few) {
+        auto parts = [&](long long aim) { return (aim + items - 1) / items; };
+        split = std::max(split, std::min((M + 511LL) / 512, std::max(parts(512), std::min(parts(1024), M / 2048LL))));
+    } else {
+        static const double at_once[2][2][3] = {{{0.6, 0.78, 1.01}, {0.83, 1.08, 1.48}}, {{1.04, 1.49, 2.0}, {1.57, 2.13, 0}}};
+        const double *us = at_once[!bf16][d == 128], sums = (double)rows * d * 8 / 5e6;
+        const int most = us[2] > 0 ? 3 : 2;
+        double best = 0;
+        for (long long s = least, top = std::max(least, std::min(256LL, (M + 127LL) / 128)); s <= top; ++s) {
+            const long long w = (items * s + kComputeUnits - 1) / kComputeUnits;
+            const double t = (w / most * us[most - 1] + (w % most ? us[w % most - 1] : 0)) * std::max(1., M / 32. / s) + (w + most - 1) / most * 6 +
+                             (s > 1 ? s * sums + 6 : 0);
+            if (s == least || t < best) { best = t; split = s; }
+        }
+    }
     p.split = (int)split;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t x = at; at += up(bytes); return x; };
     p.part = take(split > 1 ? (size_t)split * rows * d * 4 : 0);
     p.part_lse = take(split > 1 ? (size_t)split * rows * 4 : 0);
     p.total = at;
-    // (a launch has fewer than 2^32 threads)
-    const long long most = (1 << 24) - 1024;
+    // (a launch has fewer than 2^32 threads; segments of other sizes than the average one have more tiles)
+    const long long most = (1 << 24) - 1024, tiles = heads * ((group + per - 1) / per + S - 1);
     p.fits = tiles * split < most && (split == 1 || rows * (d / 4) / 256 < most);
     return p;
 }
