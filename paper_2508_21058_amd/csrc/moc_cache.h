@@ -36,14 +36,14 @@ struct CacheAttnArgs {
     long long rows;                            // B * H * N
     int N, M, n_seg, H, G, BHk;                // G query heads on a key head
     int tiles, split;                          // query tiles of a key head, parts of a range
-    bool few;                                  // see CachePlan
+    int few;                                   // see CachePlan
     float scale, scale_log2;
     int32_t q_off[MOC_MAX_CROSS_SEGMENTS + 1];
     int32_t tile_at[MOC_MAX_CROSS_SEGMENTS + 1];      // first query tile of a segment
 };
 struct CachePlan {
     int split;
-    bool few;                                  // few rows a segment: the kernel whose waves share out the tokens
+    int few;                                   // few rows a segment: the kernel whose waves share out the tokens, with so many (16, 32) rows; else 0
     bool fits;
     size_t part, part_lse, total;              // workspace, byte offsets
 };

@@ -332,62 +332,89 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
     }
 }
 
-// The same for few rows, which is bound by HBM: a workgroup has up to 32 of them, and its four waves take the tiles of its part of the range in turn,
-// each with statistics and sums of its own, joined through LDS at the end. K goes from memory to the matrix cores through registers (a lane's half
-// of a row are the features of all its steps: 64 bytes in a row), V through LDS, since the second product wants it transposed. Nothing is shared
-// between workgroups, and ranges differ in length, so items go out in plain order: every XCD has some of every sample.
+// The same for few rows, which is bound by HBM: a workgroup has up to 16 NQ of them, and its four waves take the tiles of its part of the range in turn,
+// each with statistics and sums of its own, joined through LDS at the end. Products are 16 x 16 (a lane owns a query of each block of 16, four lanes
+// share one): a tile is half the work of 32 x 32 for up to 16 rows, and a wave alone on its SIMD takes 1.0 us for the latter. K goes from memory to the matrix
+// cores through registers (a lane's quarter of a row are the features of all its steps), V through LDS, since the second product wants it transposed. Nothing is
+// shared between workgroups, and ranges differ in length, so items go out in plain order: every XCD has some of every sample.
 //
 // Probabilities are two bf16 terms here (three for fp32): matrix cores wait for memory anyway, and results are then as exact as products of floats.
-constexpr int kFewRows = 32, kFewWaves = 4;
-template <int D, typename T>
-__global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(CacheAttnArgs a) {
-    constexpr int BN = 32, DB = D / 32, KS = D / 16, RB = D * 2, TB = BN * RB, NT = kTerms<T>, NP = NT + (NT == 1), NL = D / 32;
-    constexpr int JOIN = 2 * DB * 4096;                        // the sums of two waves
+constexpr int kFewWaves = 4;
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// max (or sum) over the four lanes of a query
+__device__ __forceinline__ float quad_max(float v) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return xhalf_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return xhalf_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+template <int D, typename T, int NQ>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void cache_attn_few_kernel(CacheAttnArgs a) {
+    constexpr int BN = 32, DB = D / 16, KS = D / 32, RB = D * 2, TB = BN * RB, NT = kTerms<T>, NP = NT + (NT == 1), NK = D / 64, NV = D / 32;
+    constexpr int JOIN = kFewWaves / 2 * NQ * DB * 1024;       // the sums of half the waves
     __shared__ __attribute__((aligned(1024))) char smem[kFewWaves * TB > JOIN ? kFewWaves * TB : JOIN];
-    __shared__ float stat[kFewWaves][2][32];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
+    __shared__ float stat[kFewWaves][2][16 * NQ];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, l16 = lane & 15;
     CacheItem it;
-    if (!cache_item(a, blockIdx.x, kFewRows, it)) return;
+    if (!cache_item(a, blockIdx.x, 16 * NQ, it)) return;
     cache_slice(it, a.split);
-    const int rc = it.first + min(l32, it.count - 1), g = rc / it.n;
-    const bool row_valid = l32 < it.count;
-    const size_t row = (size_t)it.row0 + (g * a.N + (rc - g * it.n));
-    f32x16 oacc[DB];
+    size_t row[NQ];
+    bf16x8 qf[NQ][KS][NT];                                     // (asked for before the pages are)
 #pragma unroll
-    for (int b = 0; b < DB; ++b) oacc[b] = zero16();
-    float m_run = -INFINITY, l_run = 0.f;
-    bf16x8 qf[KS][NT];                                         // (asked for before the pages are)
+    for (int q = 0; q < NQ; ++q) {
+        const int rc = it.first + min(16 * q + l16, it.count - 1), g = rc / it.n;
+        row[q] = (size_t)it.row0 + (g * a.N + (rc - g * it.n));
 #pragma unroll
-    for (int s = 0; s < KS; ++s) query_terms(static_cast<const T *>(a.q) + row * D + half * (D / 2) + 8 * s, qf[s]);
+        for (int s = 0; s < KS; ++s) query_terms(static_cast<const T *>(a.q) + row[q] * D + quarter * (D / 4) + 8 * s, qf[q][s]);
+    }
+    f32x4 oacc[NQ][DB];
+    float m_run[NQ], l_run[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        m_run[q] = -INFINITY;
+        l_run[q] = 0.f;
+#pragma unroll
+        for (int b = 0; b < DB; ++b) oacc[q][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     TileWalk<BN * kFewWaves> walk(a, it, (it.begin & ~31) + wave * BN);
     Tile t;
     if (walk.step(t)) {
         constexpr int LPR = D / 16, RPL = 64 / LPR;            // V: lanes a row, rows a load
         char *vt = smem + wave * TB;
-        u32x4 kraw[NL], vraw[NL];
+        u32x4 kraw[2][NK], vraw[NV];
         auto load = [&] {
             const size_t slot = (size_t)t.page * a.pool.Hk + it.hk;
             auto at = [&](int r) { return (min(max(t.pos + r, it.begin), it.end - 1) & (kPage - 1)) * D; };      // rows outside the range repeat one inside
-            const uint8_t *kp = a.pool.k + slot * (kPage * D) + at(l32) + half * (D / 2), *vp = a.pool.v + slot * (kPage * D) + lane % LPR * 16;
+            const uint8_t *kp = a.pool.k + slot * (kPage * D) + quarter * (D / 4), *vp = a.pool.v + slot * (kPage * D) + lane % LPR * 16;
 #pragma unroll
-            for (int j = 0; j < NL; ++j) kraw[j] = *reinterpret_cast<const u32x4 *>(kp + 16 * j);
+            for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int j = 0; j < NL; ++j) vraw[j] = *reinterpret_cast<const u32x4 *>(vp + at(j * RPL + lane / LPR));
+                for (int j = 0; j < NK; ++j) kraw[m][j] = *reinterpret_cast<const u32x4 *>(kp + at(16 * m + l16) + 16 * j);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) vraw[j] = *reinterpret_cast<const u32x4 *>(vp + at(j * RPL + lane / LPR));
         };
         load();
-        Ops<D, bf16_t> ops;
-        ops.init(lane);
-        pin_terms(qf);
+        // The transposed operand of feature block b: lane (quarter, i) of the block's features i gets tokens 4 quarter .. + 4, and those 16 on.
+        int tr[DB];
+#pragma unroll
+        for (int b = 0; b < DB; ++b) tr[b] = (SwTile<D>::off(4 * quarter + (l16 >> 2), 2 * b + ((l16 & 3) >> 1)) + (l16 & 1) * 4) * 2;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) pin_terms(qf[q]);
         const float c = a.scale_log2;
         bool more = true;
         while (more) {
-            u32x4 kw[KS];
+            bf16x8 kw[2][KS];
             float kscale, vscale;
             walk.scales(t, kscale, vscale);
 #pragma unroll
-            for (int j = 0; j < NL; ++j) {
-                kw[2 * j] = widen8(u32x2{kraw[j][0], kraw[j][1]}, kscale);
-                kw[2 * j + 1] = widen8(u32x2{kraw[j][2], kraw[j][3]}, kscale);
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int j = 0; j < KS; ++j)
+                    kw[m][j] = __builtin_bit_cast(bf16x8, widen8(u32x2{kraw[m][j >> 1][2 * (j & 1)], kraw[m][j >> 1][2 * (j & 1) + 1]}, kscale));
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
                 const int r = j * RPL + lane / LPR;
                 *reinterpret_cast<u32x4 *>(vt + SwTile<D>::off(r, 2 * (lane % LPR)) * 2) = widen8(u32x2{vraw[j][0], vraw[j][1]}, vscale);
                 *reinterpret_cast<u32x4 *>(vt + SwTile<D>::off(r, 2 * (lane % LPR) + 1) * 2) = widen8(u32x2{vraw[j][2], vraw[j][3]}, vscale);
@@ -395,118 +422,128 @@ __global__ __launch_bounds__(256, 2) void cache_attn_few_kernel(CacheAttnArgs a)
             const int lo = it.begin - t.pos, hi = it.end - t.pos;
             more = walk.step(t);
             if (more) load();
-            f32x16 s = zero16();
+            bf16x8 pf[NQ][3];
 #pragma unroll
-            for (int i = 0; i < KS; ++i)
+            for (int q = 0; q < NQ; ++q) {
+                float x[8];                                      // token 16 (i / 4) + 4 quarter + i % 4
 #pragma unroll
-                for (int x = NT - 1; x >= 0; --x) s = mfma32(__builtin_bit_cast(bf16x8, kw[i]), qf[i][x], s);
-            if (lo > 0 || hi < BN) {
+                for (int m = 0; m < 2; ++m) {
+                    f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int n = (i >> 2) * 8 + half * 4 + (i & 3);
-                    if (n < lo || n >= hi) s[i] = -INFINITY;
+                    for (int i = 0; i < KS; ++i)
+#pragma unroll
+                        for (int y = NT - 1; y >= 0; --y) s = mfma16(kw[m][i], qf[q][i][y], s);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[4 * m + i] = s[i];
                 }
+                if (lo > 0 || hi < BN) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int n = (i >> 2) * 16 + quarter * 4 + (i & 3);
+                        if (n < lo || n >= hi) x[i] = -INFINITY;
+                    }
+                }
+                float mx = x[0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) mx = fmaxf(mx, x[i]);
+                const float m_new = fmaxf(m_run[q], quad_max(mx));
+                if (__any((m_new - m_run[q]) * c > 8.f)) {       // moved, and the sums rescaled, only when it has grown by 2^8
+                    const float alpha = __builtin_amdgcn_exp2f((m_run[q] - m_new) * c);
+                    l_run[q] *= alpha;
+#pragma unroll
+                    for (int b = 0; b < DB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) oacc[q][b][i] *= alpha;
+                    m_run[q] = m_new;
+                }
+                const float mc = m_run[q] * c;
+                float l_tile = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, -mc));
+                    l_tile += x[i];
+                }
+                l_run[q] += l_tile;
+                three_terms(x, pf[q]);
             }
-            float mx = s[0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
-            const float m_new = fmaxf(m_run, xhalf_max(mx));
-            if (__any((m_new - m_run) * c > 8.f)) {              // moved, and the sums rescaled, only when it has grown by 2^8
-                const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * c);
-                l_run *= alpha;
-#pragma unroll
-                for (int b = 0; b < DB; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) oacc[b][i] *= alpha;
-                m_run = m_new;
-            }
-            const float mc = m_run * c;
-            float l_tile = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -mc));
-                l_tile += s[i];
-            }
-            l_run += l_tile;
             __builtin_amdgcn_wave_barrier();                     // (a wave reads only what it wrote itself, and LDS serves it in order)
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                bf16x8 pf[3];
-                float x[8];
+            for (int b = 0; b < DB; ++b) {
+                typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+                typedef short s16x8 __attribute__((ext_vector_type(8)));
+                const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + tr[b])), v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + tr[b] + 16 * RB));
+                const bf16x8 vf = __builtin_bit_cast(bf16x8, s16x8{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]});
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = s[8 * ks + i];
-                three_terms(x, pf);
+                for (int q = 0; q < NQ; ++q)
 #pragma unroll
-                for (int b = 0; b < DB; ++b) {
-                    const bf16x8 vf = ops.tfrag(vt, 0, b, ks);
-#pragma unroll
-                    for (int x = NP - 1; x >= 0; --x) oacc[b] = mfma32(vf, pf[x], oacc[b]);
-                }
+                    for (int y = NP - 1; y >= 0; --y) oacc[q][b] = mfma16(vf, pf[q][y], oacc[q][b]);
             }
             __builtin_amdgcn_wave_barrier();
         }
     }
-    // Joins the waves: everything relative to the largest maximum, then 2 + 3 to 0 + 1, 1 to 0.
-    float l = xhalf_sum(l_run);
-    if (half == 0) {
-        stat[wave][0][l32] = m_run;
-        stat[wave][1][l32] = l;
+    // Joins the waves: everything relative to the largest maximum, then the upper half of them to the lower one, and so on.
+    float l[NQ], m[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        l[q] = quad_sum(l_run[q]);
+        if (quarter == 0) {
+            stat[wave][0][16 * q + l16] = m_run[q];
+            stat[wave][1][16 * q + l16] = l[q];
+        }
     }
     __syncthreads();
-    float m = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) m = fmaxf(m, stat[w][0][l32]);
-    auto weight = [&](float x) { return x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x - m) * a.scale_log2); };
-    l = 0.f;
+    for (int q = 0; q < NQ; ++q) {
+        m[q] = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) l += stat[w][1][l32] * weight(stat[w][0][l32]);
-    const float mine = weight(m_run);
+        for (int w = 0; w < kFewWaves; ++w) m[q] = fmaxf(m[q], stat[w][0][16 * q + l16]);
+        auto weight = [&](float x) { return x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x - m[q]) * a.scale_log2); };
+        l[q] = 0.f;
 #pragma unroll
-    for (int b = 0; b < DB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) oacc[b][i] *= mine;
-#pragma unroll
-    for (int from = 2; from > 0; from >>= 1) {
-        char *buf = smem + (wave - from) * (DB * 4096) + lane * 16;
-        if (wave >= from && wave < 2 * from) {
-#pragma unroll
-            for (int b = 0; b < DB; ++b)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    *reinterpret_cast<f32x4 *>(buf + (b * 4 + j) * 1024) = f32x4{oacc[b][4 * j], oacc[b][4 * j + 1], oacc[b][4 * j + 2], oacc[b][4 * j + 3]};
-        }
-        __syncthreads();
-        if (wave < from) {
-            buf = smem + wave * (DB * 4096) + lane * 16;
-#pragma unroll
-            for (int b = 0; b < DB; ++b)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const f32x4 x = *reinterpret_cast<const f32x4 *>(buf + (b * 4 + j) * 1024);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) oacc[b][4 * j + i] += x[i];
-                }
-        }
-        __syncthreads();
-    }
-    if (wave > 0 || !row_valid) return;
-    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;      // nothing attended: o = 0, lse = -inf
-    const float lse = l > 0.f || l != l ? m * a.scale + logf(l) : -INFINITY;
-    if (half == 0) *(a.split > 1 ? a.part_lse + (size_t)it.z * a.rows + row : a.lse + row) = lse;
-    if (a.split > 1) {
-        if (lse != -INFINITY) store_rows_f32<D>(oacc, inv, a.part + ((size_t)it.z * a.rows + row) * D, half);
-    } else {
-        T *out = static_cast<T *>(a.o) + row * D;
+        for (int w = 0; w < kFewWaves; ++w) l[q] += stat[w][1][16 * q + l16] * weight(stat[w][0][16 * q + l16]);
+        const float mine = weight(m_run[q]);
 #pragma unroll
         for (int b = 0; b < DB; ++b)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                Io<T>::store4(out + b * 32 + j * 8 + half * 4, oacc[b][4 * j] * inv, oacc[b][4 * j + 1] * inv, oacc[b][4 * j + 2] * inv, oacc[b][4 * j + 3] * inv);
+            for (int i = 0; i < 4; ++i) oacc[q][b][i] *= mine;
+    }
+#pragma unroll
+    for (int from = kFewWaves / 2; from > 0; from >>= 1) {
+        char *buf = smem + (wave >= from ? wave - from : wave) * (NQ * DB * 1024) + lane * 16;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q)
+            if (wave >= from && wave < 2 * from && 16 * q + l16 < it.count) {
+#pragma unroll
+                for (int b = 0; b < DB; ++b) *reinterpret_cast<f32x4 *>(buf + (q * DB + b) * 1024) = oacc[q][b];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < NQ; ++q)
+            if (wave < from && 16 * q + l16 < it.count) {
+#pragma unroll
+                for (int b = 0; b < DB; ++b) oacc[q][b] += *reinterpret_cast<const f32x4 *>(buf + (q * DB + b) * 1024);
+            }
+        __syncthreads();
+    }
+    if (wave > 0) return;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        if (16 * q + l16 >= it.count) continue;
+        const float inv = l[q] > 0.f || l[q] != l[q] ? 1.f / l[q] : 0.f;      // nothing attended: o = 0, lse = -inf
+        const float lse = l[q] > 0.f || l[q] != l[q] ? m[q] * a.scale + logf(l[q]) : -INFINITY;
+        if (quarter == 0) *(a.split > 1 ? a.part_lse + (size_t)it.z * a.rows + row[q] : a.lse + row[q]) = lse;
+        if (a.split > 1 && lse == -INFINITY) continue;
+#pragma unroll
+        for (int b = 0; b < DB; ++b) {
+            const f32x4 x = oacc[q][b] * inv;
+            if (a.split > 1) *reinterpret_cast<f32x4 *>(a.part + ((size_t)it.z * a.rows + row[q]) * D + 16 * b + 4 * quarter) = x;
+            else Io<T>::store4(static_cast<T *>(a.o) + row[q] * D + 16 * b + 4 * quarter, x[0], x[1], x[2], x[3]);
+        }
     }
 }
 
 template <int D, typename T> static void attn_dispatch(CacheAttnArgs &a, hipStream_t st) {
-    const int per = a.few ? kFewRows : kCrossRows;
+    const int per = a.few ? a.few : kCrossRows;
     a.tiles = 0;
     for (int s = 0; s < a.n_seg; ++s) {
         a.tile_at[s] = a.tiles;
@@ -516,7 +553,8 @@ template <int D, typename T> static void attn_dispatch(CacheAttnArgs &a, hipStre
     const long long items = (long long)a.tiles * a.BHk * a.split;
     if (a.few) {
         MOC_PROF("cache_attn_few", st);
-        cache_attn_few_kernel<D, T><<<(unsigned)items, 256, 0, st>>>(a);
+        if (a.few == 16) cache_attn_few_kernel<D, T, 1><<<(unsigned)items, 64 * kFewWaves, 0, st>>>(a);
+        else cache_attn_few_kernel<D, T, 2><<<(unsigned)items, 64 * kFewWaves, 0, st>>>(a);
     } else {
         MOC_PROF("cache_attn", st);
         cache_attn_kernel<D, T><<<xcd_grid(items), 256, 0, st>>>(a);
@@ -545,8 +583,8 @@ CachePlan cache_attn_plan(int B, int H, int Hk, int N, int M, int d, int S, int 
     const bool bf16 = dtype == MOC_BF16;
     const long long rows = (long long)B * H * N, chain = bf16 ? kChainTerms : kChainTerms / 4, least = (M + chain - 1) / chain;
     const long long group = (long long)N * (H / Hk), heads = (long long)B * Hk, own = (group + S - 1) / S;          // rows of a segment
-    p.few = own <= kFewRows;
-    const long long per = p.few ? kFewRows : kCrossRows, items = heads * std::min<long long>(S, N) * ((own + per - 1) / per);
+    p.few = own <= 16 ? 16 : own <= 32 ? 32 : 0;
+    const long long per = p.few ? p.few : kCrossRows, items = heads * std::min<long long>(S, N) * ((own + per - 1) / per);
     long long split = least;
     if (p.few) {
         auto parts = [&](long long aim) { return (aim + items - 1) / items; };
