@@ -77,16 +77,19 @@ struct CacheItem {
     int begin, end;                  // tokens that are attended
     long long row0;                  // query 0 of the segment and of the first head in [B * H * N]
 };
-__device__ __forceinline__ bool cache_item(const CacheAttnArgs &a, int logical, int rows, CacheItem &it) {
-    it.z = logical % a.split;
-    int i = logical / a.split;
-    const int bhk = i / a.tiles, t = i - bhk * a.tiles;
-    it.b = bhk / a.pool.Hk;
+// Item z of tile t of a key head of all samples. (A workgroup of few rows lives for some microseconds, in which a wave issues an instruction every seven
+// clocks: divisions are made only where there is something to divide.)
+__device__ __forceinline__ bool cache_item(const CacheAttnArgs &a, int bhk, int t, int z, int rows, CacheItem &it) {
+    it.z = z;
+    it.b = a.BHk == a.pool.Hk ? 0 : a.pool.Hk == 1 ? bhk : bhk / a.pool.Hk;
     it.hk = bhk - it.b * a.pool.Hk;
-    int s = 0, hi = a.n_seg;                                      // the last segment with tile_at <= t
-    while (hi - s > 1) {
-        const int mid = (s + hi) >> 1;
-        if (a.tile_at[mid] <= t) s = mid; else hi = mid;
+    int s = 0;
+    if (a.n_seg > 1) {
+        int hi = a.n_seg;                                         // the last segment with tile_at <= t
+        while (hi - s > 1) {
+            const int mid = (s + hi) >> 1;
+            if (a.tile_at[mid] <= t) s = mid; else hi = mid;
+        }
     }
     it.n = a.q_off[s + 1] - a.q_off[s];
     it.first = (t - a.tile_at[s]) * rows;
@@ -101,15 +104,21 @@ __device__ __forceinline__ bool cache_item(const CacheAttnArgs &a, int logical, 
     }
     it.begin = __builtin_amdgcn_readfirstlane(r.first);
     it.end = __builtin_amdgcn_readfirstlane(r.end);
+    // part z of the range: whole tiles of 32 tokens that begin at multiples of 32
+    if (a.split > 1 && it.begin < it.end) {
+        const uint32_t t0 = it.begin >> 5, tiles = ((it.end + 31) >> 5) - t0, per = (tiles + a.split - 1) / (uint32_t)a.split;
+        const uint32_t from = min(tiles, per * z), to = min(tiles, from + per);
+        it.begin = max(it.begin, (int)((t0 + from) << 5));
+        it.end = min(it.end, (int)((t0 + to) << 5));
+        if (from >= to) it.begin = it.end = 0;
+    }
     return it.count > 0;
 }
-// Part z of a range, whole tiles of 32 tokens that begin at multiples of 32.
-__device__ __forceinline__ void cache_slice(CacheItem &it, int n) {
-    if (n == 1 || it.end <= it.begin) return;
-    const int t0 = it.begin >> 5, tiles = ((it.end + 31) >> 5) - t0, begin = it.begin, end = it.end;
-    it.begin = max(begin, (t0 + (int)((long long)tiles * it.z / n)) << 5);
-    it.end = min(end, (t0 + (int)((long long)tiles * (it.z + 1) / n)) << 5);
-    if (it.end <= it.begin) it.begin = it.end = 0;
+// Row r of the list, behind row0.
+__device__ __forceinline__ int listed_row(const CacheAttnArgs &a, const CacheItem &it, int r) {
+    if (it.n == 1) return r * a.N;
+    const int g = (uint32_t)r / (uint32_t)it.n;
+    return g * a.N + (r - g * it.n);
 }
 
 // Walks a range every STRIDE tokens, where pages are there. A wave's lanes hold the page numbers and exponents of 64 blocks at a
@@ -126,7 +135,7 @@ template <int STRIDE> struct TileWalk {
     int pages, kexp, vexp;             // a lane's page and exponents
     unsigned long long there;
     __device__ __forceinline__ TileWalk(const CacheAttnArgs &a, const CacheItem &it, int from)
-        : pool(a.pool), table(a.pool.table + (size_t)it.b * a.pool.blocks), hk(it.hk), end(it.end), next(from), base(INT_MIN) {}
+        : pool(a.pool), table(a.pool.table + (size_t)it.b * a.pool.blocks), hk(it.hk), end(it.end), next(from), base(0), there(0) {}
     __device__ __forceinline__ void look(int block) {
         const int mine = block + (int)(threadIdx.x & 63);
         base = block;
@@ -137,11 +146,20 @@ template <int STRIDE> struct TileWalk {
         kexp = pool.k_exp[slot];
         vexp = pool.v_exp[slot];
     }
+    // Waits for the exponents: where they are looked up in a loop, a wait at their use would be one for the codes asked for since.
+    __device__ __forceinline__ void settle() { asm volatile("" : "+v"(kexp), "+v"(vexp)); }
+    // The first lookup, which the codes of the first tiles need not wait for: settle() is the caller's.
+    __device__ __forceinline__ void begin() {
+        if (next < end) look(next >> 6);
+    }
     // -> the next tile; false: none is left
     __device__ __forceinline__ bool step(Tile &t) {
         while (next < end) {
             const int block = next >> 6;
-            if (base == INT_MIN || block >= base + 64) look(block);
+            if (block >= base + 64) {
+                look(block);
+                settle();
+            }
             const unsigned long long rest = there >> (block - base);
             if (rest & 1) break;
             // (behind the missing pages, or the lanes; strides of pages keep their step)
@@ -154,9 +172,9 @@ template <int STRIDE> struct TileWalk {
         next += STRIDE;
         return true;
     }
-    // The scales of the last tile that step() gave. (Apart from it: the codes are asked for while exponents are on their way.)
+    // The scales of a tile, asked for before a later one is looked up.
     __device__ __forceinline__ void scales(const Tile &t, float &k, float &v) const {
-        auto pow2 = [&](int e) { return __uint_as_float((uint32_t)(min(max(__builtin_amdgcn_readlane(e, t.lane & 63), kLeastExp), kMostExp) + 127) << 23); };
+        auto pow2 = [&](int e) { return __uint_as_float((uint32_t)(min(max(__builtin_amdgcn_readlane(e, t.lane), kLeastExp), kMostExp) + 127) << 23); };
         k = pow2(kexp);
         v = pow2(vexp);
     }
@@ -170,11 +188,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
     CacheItem it;
     int logical;
-    if (!xcd_remap((long long)a.tiles * a.BHk * a.split, logical) || !cache_item(a, logical, kCrossRows, it)) return;
-    cache_slice(it, a.split);
-    const int r = wave * 32 + l32, rc = it.first + min(r, it.count - 1), g = rc / it.n;
+    if (!xcd_remap((long long)a.tiles * a.BHk * a.split, logical)) return;
+    const int i = logical / a.split, bhk = i / a.tiles;
+    if (!cache_item(a, bhk, i - bhk * a.tiles, logical - i * a.split, kCrossRows, it)) return;
+    const int r = wave * 32 + l32;
     const bool row_valid = r < it.count;
-    const int local = g * a.N + (rc - g * it.n);               // row behind row0
+    const int local = listed_row(a, it, it.first + min(r, it.count - 1));
     const size_t row = (size_t)it.row0 + local;
     float *pout = a.split > 1 ? a.part + ((size_t)it.z * a.rows + row) * D : nullptr;
     float *lout = a.split > 1 ? a.part_lse + (size_t)it.z * a.rows + row : a.lse + row;
@@ -183,6 +202,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
     for (int b = 0; b < DB; ++b) oacc[b] = zero16();
     float m_run = -INFINITY, l_run = 0.f;
     TileWalk<kPage> walk(a, it, it.begin & ~(kPage - 1));
+    walk.begin();
     Tile t;
     if (walk.step(t)) {
         // A thread's share of a tile: 16 codes of a row of K and of V (64 features: of one of the two).
@@ -206,9 +226,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
                 raw[j][1] = *reinterpret_cast<const u32x2 *>(base + (off ^ 8));
             }
         };
+        float kscale, vscale;                // of the tile in `raw`
         auto stage = [&](char *kt) {
-            float kscale, vscale;
-            walk.scales(t, kscale, vscale);
 #pragma unroll
             for (int j = 0; j < NL; ++j) {
                 const bool v = (NL == 1 ? which : j) != 0;
@@ -221,14 +240,20 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
         int pos = t.pos;                     // of the page whose tiles are in LDS, or the first of which is
         bool another = false, more = true;   // another page is there; another tile
         const bool from_half = it.begin - pos >= BN;
+        auto scales = [&] { walk.scales(t, kscale, vscale); };
         if (!from_half) {
             load(IC<0>{});
+            walk.settle();
+            scales();
             stage(smem);
             load(IC<1>{});
         } else {
             load(IC<1>{});
+            walk.settle();
+            scales();
             stage(smem + 2 * TB);
             another = walk.step(t);
+            scales();
             load(IC<0>{});
         }
         Ops<D, bf16_t> ops;
@@ -248,6 +273,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
                 if (HP == 0) {
                     more = hi > BN;
                     another = walk.step(t);
+                    scales();
                     load(IC<0>{});
                 } else {
                     more = another;
@@ -358,14 +384,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void cache_attn_few_kernel(Cache
     __shared__ float stat[kFewWaves][2][16 * NQ];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, l16 = lane & 15;
     CacheItem it;
-    if (!cache_item(a, blockIdx.x, 16 * NQ, it)) return;
-    cache_slice(it, a.split);
+    if (!cache_item(a, blockIdx.z, blockIdx.y, blockIdx.x, 16 * NQ, it)) return;
     size_t row[NQ];
     bf16x8 qf[NQ][KS][NT];                                     // (asked for before the pages are)
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-        const int rc = it.first + min(16 * q + l16, it.count - 1), g = rc / it.n;
-        row[q] = (size_t)it.row0 + (g * a.N + (rc - g * it.n));
+        row[q] = (size_t)it.row0 + listed_row(a, it, it.first + min(16 * q + l16, it.count - 1));
 #pragma unroll
         for (int s = 0; s < KS; ++s) query_terms(static_cast<const T *>(a.q) + row[q] * D + quarter * (D / 4) + 8 * s, qf[q][s]);
     }
@@ -379,23 +403,40 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void cache_attn_few_kernel(Cache
         for (int b = 0; b < DB; ++b) oacc[q][b] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     TileWalk<BN * kFewWaves> walk(a, it, (it.begin & ~31) + wave * BN);
+    walk.begin();
     Tile t;
     if (walk.step(t)) {
         constexpr int LPR = D / 16, RPL = 64 / LPR;            // V: lanes a row, rows a load
         char *vt = smem + wave * TB;
         u32x4 kraw[2][NK], vraw[NV];
+        float kscale, vscale;                                  // of the tile whose codes are asked for, which is
+        int pos;                                               // one ahead
+        const uint32_t kmine = l16 * D + quarter * (D / 4), vmine = lane * 16;
         auto load = [&] {
-            const size_t slot = (size_t)t.page * a.pool.Hk + it.hk;
-            auto at = [&](int r) { return (min(max(t.pos + r, it.begin), it.end - 1) & (kPage - 1)) * D; };      // rows outside the range repeat one inside
-            const uint8_t *kp = a.pool.k + slot * (kPage * D) + quarter * (D / 4), *vp = a.pool.v + slot * (kPage * D) + lane % LPR * 16;
+            const uint8_t *kp = a.pool.k, *vp = a.pool.v;
+            const size_t tile = ((size_t)t.page * a.pool.Hk + it.hk) * (kPage * D);
+            if (t.pos < it.begin || t.pos + BN > it.end) {     // rows outside the range repeat one inside
+                auto at = [&](int r) { return (uint32_t)(min(max(t.pos + r, it.begin), it.end - 1) & (kPage - 1)) * D; };
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int j = 0; j < NK; ++j) kraw[m][j] = *reinterpret_cast<const u32x4 *>(kp + at(16 * m + l16) + 16 * j);
+                    for (int j = 0; j < NK; ++j) kraw[m][j] = *reinterpret_cast<const u32x4 *>(kp + tile + (at(16 * m + l16) + quarter * (D / 4) + 16 * j));
 #pragma unroll
-            for (int j = 0; j < NV; ++j) vraw[j] = *reinterpret_cast<const u32x4 *>(vp + at(j * RPL + lane / LPR));
+                for (int j = 0; j < NV; ++j) vraw[j] = *reinterpret_cast<const u32x4 *>(vp + tile + (at(j * RPL + lane / LPR) + lane % LPR * 16));
+            } else {
+                const uint8_t *kt = kp + tile + (t.pos & (kPage - 1)) * D, *vt = vp + tile + (t.pos & (kPage - 1)) * D;
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int j = 0; j < NK; ++j) kraw[m][j] = *reinterpret_cast<const u32x4 *>(kt + kmine + (16 * m * D + 16 * j));
+#pragma unroll
+                for (int j = 0; j < NV; ++j) vraw[j] = *reinterpret_cast<const u32x4 *>(vt + vmine + 1024 * j);
+            }
+            pos = t.pos;
         };
         load();
+        walk.settle();
+        walk.scales(t, kscale, vscale);
         // The transposed operand of feature block b: lane (quarter, i) of the block's features i gets tokens 4 quarter .. + 4, and those 16 on.
         int tr[DB];
 #pragma unroll
@@ -406,8 +447,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void cache_attn_few_kernel(Cache
         bool more = true;
         while (more) {
             bf16x8 kw[2][KS];
-            float kscale, vscale;
-            walk.scales(t, kscale, vscale);
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -419,33 +458,36 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void cache_attn_few_kernel(Cache
                 *reinterpret_cast<u32x4 *>(vt + SwTile<D>::off(r, 2 * (lane % LPR)) * 2) = widen8(u32x2{vraw[j][0], vraw[j][1]}, vscale);
                 *reinterpret_cast<u32x4 *>(vt + SwTile<D>::off(r, 2 * (lane % LPR) + 1) * 2) = widen8(u32x2{vraw[j][2], vraw[j][3]}, vscale);
             }
-            const int lo = it.begin - t.pos, hi = it.end - t.pos;
+            const int lo = it.begin - pos, hi = it.end - pos;
             more = walk.step(t);
-            if (more) load();
+            if (more) {
+                load();
+                walk.scales(t, kscale, vscale);
+            }
             bf16x8 pf[NQ][3];
 #pragma unroll
             for (int q = 0; q < NQ; ++q) {
-                float x[8];                                      // token 16 (i / 4) + 4 quarter + i % 4
+                float y[8];                                      // token 16 (i / 4) + 4 quarter + i % 4
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
                     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int i = 0; i < KS; ++i)
 #pragma unroll
-                        for (int y = NT - 1; y >= 0; --y) s = mfma16(kw[m][i], qf[q][i][y], s);
+                        for (int z = NT - 1; z >= 0; --z) s = mfma16(kw[m][i], qf[q][i][z], s);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[4 * m + i] = s[i];
+                    for (int i = 0; i < 4; ++i) y[4 * m + i] = s[i];
                 }
                 if (lo > 0 || hi < BN) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int n = (i >> 2) * 16 + quarter * 4 + (i & 3);
-                        if (n < lo || n >= hi) x[i] = -INFINITY;
+                        if (n < lo || n >= hi) y[i] = -INFINITY;
                     }
                 }
-                float mx = x[0];
+                float mx = y[0];
 #pragma unroll
-                for (int i = 1; i < 8; ++i) mx = fmaxf(mx, x[i]);
+                for (int i = 1; i < 8; ++i) mx = fmaxf(mx, y[i]);
                 const float m_new = fmaxf(m_run[q], quad_max(mx));
                 if (__any((m_new - m_run[q]) * c > 8.f)) {       // moved, and the sums rescaled, only when it has grown by 2^8
                     const float alpha = __builtin_amdgcn_exp2f((m_run[q] - m_new) * c);
@@ -460,11 +502,11 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void cache_attn_few_kernel(Cache
                 float l_tile = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, -mc));
-                    l_tile += x[i];
+                    y[i] = __builtin_amdgcn_exp2f(fmaf(y[i], c, -mc));
+                    l_tile += y[i];
                 }
                 l_run[q] += l_tile;
-                three_terms(x, pf[q]);
+                three_terms(y, pf[q]);
             }
             __builtin_amdgcn_wave_barrier();                     // (a wave reads only what it wrote itself, and LDS serves it in order)
 #pragma unroll
@@ -553,8 +595,9 @@ template <int D, typename T> static void attn_dispatch(CacheAttnArgs &a, hipStre
     const long long items = (long long)a.tiles * a.BHk * a.split;
     if (a.few) {
         MOC_PROF("cache_attn_few", st);
-        if (a.few == 16) cache_attn_few_kernel<D, T, 1><<<(unsigned)items, 64 * kFewWaves, 0, st>>>(a);
-        else cache_attn_few_kernel<D, T, 2><<<(unsigned)items, 64 * kFewWaves, 0, st>>>(a);
+        const dim3 grid(a.split, a.tiles, a.BHk);
+        if (a.few == 16) cache_attn_few_kernel<D, T, 1><<<grid, 64 * kFewWaves, 0, st>>>(a);
+        else cache_attn_few_kernel<D, T, 2><<<grid, 64 * kFewWaves, 0, st>>>(a);
     } else {
         MOC_PROF("cache_attn", st);
         cache_attn_kernel<D, T><<<xcd_grid(items), 256, 0, st>>>(a);
