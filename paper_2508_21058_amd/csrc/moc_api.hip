@@ -1365,6 +1365,7 @@ int moc_cache_attn(const moc_cache *cache, int32_t B, int32_t H, int32_t N, int 
     a.N = N; a.M = M; a.n_seg = S; a.H = H; a.G = H / cache->Hk; a.BHk = B * cache->Hk;
     a.split = p.split;
     a.few = p.few;
+    a.full = p.full;
     a.scale = softmax_scale;
     a.scale_log2 = softmax_scale * 1.4426950408889634f;
     for (int s = 0; s <= S; ++s) a.q_off[s] = S == 1 ? s * N : q_offsets[s];

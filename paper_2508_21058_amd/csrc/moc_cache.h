@@ -31,18 +31,19 @@ struct CacheAttnArgs {
     const void *q;
     void *o;
     float *lse;
-    float *part, *part_lse;                    // split calls: [split][B * H * N][d], [split][B * H * N]
+    float *part, *part_lse;                    // of what is cut, few rows: [split][B * H * N][d], [split][B * H * N]; else [items][split][kCrossRows][d], ..
     const CrossRange *ranges;                  // [B][n_seg] or nullptr
     long long rows;                            // B * H * N
     int N, M, n_seg, H, G, BHk;                // G query heads on a key head
     int tiles, split;                          // query tiles of a key head, parts of a range
+    int slice, full;                           // many rows: items of an XCD, and how many of them are not cut
     int few;                                   // see CachePlan
     float scale, scale_log2;
     int32_t q_off[MOC_MAX_CROSS_SEGMENTS + 1];
     int32_t tile_at[MOC_MAX_CROSS_SEGMENTS + 1];      // first query tile of a segment
 };
 struct CachePlan {
-    int split;
+    int split, full;
     int few;                                   // few rows a segment: the kernel whose waves share out the tokens, with so many (16, 32) rows; else 0
     bool fits;
     size_t part, part_lse, total;              // workspace, byte offsets

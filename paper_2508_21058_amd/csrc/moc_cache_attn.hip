@@ -72,15 +72,14 @@ template <typename T> __device__ __forceinline__ void score_terms(const f32x16 &
 
 // Rows [first, first + count) of the list of a segment's queries: query i of head g is row g * n + i.
 struct CacheItem {
-    int b, hk, z;
+    int b, hk;
     int first, count, n;             // n: queries of the segment
     int begin, end;                  // tokens that are attended
     long long row0;                  // query 0 of the segment and of the first head in [B * H * N]
 };
-// Item z of tile t of a key head of all samples. (A workgroup of few rows lives for some microseconds, in which a wave issues an instruction every seven
+// Part z of tile t of a key head of all samples. (A workgroup of few rows lives for some microseconds, in which a wave issues an instruction every seven
 // clocks: divisions are made only where there is something to divide.)
-__device__ __forceinline__ bool cache_item(const CacheAttnArgs &a, int bhk, int t, int z, int rows, CacheItem &it) {
-    it.z = z;
+__device__ __forceinline__ bool cache_item(const CacheAttnArgs &a, int bhk, int t, int z, int parts, int rows, CacheItem &it) {
     it.b = a.BHk == a.pool.Hk ? 0 : a.pool.Hk == 1 ? bhk : bhk / a.pool.Hk;
     it.hk = bhk - it.b * a.pool.Hk;
     int s = 0;
@@ -105,8 +104,8 @@ __device__ __forceinline__ bool cache_item(const CacheAttnArgs &a, int bhk, int 
     it.begin = __builtin_amdgcn_readfirstlane(r.first);
     it.end = __builtin_amdgcn_readfirstlane(r.end);
     // part z of the range: whole tiles of 32 tokens that begin at multiples of 32
-    if (a.split > 1 && it.begin < it.end) {
-        const uint32_t t0 = it.begin >> 5, tiles = ((it.end + 31) >> 5) - t0, per = (tiles + a.split - 1) / (uint32_t)a.split;
+    if (parts > 1 && it.begin < it.end) {
+        const uint32_t t0 = it.begin >> 5, tiles = ((it.end + 31) >> 5) - t0, per = (tiles + parts - 1) / (uint32_t)parts;
         const uint32_t from = min(tiles, per * z), to = min(tiles, from + per);
         it.begin = max(it.begin, (int)((t0 + from) << 5));
         it.end = min(it.end, (int)((t0 + to) << 5));
@@ -187,16 +186,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
     __shared__ __attribute__((aligned(1024))) char smem[4 * TB > PATCH ? 4 * TB : PATCH];      // K, V, twice
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
     CacheItem it;
-    int logical;
-    if (!xcd_remap((long long)a.tiles * a.BHk * a.split, logical)) return;
-    const int i = logical / a.split, bhk = i / a.tiles;
-    if (!cache_item(a, bhk, i - bhk * a.tiles, logical - i * a.split, kCrossRows, it)) return;
+    // An XCD has a run of a.slice items, neighbours in heads, for its L2: the first a.full in one piece, part z of the others after part z - 1 of all of them.
+    const int xcd = blockIdx.x % kXcds, nth = blockIdx.x / kXcds, cut = a.slice - a.full, z = nth < a.full ? 0 : (nth - a.full) / cut;
+    const int in_slice = nth - z * cut, item = xcd * a.slice + in_slice, parts = in_slice < a.full ? 1 : a.split;
+    if (item >= a.tiles * a.BHk) return;
+    const int bhk = item / a.tiles;
+    if (!cache_item(a, bhk, item - bhk * a.tiles, z, parts, kCrossRows, it)) return;
     const int r = wave * 32 + l32;
     const bool row_valid = r < it.count;
     const int local = listed_row(a, it, it.first + min(r, it.count - 1));
     const size_t row = (size_t)it.row0 + local;
-    float *pout = a.split > 1 ? a.part + ((size_t)it.z * a.rows + row) * D : nullptr;
-    float *lout = a.split > 1 ? a.part_lse + (size_t)it.z * a.rows + row : a.lse + row;
+    const size_t prow = ((size_t)(xcd * cut + in_slice - a.full) * a.split + z) * kCrossRows + r;      // of the parts
     f32x16 oacc[DB];
 #pragma unroll
     for (int b = 0; b < DB; ++b) oacc[b] = zero16();
@@ -347,15 +347,66 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
     const float l = xhalf_sum(l_run);
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;      // nothing attended: o = 0, lse = -inf
     const float lse = l > 0.f || l != l ? m_run * a.scale + logf(l) : -INFINITY;
-    if (row_valid && half == 0) *lout = lse;
-    if (a.split > 1) {
-        if (row_valid && lse != -INFINITY) store_rows_f32<D>(oacc, inv, pout, half);
+    if (row_valid && half == 0) *(parts > 1 ? a.part_lse + prow : a.lse + row) = lse;
+    if (parts > 1) {
+        if (row_valid && lse != -INFINITY) store_rows_f32<D>(oacc, inv, a.part + prow * D, half);
     } else if constexpr (sizeof(T) == 4) {
         if (row_valid) store_rows_f32<D>(oacc, inv, static_cast<float *>(a.o) + row * D, half);
     } else {
         __syncthreads();
         store_rows_bf16<D>(smem, wave, lane, oacc, inv, row_valid ? local : -1, static_cast<bf16_t *>(a.o) + (size_t)it.row0 * D);
     }
+}
+
+// Joins the parts of the items that were cut: lse = log sum_z exp(lse_z), o = sum_z exp(lse_z - lse) o_z; a part without tokens has lse_z = -inf and no
+// o_z. Four features a thread, a row of 128 features in every 32.
+constexpr int kJoinThreads = 256;
+template <int D, typename T> __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheAttnArgs a) {
+    constexpr int LPR = D / 4, ROWS = kJoinThreads / LPR, WGS = kCrossRows / ROWS;
+    const int slot = blockIdx.x / WGS, cut = a.slice - a.full, xcd = slot / cut, item = xcd * a.slice + a.full + slot - xcd * cut;
+    if (item >= a.tiles * a.BHk) return;
+    const int bhk = item / a.tiles;
+    CacheItem it;
+    if (!cache_item(a, bhk, item - bhk * a.tiles, 0, 1, kCrossRows, it)) return;
+    const int c = threadIdx.x % LPR * 4;
+    const int r = blockIdx.x % WGS * ROWS + threadIdx.x / LPR;
+    if (r >= it.count) return;
+    const float *lse = a.part_lse + (size_t)slot * a.split * kCrossRows + r, *part = a.part + ((size_t)slot * a.split * kCrossRows + r) * D + c;
+    float mx = -INFINITY, sum = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    constexpr int AT = 8;                                       // parts that are asked for at once
+    for (int z0 = 0; z0 < a.split; z0 += AT) {
+        float x[AT];
+        f32x4 p[AT];
+#pragma unroll
+        for (int u = 0; u < AT; ++u) {
+            const int z = min(z0 + u, a.split - 1);
+            x[u] = lse[z * kCrossRows];
+            p[u] = *reinterpret_cast<const f32x4 *>(part + (size_t)z * kCrossRows * D);
+        }
+        float top = mx;
+#pragma unroll
+        for (int u = 0; u < AT; ++u) {
+            if (z0 + u >= a.split) x[u] = -INFINITY;
+            top = x[u] != x[u] ? INFINITY : fmaxf(top, x[u]);   // (a NaN makes the weights NaN: inf - inf)
+        }
+        if (top == -INFINITY) continue;
+        const float old = expf(mx - top);                       // (0 where there was none before)
+        sum *= old;
+        o *= old;
+        mx = top;
+#pragma unroll
+        for (int u = 0; u < AT; ++u) {
+            if (x[u] == -INFINITY) continue;                    // (its row was not written)
+            const float w = expf(x[u] - mx);
+            sum += w;
+            o += w * p[u];
+        }
+    }
+    const size_t row = (size_t)it.row0 + listed_row(a, it, it.first + r);
+    if (c == 0) a.lse[row] = mx > -INFINITY ? mx + logf(sum) : -INFINITY;
+    const float inv = mx > -INFINITY ? 1.f / sum : 0.f;
+    Io<T>::store4(static_cast<T *>(a.o) + row * D + c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
 }
 
 // The same for few rows, which is bound by HBM: a workgroup has up to 16 NQ of them, and its four waves take the tiles of its part of the range in turn,
@@ -384,7 +435,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void cache_attn_few_kernel(Cache
     __shared__ float stat[kFewWaves][2][16 * NQ];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, l16 = lane & 15;
     CacheItem it;
-    if (!cache_item(a, blockIdx.z, blockIdx.y, blockIdx.x, 16 * NQ, it)) return;
+    const int z = blockIdx.x;
+    if (!cache_item(a, blockIdx.z, blockIdx.y, z, a.split, 16 * NQ, it)) return;
     size_t row[NQ];
     bf16x8 qf[NQ][KS][NT];                                     // (asked for before the pages are)
 #pragma unroll
@@ -573,12 +625,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void cache_attn_few_kernel(Cache
         if (16 * q + l16 >= it.count) continue;
         const float inv = l[q] > 0.f || l[q] != l[q] ? 1.f / l[q] : 0.f;      // nothing attended: o = 0, lse = -inf
         const float lse = l[q] > 0.f || l[q] != l[q] ? m[q] * a.scale + logf(l[q]) : -INFINITY;
-        if (quarter == 0) *(a.split > 1 ? a.part_lse + (size_t)it.z * a.rows + row[q] : a.lse + row[q]) = lse;
+        if (quarter == 0) *(a.split > 1 ? a.part_lse + (size_t)z * a.rows + row[q] : a.lse + row[q]) = lse;
         if (a.split > 1 && lse == -INFINITY) continue;
 #pragma unroll
         for (int b = 0; b < DB; ++b) {
             const f32x4 x = oacc[q][b] * inv;
-            if (a.split > 1) *reinterpret_cast<f32x4 *>(a.part + ((size_t)it.z * a.rows + row[q]) * D + 16 * b + 4 * quarter) = x;
+            if (a.split > 1) *reinterpret_cast<f32x4 *>(a.part + ((size_t)z * a.rows + row[q]) * D + 16 * b + 4 * quarter) = x;
             else Io<T>::store4(static_cast<T *>(a.o) + row[q] * D + 16 * b + 4 * quarter, x[0], x[1], x[2], x[3]);
         }
     }
@@ -592,17 +644,31 @@ template <int D, typename T> static void attn_dispatch(CacheAttnArgs &a, hipStre
         a.tiles += ((a.q_off[s + 1] - a.q_off[s]) * a.G + per - 1) / per;
     }
     a.tile_at[a.n_seg] = a.tiles;
-    const long long items = (long long)a.tiles * a.BHk * a.split;
+    constexpr int type = sizeof(T) == 2 ? MOC_BF16 : MOC_F32;
     if (a.few) {
-        MOC_PROF("cache_attn_few", st);
-        const dim3 grid(a.split, a.tiles, a.BHk);
-        if (a.few == 16) cache_attn_few_kernel<D, T, 1><<<grid, 64 * kFewWaves, 0, st>>>(a);
-        else cache_attn_few_kernel<D, T, 2><<<grid, 64 * kFewWaves, 0, st>>>(a);
-    } else {
-        MOC_PROF("cache_attn", st);
-        cache_attn_kernel<D, T><<<xcd_grid(items), 256, 0, st>>>(a);
+        {
+            MOC_PROF("cache_attn_few", st);
+            const dim3 grid(a.split, a.tiles, a.BHk);
+            if (a.few == 16) cache_attn_few_kernel<D, T, 1><<<grid, 64 * kFewWaves, 0, st>>>(a);
+            else cache_attn_few_kernel<D, T, 2><<<grid, 64 * kFewWaves, 0, st>>>(a);
+        }
+        if (a.split > 1) launch_join(a.part, a.part_lse, a.split, a.rows, D, type, a.o, a.lse, st);
+        return;
     }
-    if (a.split > 1) launch_join(a.part, a.part_lse, a.split, a.rows, D, sizeof(T) == 2 ? MOC_BF16 : MOC_F32, a.o, a.lse, st);
+    a.slice = (int)(((long long)a.tiles * a.BHk + kXcds - 1) / kXcds);
+    if (a.split == 1 || a.full >= a.slice) {
+        a.split = 1;
+        a.full = a.slice;
+    }
+    const int cut = a.slice - a.full;
+    {
+        MOC_PROF("cache_attn", st);
+        cache_attn_kernel<D, T><<<(unsigned)(kXcds * (a.full + cut * a.split)), 256, 0, st>>>(a);
+    }
+    if (cut > 0) {
+        MOC_PROF("cache_join", st);
+        cache_join_kernel<D, T><<<(unsigned)(kXcds * cut * (kCrossRows * D / 4 / kJoinThreads)), kJoinThreads, 0, st>>>(a);
+    }
 }
 
 hipError_t launch_cache_attn(CacheAttnArgs a, int d, int dtype, hipStream_t st) {
@@ -617,9 +683,10 @@ hipError_t launch_cache_attn(CacheAttnArgs a, int d, int dtype, hipStream_t st) 
 // Few rows: 512 workgroups, two on a compute unit, of 512 tokens at least; 1,024 where they have 2,048 tokens each, so that ranges of different lengths
 // even out (eight samples, four key heads, 39k to 131k tokens: in 8 / 16 / 32 / 64 parts 167 / 145 / 141 / 144 us; four of 8k at most in 8 / 16 / 32 / 64
 // parts 26 / 24 / 25 / 29).
-// Many rows: from an estimate of the time, as for cross attention. w workgroups on a compute unit run three at a time (two heads of 128 fp32 features);
-// 32 tokens take `at_once[r - 1]` us with r of them, to begin and end 6 us a round, and parts cost their sums, written and read again. (24 heads, 1,560
+// Many rows: from an estimate of the time. w workgroups on a compute unit run three at a time (two heads of 128 fp32 features); 32 tokens take
+// `at_once[r - 1]` us with r of them, to begin and end 6 us a round, and parts cost their sums, written and read again. (24 heads, 1,560
 // queries, 33k tokens: one part 1,122 us, two 792, three 790, four 710, six 765, eight 741; two heads of 903 rows, 2k tokens: one 59, four 26, eight 22, sixteen 24.)
+// Where there are more items than the chip takes at once, whole rounds of them are left in one piece and the rest is cut.
 CachePlan cache_attn_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype) {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     CachePlan p;
@@ -628,31 +695,47 @@ CachePlan cache_attn_plan(int B, int H, int Hk, int N, int M, int d, int S, int 
     const long long group = (long long)N * (H / Hk), heads = (long long)B * Hk, own = (group + S - 1) / S;          // rows of a segment
     p.few = own <= 16 ? 16 : own <= 32 ? 32 : 0;
     const long long per = p.few ? p.few : kCrossRows, items = heads * std::min<long long>(S, N) * ((own + per - 1) / per);
+    // segments of other sizes than the average one have more tiles
+    const long long tiles = (group + per - 1) / per + S - 1, most_wgs = (1 << 24) - 1024;      // (a launch has fewer than 2^32 threads)
     long long split = least;
+    p.full = 0;
+    size_t part_rows;
     if (p.few) {
         auto parts = [&](long long aim) { return (aim + items - 1) / items; };
         split = std::max(split, std::min((M + 511LL) / 512, std::max(parts(512), std::min(parts(1024), M / 2048LL))));
+        part_rows = split > 1 ? (size_t)split * rows : 0;
+        p.fits = heads * tiles * split < most_wgs && tiles <= 65535 && (split == 1 || rows * (d / 4) / 256 < most_wgs);
     } else {
         static const double at_once[2][2][3] = {{{0.6, 0.78, 1.01}, {0.83, 1.08, 1.48}}, {{1.04, 1.49, 2.0}, {1.57, 2.13, 0}}};
-        const double *us = at_once[!bf16][d == 128], sums = (double)rows * d * 8 / 5e6;
+        const double *us = at_once[!bf16][d == 128];
         const int most = us[2] > 0 ? 3 : 2;
-        double best = 0;
-        for (long long s = least, top = std::max(least, std::min(256LL, (M + 127LL) / 128)); s <= top; ++s) {
-            const long long w = (items * s + kComputeUnits - 1) / kComputeUnits;
-            const double t = (w / most * us[most - 1] + (w % most ? us[w % most - 1] : 0)) * std::max(1., M / 32. / s) + (w + most - 1) / most * 6 +
-                             (s > 1 ? s * sums + 6 : 0);
-            if (s == least || t < best) { best = t; split = s; }
-        }
+        const long long at_a_time = (long long)most * kComputeUnits, rounds = items / at_a_time;
+        const long long first = least > 1 ? 0 : std::max(0LL, rounds - 1), last = least > 1 ? 0 : rounds, top = std::max(least, std::min(256LL, (M + 127LL) / 128));
+        auto time = [&](long long f, long long s) {
+            const long long rest = items - f * at_a_time, w = (rest * s + kComputeUnits - 1) / kComputeUnits;
+            const double whole = f * (us[most - 1] * std::max(1., M / 32.) + 6), sums = (double)rest * kCrossRows * d * 8 / 5e6;
+            return whole + (w / most * us[most - 1] + (w % most ? us[w % most - 1] : 0)) * std::max(1., M / 32. / s) + (w + most - 1) / most * 6 +
+                   (s > 1 && rest > 0 ? s * sums + 6 : 0);
+        };
+        double best = time(first, least);
+        for (long long f = first; f <= last; ++f)
+            for (long long s = least; s <= top; ++s) best = std::min(best, time(f, s));
+        for (long long f = first; f <= last; ++f)            // of what is as good, the smaller pieces: ranges differ in length
+            for (long long s = least; s <= top; ++s)
+                if (time(f, s) <= 1.02 * best) {
+                    split = s;
+                    p.full = (int)(f * at_a_time / kXcds);
+                }
+        const long long slice = (heads * tiles + kXcds - 1) / kXcds, cut = std::max(0LL, slice - p.full);
+        part_rows = split > 1 ? (size_t)(kXcds * cut * split) * kCrossRows : 0;
+        p.fits = kXcds * (p.full + cut * split) < most_wgs && kXcds * cut * (kCrossRows * d / 4 / kJoinThreads) < most_wgs;
     }
     p.split = (int)split;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t x = at; at += up(bytes); return x; };
-    p.part = take(split > 1 ? (size_t)split * rows * d * 4 : 0);
-    p.part_lse = take(split > 1 ? (size_t)split * rows * 4 : 0);
+    p.part = take(part_rows * d * 4);
+    p.part_lse = take(part_rows * 4);
     p.total = at;
-    // (a launch has fewer than 2^32 threads; segments of other sizes than the average one have more tiles)
-    const long long most = (1 << 24) - 1024, tiles = heads * ((group + per - 1) / per + S - 1);
-    p.fits = tiles * split < most && (split == 1 || rows * (d / 4) / 256 < most);
     return p;
 }
 
