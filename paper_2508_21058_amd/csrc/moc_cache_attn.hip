@@ -122,7 +122,7 @@ __device__ __forceinline__ int listed_row(const CacheAttnArgs &a, const CacheIte
 
 // Walks a range every STRIDE tokens, where pages are there. A wave's lanes hold the page numbers and exponents of 64 blocks at a
 // time: a tile's are lane reads, and a missing page is a bit that is looked over. (Asked for tile by tile through the scalar cache, each waited for the
-// answer at the next barrier: 24 heads of 4,096 queries and 32k tokens CARD us, this way NOW.)
+// answer at the next barrier: 24 heads of 4,096 queries and 32k tokens 1,665 us, this way 1,644.)
 struct Tile {
     int pos, page, lane;
 };
@@ -213,15 +213,23 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
         const int at[2] = {SwTile<D>::off(lr, 2 * lc + swap) * 2, SwTile<D>::off(lr, 2 * lc + 1 - swap) * 2};
         const uint32_t mine = lr * D + lc * 16 + 8 * swap;
         u32x2 raw[NL][2];
+        const uint8_t *kbase, *vbase;        // codes of the page that is asked for
+        bool cut_page;
+        auto turn = [&] {
+            const size_t page = ((size_t)t.page * a.pool.Hk + it.hk) * (kPage * D);
+            kbase = a.pool.k + page;
+            vbase = a.pool.v + page;
+            cut_page = t.pos < it.begin || t.pos + kPage > it.end;
+        };
+        turn();
         auto load = [&](auto half_page) {
             constexpr int HP = decltype(half_page)::value;
-            const size_t page = ((size_t)t.page * a.pool.Hk + it.hk) * (kPage * D);
             uint32_t off = mine + HP * BN * D;
-            if (t.pos < it.begin || t.pos + kPage > it.end)                        // rows outside the range repeat one inside
+            if (cut_page)                                                          // rows outside the range repeat one inside
                 off = (min(max(t.pos + HP * BN + lr, it.begin), it.end - 1) & (kPage - 1)) * D + lc * 16 + 8 * swap;
 #pragma unroll
             for (int j = 0; j < NL; ++j) {
-                const uint8_t *base = ((NL == 1 ? which : j) ? a.pool.v : a.pool.k) + page;
+                const uint8_t *base = (NL == 1 ? which : j) ? vbase : kbase;
                 raw[j][0] = *reinterpret_cast<const u32x2 *>(base + off);
                 raw[j][1] = *reinterpret_cast<const u32x2 *>(base + (off ^ 8));
             }
@@ -235,8 +243,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
                 for (int u = 0; u < 2; ++u) *reinterpret_cast<u32x4 *>(kt + (v ? TB : 0) + at[u]) = widen8(raw[j][u], v ? vscale : kscale);
             }
         };
-        // The two tiles of a page have a buffer each, and a copy of the loop. Two tiles ahead of the one in LDS is asked for, one ahead is written between
-        // the products. Behind the last tile it is asked for and written again, which nobody reads: no branch cuts the schedule.
+        // The two tiles of a page have a buffer each, and a copy of the loop. While one is in the products, the next is written to LDS (its codes have come)
+        // and the one behind it is asked for. Behind the last tile that is done again with what is there, which nobody reads. (Written after the scores or
+        // after the softmax instead: a frame of 1,560 queries 695 or 755 us for 688.)
         int pos = t.pos;                     // of the page whose tiles are in LDS, or the first of which is
         bool another = false, more = true;   // another page is there; another tile
         const bool from_half = it.begin - pos >= BN;
@@ -253,6 +262,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
             scales();
             stage(smem + 2 * TB);
             another = walk.step(t);
+            turn();
             scales();
             load(IC<0>{});
         }
@@ -268,24 +278,20 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
             constexpr int HP = decltype(half_page)::value;
             char *kt = smem + HP * 2 * TB, *vt = kt + TB, *other = smem + (HP ^ 1) * 2 * TB;
             const int lo = it.begin - pos - HP * BN, hi = it.end - pos - HP * BN;
-            auto ahead = [&] {
-                stage(other);
-                if (HP == 0) {
-                    more = hi > BN;
-                    another = walk.step(t);
-                    scales();
-                    load(IC<0>{});
-                } else {
-                    more = another;
-                    pos = t.pos;
-                    load(IC<1>{});
-                }
-            };
             __syncthreads();
-            if (wave * 32 >= it.count) {
-                ahead();
-                return;
+            stage(other);
+            if (HP == 0) {
+                more = hi > BN;
+                another = walk.step(t);
+                turn();
+                scales();
+                load(IC<0>{});
+            } else {
+                more = another;
+                pos = t.pos;
+                load(IC<1>{});
             }
+            if (wave * 32 >= it.count) return;
             ops.pin();
             f32x16 s = zero16();
 #pragma unroll
@@ -294,12 +300,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
 #pragma unroll
                 for (int x = NT - 1; x >= 0; --x) s = mfma32(kf, qf[i][x], s);
             }
-            ahead();
             if (lo > 0 || hi < BN) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int n = (i >> 2) * 8 + half * 4 + (i & 3);
-                    if (n < lo || n >= hi) s[i] = -INFINITY;
+                    const int n = (i >> 2) * 8 + (i & 3);
+                    if (half * 4 < lo - n || half * 4 >= hi - n) s[i] = -INFINITY;
                 }
             }
             float mx = s[0];
@@ -533,8 +538,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void cache_attn_few_kernel(Cache
                 if (lo > 0 || hi < BN) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int n = (i >> 2) * 16 + quarter * 4 + (i & 3);
-                        if (n < lo || n >= hi) y[i] = -INFINITY;
+                        const int n = (i >> 2) * 16 + (i & 3);
+                        if (quarter * 4 < lo - n || quarter * 4 >= hi - n) y[i] = -INFINITY;
                     }
                 }
                 float mx = y[0];
@@ -650,7 +655,7 @@ template <int D, typename T> static void attn_dispatch(CacheAttnArgs &a, hipStre
             MOC_PROF("cache_attn_few", st);
             const dim3 grid(a.split, a.tiles, a.BHk);
             if (a.few == 16) cache_attn_few_kernel<D, T, 1><<<grid, 64 * kFewWaves, 0, st>>>(a);
-            else cache_attn_few_kernel<D, T, 2><<<grid, 64 * kFewWaves, 0, st>>>(a);
+            else cache_attn_few_kernel<D, T, sizeof(T) == 4 && D == 128 ? 1 : 2><<<grid, 64 * kFewWaves, 0, st>>>(a);
         }
         if (a.split > 1) launch_join(a.part, a.part_lse, a.split, a.rows, D, type, a.o, a.lse, st);
         return;
@@ -680,7 +685,10 @@ hipError_t launch_cache_attn(CacheAttnArgs a, int d, int dtype, hipStream_t st) 
 }
 
 // Which kernel a call takes, and the parts of the ranges. Rows are those of a segment on average, so that the answer follows from the sizes alone.
-// Few rows: 512 workgroups, two on a compute unit, of 512 tokens at least; 1,024 where they have 2,048 tokens each, so that ranges of different lengths
+// Few rows: up to 16 or 32 of a segment, and up to 64 where the other kernel is slower at so many: heads of 64 features in blocks of 32 (eight samples, four
+// heads of 48 / 64 / 96 rows, 32k tokens: 52 / 53 / 82 us, the other kernel 56 / 56 / 65; 128 features 82 / 83 / 154 and 76 / 78 / 93), fp32 heads of 128 in
+// blocks of 16, two of which do not fit the registers (30 / 48 / 64 / 96 rows 73 / 147 / 128 / 199, the other kernel 111 / 153 / 155 / 164).
+// 512 workgroups, two on a compute unit, of 512 tokens at least; 1,024 where they have 2,048 tokens each, so that ranges of different lengths
 // even out (eight samples, four key heads, 39k to 131k tokens: in 8 / 16 / 32 / 64 parts 167 / 145 / 141 / 144 us; four of 8k at most in 8 / 16 / 32 / 64
 // parts 26 / 24 / 25 / 29).
 // Many rows: from an estimate of the time. w workgroups on a compute unit run three at a time (two heads of 128 fp32 features); 32 tokens take
@@ -693,7 +701,7 @@ CachePlan cache_attn_plan(int B, int H, int Hk, int N, int M, int d, int S, int 
     const bool bf16 = dtype == MOC_BF16;
     const long long rows = (long long)B * H * N, chain = bf16 ? kChainTerms : kChainTerms / 4, least = (M + chain - 1) / chain;
     const long long group = (long long)N * (H / Hk), heads = (long long)B * Hk, own = (group + S - 1) / S;          // rows of a segment
-    p.few = own <= 16 ? 16 : own <= 32 ? 32 : 0;
+    p.few = own <= 16 ? 16 : own > (bf16 && d == 128 ? 32 : 64) ? 0 : bf16 || d == 64 ? 32 : 16;
     const long long per = p.few ? p.few : kCrossRows, items = heads * std::min<long long>(S, N) * ((own + per - 1) / per);
     // segments of other sizes than the average one have more tiles
     const long long tiles = (group + per - 1) / per + S - 1, most_wgs = (1 << 24) - 1024;      // (a launch has fewer than 2^32 threads)

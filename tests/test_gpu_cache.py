@@ -277,45 +277,40 @@ def test_read_one_of_the_two_and_what_was_written():
 def reference(q, pool, Hk, ranges, offs, scale):
     """{name: (value in 64 bits, how far each element may be off)}."""
     B, H, N, d = q.shape
-    M, G, half, f32 = pool.table.shape[1] * PAGE, H // Hk, HALF[q.dtype], q.dtype == torch.float32
-    o, eo = np.zeros((B, H, N, d)), np.zeros((B, H, N, d))
-    lse, el_out = np.full((B, H, N), -math.inf), np.zeros((B, H, N))
-    x = q.double().cpu().numpy()
+    M, G, half, f32, dt = pool.table.shape[1] * PAGE, H // Hk, HALF[q.dtype], q.dtype == torch.float32, torch.float64
+    o, eo = (torch.zeros(B, H, N, d, dtype=dt, device="cuda") for _ in range(2))
+    lse, el_out = torch.full((B, H, N), -math.inf, dtype=dt, device="cuda"), torch.zeros(B, H, N, dtype=dt, device="cuda")
+    values = [torch.from_numpy(np.ldexp(c, e[:, :, None, None].astype(np.int32))).cuda() for c, e in zip(pool.codes, pool.exps)]
     for b in range(B):
+        page = torch.from_numpy(pool.table[b].astype(np.int64)).cuda()
+        ok = (page >= 0) & (page < values[0].shape[0])
+        there = ok.repeat_interleave(PAGE)
         for hk in range(Hk):
-            pos = np.arange(M)
-            K, there = pool.values(0, b, hk, pos)
-            V, _ = pool.values(1, b, hk, pos)
+            K, V = (x[torch.where(ok, page, 0), hk].reshape(M, d) for x in values)
             for s in range(len(offs) - 1):
                 a, e = (0, M) if ranges is None else ranges[b][s]
                 a, e, q0, q1 = max(a, 0), min(e, M), offs[s], offs[s + 1]
-                keep = np.flatnonzero(there[a:e]) + a if e > a else []
-                if not len(keep) or q1 <= q0:
+                if e <= a or q1 <= q0 or not bool(there[a:e].any()):
                     continue
-                k, v = K[keep], V[keep]
+                k, v = K[a:e][there[a:e]], V[a:e][there[a:e]]
+                adds = k.shape[0] * STEP
                 for h in range(hk * G, hk * G + G):
-                    Q = x[b, h, q0:q1]
+                    Q = q[b, h, q0:q1].double()
                     L = Q @ k.T * scale
-                    el = (np.abs(Q) @ np.abs(k).T).max(-1, keepdims=True) * scale * ((3 if f32 else 1) * d + 8) * STEP
-                    mx = L.max(-1, keepdims=True)
-                    P = np.exp(L - mx)
-                    Z = P.sum(-1, keepdims=True)
-                    P /= Z
-                    adds = len(keep) * STEP
+                    el = (Q.abs() @ k.abs().T).amax(-1, keepdim=True) * scale * ((3 if f32 else 1) * d + 8) * STEP
+                    P = torch.softmax(L, -1)
                     o[b, h, q0:q1] = P @ v
-                    eo[b, h, q0:q1] = (2 * el + half + (3 if f32 else 1) * adds + 4 * STEP) * (P @ np.abs(v)) + half * np.abs(o[b, h, q0:q1])
-                    lse[b, h, q0:q1] = (mx + np.log(Z))[:, 0]
-                    el_out[b, h, q0:q1] = 2 * el[:, 0] + adds + 8 * STEP * (1 + np.abs(lse[b, h, q0:q1]))
+                    eo[b, h, q0:q1] = (2 * el + half + (3 if f32 else 1) * adds + 4 * STEP) * (P @ v.abs()) + half * o[b, h, q0:q1].abs()
+                    lse[b, h, q0:q1] = torch.logsumexp(L, -1)
+                    el_out[b, h, q0:q1] = 2 * el[:, 0] + adds + 8 * STEP * (1 + lse[b, h, q0:q1].abs())
     return {"o": (o, eo), "lse": (lse, el_out)}
 
 
 def near(name, got, ref):
     value, bound = ref
-    got = got.double().cpu().numpy()
-    assert not np.isnan(got).any(), name
-    with np.errstate(invalid="ignore"):
-        off = np.where(got == value, 0.0, np.abs(got - value))
-    worst = float((off / np.maximum(bound, 1e-30)).max())
+    assert not torch.isnan(got).any(), name
+    off = torch.where(got.double() == value, torch.zeros_like(value), (got.double() - value).abs())
+    worst = float((off / bound.clamp_min(1e-30)).max())
     print(f"[cache] {name}: {worst:.3f} of the bound")
     assert (off <= bound + 1e-30).all(), f"{name}: {worst:.2f} of the bound"
 
@@ -468,6 +463,61 @@ def random_case(seed):
 def test_random_shapes(seed):
     cache, H, N, dtype, ranges, offs = random_case(seed)
     check_attn(cache, H, N, dtype, ranges=ranges, offs=offs, seed=seed)
+
+
+LARGE = [       # B, H, Hk, N, tokens, segments: more tiles of queries than the chip takes at once, whole rounds and a rest that is cut
+    (2, 24, 24, 2181, 5000, 1), (1, 12, 4, 9001, 7001, 1), (2, 24, 24, 2300, 4100, 3), (1, 24, 24, 1560, 9000, 1), (1, 8, 8, 13001, 300, 1), (3, 16, 2, 1500, 3000, 7),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("B,H,Hk,N,tokens,S", LARGE)
+def test_large_calls(B, H, Hk, N, tokens, S, d, dtype):
+    """Ranges of all samples and segments differ, one is empty; holes."""
+    g = np.random.default_rng(N)
+    cache = scattered_cache(B, tokens, Hk, d, seed=N, holes=[(b, i) for b in range(B) for i in range(3 + b, -(-tokens // PAGE), 9)])
+    offs = [N * s // S + 3 * s for s in range(S)] + [N]
+    ranges = [[(int(g.integers(0, tokens // 3)), int(g.integers(tokens // 2, tokens + 1))) for _ in range(S)] for _ in range(B)]
+    if S > 1:
+        ranges[0][1] = (77, 77)
+    check_attn(cache, H, N, dtype, ranges=ranges, offs=offs if S > 1 else None)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [128, 64])
+def test_segments_of_very_different_lengths(d, dtype):
+    """Few queries a segment on average, one segment of many: several blocks of rows of it, in the kernels for few rows."""
+    for N, offs in ((60, [0, 1, 2, 59, 60]), (300, [0, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 290, 290, 291, 292, 300]), (100, [0, 99, 100])):
+        S = len(offs) - 1
+        check_attn(scattered_cache(2, 700, 2, d), 2, N, dtype, ranges=[[(7 * s, 700 - 13 * s) for s in range(S)]] * 2, offs=offs)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows", [16, 17, 32, 33, 48, 64, 65, 128, 129])
+@pytest.mark.parametrize("d", [128, 64])
+def test_rows_around_the_kernels_blocks(d, rows, dtype):
+    """Rows of a key head: one query of many heads, and many queries of one head."""
+    for H, N in ((rows, 1), (1, rows)):
+        check_attn(scattered_cache(2, 1500, 1, d), H, N, dtype, ranges=[[(5, 1500)], [(0, 333)]])
+
+
+@pytest.mark.parametrize("N", [1, 70])
+@pytest.mark.parametrize("dtype,tokens", [(torch.bfloat16, (1 << 20) + 5000), (torch.float32, (1 << 18) + 5000)])
+def test_sums_longer_than_one_chain(dtype, tokens, N):
+    """Equal probabilities of more tokens than are added in a row: no sum is more than 2^16 (fp32 2^14) matrix additions, whose error stays within
+    2^-8 (2^-10) of what is added, in the weighted values and in the weights' own sum alike; the result's rounding is 2^-8 (2^-24)."""
+    cache = mb.kv_cache(1, tokens, 1, 64)
+    cache.k.view(torch.uint8).fill_(0x38)                     # 1.0
+    cache.v.view(torch.uint8).fill_(0x38)
+    cache.k_exp.fill_(0)
+    cache.v_exp.fill_(1)
+    q = mi.randn((1, 1, N, 64), 3, "cuda").to(dtype)
+    o, lse = mb.cache_attn(q, cache, kv_ranges=i32([[(0, tokens)]]))
+    error = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -10
+    assert float((o.double() - 2).abs().max()) <= 2 * (2 * error + HALF[dtype])
+    logit = q.double().sum(-1) * 64 ** -0.5
+    assert float((lse.double() - logit - math.log(tokens)).abs().max()) <= error + 2.0 ** -14
 
 
 @pytest.mark.parametrize("N", [1, 130])
