@@ -688,9 +688,9 @@ hipError_t launch_cache_attn(CacheAttnArgs a, int d, int dtype, hipStream_t st) 
 // Few rows: up to 16 or 32 of a segment, and up to 64 where the other kernel is slower at so many: heads of 64 features in blocks of 32 (eight samples, four
 // heads of 48 / 64 / 96 rows, 32k tokens: 52 / 53 / 82 us, the other kernel 56 / 56 / 65; 128 features 82 / 83 / 154 and 76 / 78 / 93), fp32 heads of 128 in
 // blocks of 16, two of which do not fit the registers (30 / 48 / 64 / 96 rows 73 / 147 / 128 / 199, the other kernel 111 / 153 / 155 / 164).
-// 512 workgroups, two on a compute unit, of 512 tokens at least; 1,024 where they have 2,048 tokens each, so that ranges of different lengths
-// even out (eight samples, four key heads, 39k to 131k tokens: in 8 / 16 / 32 / 64 parts 167 / 145 / 141 / 144 us; four of 8k at most in 8 / 16 / 32 / 64
-// parts 26 / 24 / 25 / 29).
+// At most 512 workgroups, two on a compute unit, of 512 tokens at least (eight samples of 131k tokens, 32 items, in 256 / 512 / 640 / 768 / 1,024 / 2,048
+// workgroups 189 / 188 / 202 / 195 / 200 / 204 us, of 39k to 131k tokens 161 / 141 / 151 / 152 / 149 / 145; two samples of 20k to 66k, 48 items, in 384 / 528 / 768
+// 108 / 127 / 107).
 // Many rows: from an estimate of the time. w workgroups on a compute unit run three at a time (two heads of 128 fp32 features); 32 tokens take
 // `at_once[r - 1]` us with r of them, to begin and end 6 us a round, and parts cost their sums, written and read again. (24 heads, 1,560
 // queries, 33k tokens: one part 1,122 us, two 792, three 790, four 710, six 765, eight 741; two heads of 903 rows, 2k tokens: one 59, four 26, eight 22, sixteen 24.)
@@ -709,8 +709,7 @@ CachePlan cache_attn_plan(int B, int H, int Hk, int N, int M, int d, int S, int 
     p.full = 0;
     size_t part_rows;
     if (p.few) {
-        auto parts = [&](long long aim) { return (aim + items - 1) / items; };
-        split = std::max(split, std::min((M + 511LL) / 512, std::max(parts(512), std::min(parts(1024), M / 2048LL))));
+        split = std::max(split, std::min((M + 511LL) / 512, 2 * kComputeUnits / items));
         part_rows = split > 1 ? (size_t)split * rows : 0;
         p.fits = heads * tiles * split < most_wgs && tiles <= 65535 && (split == 1 || rows * (d / 4) / 256 < most_wgs);
     } else {
