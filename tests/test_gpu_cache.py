@@ -412,6 +412,65 @@ def test_a_nan_stays_with_those_that_attend_it():
     assert torch.equal(torch.isnan(o), want) and torch.isfinite(lse).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N", [1, 30, 150])
+def test_a_nan_key_stays_with_those_that_attend_it(N, dtype):
+    cache = scattered_cache(2, 500, 1, 64)
+    page = int(cache.table[1, 2])
+    cache.k.view(torch.uint8)[page, 0, 0, 63] = 0xff
+    q = mi.randn((2, 2, 3 * N, 64), 3, "cuda").to(dtype)
+    offs = [0, N, 2 * N, 3 * N]
+    o, lse = mb.cache_attn(q, cache, kv_ranges=i32([[(0, 128), (0, 129), (129, 500)]] * 2), q_offsets=offs)
+    want = torch.zeros_like(lse, dtype=torch.bool)
+    want[1, :, N:2 * N] = True
+    assert torch.equal(torch.isnan(lse), want) and torch.equal(torch.isnan(o), want[..., None].expand_as(o))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N", [3, 30, 150])
+def test_a_query_that_is_not_finite_stays_alone(N, dtype):
+    cache = scattered_cache(1, 400, 1, 128)
+    q = mi.randn((1, 2, N, 128), 3, "cuda").to(dtype)
+    o, lse = mb.cache_attn(q, cache)
+    bad = q.clone()
+    bad[0, 0, 1, 5] = math.nan
+    bad[0, 1, 2, 7] = math.inf
+    o2, lse2 = mb.cache_attn(bad, cache)
+    keep = torch.ones(1, 2, N, dtype=torch.bool, device="cuda")
+    keep[0, 0, 1] = keep[0, 1, 2] = False
+    assert torch.equal(o[keep], o2[keep]) and torch.equal(lse[keep], lse2[keep])
+    assert torch.isnan(o2[~keep]).all()
+
+
+def test_exponents_that_no_write_leaves():
+    """-128 to -111 count as -110, 121 to 127 as 120, for reading, for attention and where a write finds them. (Values of 2^120 overflow in the sums: NaN
+    on both sides is the same.)"""
+    for given, taken in ((-128, -110), (-111, -110), (121, 120), (127, 120)):
+        caches = []
+        for e in (given, taken):
+            c = scattered_cache(1, 64, 1, 64)
+            c.k_exp.fill_(e)
+            c.v_exp.fill_(e)
+            x = torch.full((1, 1, 1, 64), 448.0 * 2.0 ** (100 if taken > 0 else -109), dtype=torch.bfloat16, device="cuda")
+            read = mb.cache_read(c, 64)
+            out = mb.cache_attn(x * 0, c)
+            mb.cache_write(c, x, x, i32([10]))
+            page = c.table[0].long()                          # (the pool's other pages keep what they were given)
+            caches.append([t.float() for t in (*read, *out, c.k, c.v, c.k_exp[page], c.v_exp[page])])
+        assert all(torch.allclose(a, b, rtol=0, atol=0, equal_nan=True) for a, b in zip(*caches))
+
+
+def test_write_of_broadcast_inputs():
+    cache = mb.kv_cache(3, 64, 2, 64)
+    pool = Pool(cache)
+    one = mi.randn((1, 1, 1, 64), 8, "cuda").to(torch.bfloat16)
+    x = one.expand(3, 2, 40, 64)
+    for kv in range(2):
+        pool.write(x.double().cpu().numpy(), kv, [3, 0, 24], None)
+    mb.cache_write(cache, x, x, i32([3, 0, 24]))
+    check_pool(cache, pool)
+
+
 def test_samples_share_pages():
     """A common beginning that two samples hold once."""
     cache = scattered_cache(2, 256, 2, 64)
