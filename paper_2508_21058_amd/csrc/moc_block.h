@@ -1,5 +1,5 @@
 // Arguments and launchers of the operators around the layer: head norms with rotation (moc_rope.hip) and cross attention
-// (moc_cross_fwd.hip, moc_cross_bwd.hip, moc_cross_dkdv.hip). (The cache's are in moc_cache.h.)
+// (moc_cross_fwd.hip, moc_cross_bwd.hip, moc_cross_dkdv.hip).
 #pragma once
 #include "moc_internal.h"
 
@@ -79,8 +79,6 @@ struct CrossPlan {
     size_t stats, part, part_lse, kpart, items, item_counts, total;
 };
 CrossPlan cross_plan(int B, int H, int Hk, int N, int M, int d, int S, int dtype, bool with_bwd);
-// Joins parts of attention results: o and lse from [split][rows][d] and [split][rows] (-inf: a part without a term, whose row is not read).
-void launch_join(const float *part, const float *part_lse, int split, long long rows, int d, int dtype, void *o, float *lse, hipStream_t st);
 hipError_t launch_cross_fwd(CrossArgs a, int d, int dtype, hipStream_t st);
 void launch_cross_dkdv_wide(const CrossArgs &a, hipStream_t st);
 hipError_t launch_cross_bwd(CrossArgs a, const CrossPlan &p, int d, int dtype, hipStream_t st);

@@ -363,9 +363,52 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void cache_attn_kernel
     }
 }
 
-// Joins the parts of the items that were cut: lse = log sum_z exp(lse_z), o = sum_z exp(lse_z - lse) o_z; a part without tokens has lse_z = -inf and no
-// o_z. Four features a thread, a row of 128 features in every 32.
-constexpr int kJoinThreads = 256;
+// Joins parts: lse = log sum_z exp(lse_z), o = sum_z exp(lse_z - lse) o_z; a part without tokens has lse_z = -inf and no o_z. A thread takes four features;
+// AT parts, every STEP-th from z on, are asked for at once.
+struct Joined {
+    float mx = -INFINITY, sum = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    template <int AT> __device__ __forceinline__ void add(const float *lse, const float *part, size_t rows, int d, int z, int step, int parts) {
+        for (; z < parts; z += AT * step) {
+            float x[AT];
+            f32x4 p[AT];
+#pragma unroll
+            for (int u = 0; u < AT; ++u) {
+                const size_t at = min(z + u * step, parts - 1) * rows;
+                x[u] = lse[at];
+                p[u] = *reinterpret_cast<const f32x4 *>(part + at * d);
+            }
+            float top = mx;
+#pragma unroll
+            for (int u = 0; u < AT; ++u) {
+                if (z + u * step >= parts) x[u] = -INFINITY;
+                top = x[u] != x[u] ? INFINITY : fmaxf(top, x[u]);   // (a NaN makes the weights NaN: inf - inf)
+            }
+            if (top == -INFINITY) continue;
+            turn(top);
+#pragma unroll
+            for (int u = 0; u < AT; ++u) {
+                if (x[u] == -INFINITY) continue;                    // (its row was not written)
+                const float w = expf(x[u] - mx);
+                sum += w;
+                o += w * p[u];
+            }
+        }
+    }
+    __device__ __forceinline__ void turn(float top) {
+        const float old = expf(mx - top);                           // (0 where there was none before)
+        sum *= old;
+        o *= old;
+        mx = top;
+    }
+    template <int D, typename T> __device__ __forceinline__ void store(const CacheAttnArgs &a, size_t row, int c) const {
+        if (c == 0) a.lse[row] = mx > -INFINITY ? mx + logf(sum) : -INFINITY;
+        const float inv = mx > -INFINITY ? 1.f / sum : 0.f;
+        Io<T>::store4(static_cast<T *>(a.o) + row * D + c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    }
+};
+constexpr int kJoinThreads = 256, kJoinRows = 1 << 14;
+// ... of the items that were cut, many rows.
 template <int D, typename T> __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheAttnArgs a) {
     constexpr int LPR = D / 4, ROWS = kJoinThreads / LPR, WGS = kCrossRows / ROWS;
     const int slot = blockIdx.x / WGS, cut = a.slice - a.full, xcd = slot / cut, item = xcd * a.slice + a.full + slot - xcd * cut;
@@ -373,45 +416,47 @@ template <int D, typename T> __global__ __launch_bounds__(kJoinThreads) void cac
     const int bhk = item / a.tiles;
     CacheItem it;
     if (!cache_item(a, bhk, item - bhk * a.tiles, 0, 1, kCrossRows, it)) return;
-    const int c = threadIdx.x % LPR * 4;
-    const int r = blockIdx.x % WGS * ROWS + threadIdx.x / LPR;
+    const int c = threadIdx.x % LPR * 4, r = blockIdx.x % WGS * ROWS + threadIdx.x / LPR;
     if (r >= it.count) return;
-    const float *lse = a.part_lse + (size_t)slot * a.split * kCrossRows + r, *part = a.part + ((size_t)slot * a.split * kCrossRows + r) * D + c;
-    float mx = -INFINITY, sum = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    constexpr int AT = 8;                                       // parts that are asked for at once
-    for (int z0 = 0; z0 < a.split; z0 += AT) {
-        float x[AT];
-        f32x4 p[AT];
-#pragma unroll
-        for (int u = 0; u < AT; ++u) {
-            const int z = min(z0 + u, a.split - 1);
-            x[u] = lse[z * kCrossRows];
-            p[u] = *reinterpret_cast<const f32x4 *>(part + (size_t)z * kCrossRows * D);
+    const size_t first = (size_t)slot * a.split * kCrossRows + r;
+    Joined x;
+    x.add<8>(a.part_lse + first, a.part + first * D + c, kCrossRows, D, 0, 1, a.split);
+    x.store<D, T>(a, (size_t)it.row0 + listed_row(a, it, it.first + r), c);
+}
+// ... of few rows: SL threads share the parts of four features of a row, joined through LDS in their order. (One row a workgroup where rows are few.)
+template <int D, typename T, int SL> __global__ __launch_bounds__(kJoinThreads) void cache_few_join_kernel(CacheAttnArgs a) {
+    constexpr int LPR = D / 4, ROWS = kJoinThreads / (LPR * SL);
+    static_assert(SL == 1 || ROWS == 1, "a workgroup joins one row through LDS");
+    __shared__ __attribute__((aligned(16))) float share[SL][D + 4];
+    const int c = threadIdx.x % LPR * 4, j = threadIdx.x / LPR % SL;
+    const size_t row = (size_t)blockIdx.x * ROWS + threadIdx.x / (LPR * SL);
+    if (row >= (size_t)a.rows) return;
+    Joined x;
+    x.add<SL == 1 ? 8 : 4>(a.part_lse + row, a.part + row * D + c, (size_t)a.rows, D, j, SL, a.split);
+    if (SL > 1) {
+        *reinterpret_cast<f32x4 *>(&share[j][c]) = x.o;
+        if (c == 0) {
+            share[j][D] = x.sum;
+            share[j][D + 1] = x.mx;
         }
-        float top = mx;
+        __syncthreads();
+        if (j > 0) return;
+        float top = x.mx;
 #pragma unroll
-        for (int u = 0; u < AT; ++u) {
-            if (z0 + u >= a.split) x[u] = -INFINITY;
-            top = x[u] != x[u] ? INFINITY : fmaxf(top, x[u]);   // (a NaN makes the weights NaN: inf - inf)
-        }
-        if (top == -INFINITY) continue;
-        const float old = expf(mx - top);                       // (0 where there was none before)
-        sum *= old;
-        o *= old;
-        mx = top;
+        for (int i = 1; i < SL; ++i) top = fmaxf(top, share[i][D + 1]);
+        if (top > -INFINITY) {
+            x.turn(top);
 #pragma unroll
-        for (int u = 0; u < AT; ++u) {
-            if (x[u] == -INFINITY) continue;                    // (its row was not written)
-            const float w = expf(x[u] - mx);
-            sum += w;
-            o += w * p[u];
+            for (int i = 1; i < SL; ++i) {
+                const float m = share[i][D + 1];
+                if (m == -INFINITY) continue;
+                const float w = expf(m - top);
+                x.sum += w * share[i][D];
+                x.o += w * *reinterpret_cast<const f32x4 *>(&share[i][c]);
+            }
         }
     }
-    const size_t row = (size_t)it.row0 + listed_row(a, it, it.first + r);
-    if (c == 0) a.lse[row] = mx > -INFINITY ? mx + logf(sum) : -INFINITY;
-    const float inv = mx > -INFINITY ? 1.f / sum : 0.f;
-    Io<T>::store4(static_cast<T *>(a.o) + row * D + c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    x.store<D, T>(a, row, c);
 }
 
 // The same for few rows, which is bound by HBM: a workgroup has up to 16 NQ of them, and its four waves take the tiles of its part of the range in turn,
@@ -649,7 +694,6 @@ template <int D, typename T> static void attn_dispatch(CacheAttnArgs &a, hipStre
         a.tiles += ((a.q_off[s + 1] - a.q_off[s]) * a.G + per - 1) / per;
     }
     a.tile_at[a.n_seg] = a.tiles;
-    constexpr int type = sizeof(T) == 2 ? MOC_BF16 : MOC_F32;
     if (a.few) {
         {
             MOC_PROF("cache_attn_few", st);
@@ -657,7 +701,12 @@ template <int D, typename T> static void attn_dispatch(CacheAttnArgs &a, hipStre
             if (a.few == 16) cache_attn_few_kernel<D, T, 1><<<grid, 64 * kFewWaves, 0, st>>>(a);
             else cache_attn_few_kernel<D, T, sizeof(T) == 4 && D == 128 ? 1 : 2><<<grid, 64 * kFewWaves, 0, st>>>(a);
         }
-        if (a.split > 1) launch_join(a.part, a.part_lse, a.split, a.rows, D, type, a.o, a.lse, st);
+        if (a.split > 1) {
+            MOC_PROF("cache_join", st);
+            constexpr int SL = kJoinThreads / (D / 4);
+            if (a.split <= 4 || a.rows >= kJoinRows) cache_few_join_kernel<D, T, 1><<<(unsigned)((a.rows + SL - 1) / SL), kJoinThreads, 0, st>>>(a);
+            else cache_few_join_kernel<D, T, SL><<<(unsigned)a.rows, kJoinThreads, 0, st>>>(a);
+        }
         return;
     }
     a.slice = (int)(((long long)a.tiles * a.BHk + kXcds - 1) / kXcds);

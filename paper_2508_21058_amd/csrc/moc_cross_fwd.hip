@@ -169,33 +169,18 @@ template <int D, typename T, int SL> __global__ __launch_bounds__(kJoinThreads) 
     Io<T>::store4(static_cast<T *>(a.o) + row * D + c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
 }
 
-template <int D, typename T> static void join_dispatch(const CrossArgs &a, hipStream_t st) {
-    MOC_PROF("cross_join", st);
-    constexpr int SL = kJoinThreads / (D / 4);
-    if (a.split <= kJoinFew || a.rows >= kJoinRows) cross_join_kernel<D, T, 1><<<(unsigned)((a.rows + SL - 1) / SL), kJoinThreads, 0, st>>>(a);
-    else cross_join_kernel<D, T, SL><<<(unsigned)a.rows, kJoinThreads, 0, st>>>(a);
-}
-void launch_join(const float *part, const float *part_lse, int split, long long rows, int d, int dtype, void *o, float *lse, hipStream_t st) {
-    CrossArgs a{};
-    a.part = const_cast<float *>(part);
-    a.part_lse = const_cast<float *>(part_lse);
-    a.split = split;
-    a.rows = rows;
-    a.o = o;
-    a.lse = lse;
-    if (d == 128 && dtype == MOC_BF16) join_dispatch<128, bf16_t>(a, st);
-    else if (d == 128) join_dispatch<128, float>(a, st);
-    else if (dtype == MOC_BF16) join_dispatch<64, bf16_t>(a, st);
-    else join_dispatch<64, float>(a, st);
-}
-
 template <int D, typename T> static void fwd_dispatch(CrossArgs &a, hipStream_t st) {
     cross_tiles(a);
     {
         MOC_PROF("cross_fwd", st);
         cross_fwd_kernel<D, T><<<xcd_grid((long long)a.tiles * a.copies * a.BHk * a.split), 256, 0, st>>>(a);
     }
-    if (a.split > 1) join_dispatch<D, T>(a, st);
+    if (a.split > 1) {
+        MOC_PROF("cross_join", st);
+        constexpr int SL = kJoinThreads / (D / 4);
+        if (a.split <= kJoinFew || a.rows >= kJoinRows) cross_join_kernel<D, T, 1><<<(unsigned)((a.rows + SL - 1) / SL), kJoinThreads, 0, st>>>(a);
+        else cross_join_kernel<D, T, SL><<<(unsigned)a.rows, kJoinThreads, 0, st>>>(a);
+    }
 }
 
 hipError_t launch_cross_fwd(CrossArgs a, int d, int dtype, hipStream_t st) {
