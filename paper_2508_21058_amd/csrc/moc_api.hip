@@ -1243,13 +1243,15 @@ CacheSpans cache_spans(const moc_cache *c, int32_t B) {
     return {{c->k, codes}, {c->v, codes}, {c->k_exp, heads}, {c->v_exp, heads}, {c->table, (size_t)B * c->blocks * 4}};
 }
 
-// What lies between the first and the last element of a strided tensor.
+// What lies between the first and the last element of a strided tensor; all of memory where strides reach beyond it.
 Span rows_span(const moc_rows *r, int32_t B, int32_t N, int32_t H, int32_t d, int dtype, long long sb, long long sh, long long sn) {
-    const long long s[3] = {sb * (B - 1), sh * (H - 1), sn * (N - 1)};
-    long long lo = 0, hi = d;
-    for (long long x : s) (x < 0 ? lo : hi) += x;
+    const __int128 s[3] = {(__int128)sb * (B - 1), (__int128)sh * (H - 1), (__int128)sn * (N - 1)};
+    __int128 lo = 0, hi = d;
+    for (const __int128 x : s) (x < 0 ? lo : hi) += x;
     const int e = dtype == MOC_F32 ? 4 : 2;
-    return {static_cast<const char *>(r->data) + lo * e, (size_t)(hi - lo) * e};
+    const __int128 at = reinterpret_cast<uintptr_t>(r->data), first = at + lo * e, bytes = (hi - lo) * e;
+    if (first <= 0 || first + bytes > UINTPTR_MAX) return {reinterpret_cast<const void *>((uintptr_t)1), SIZE_MAX};
+    return {reinterpret_cast<const void *>((uintptr_t)first), (size_t)bytes};
 }
 
 // The parts of a call that the write and the read share.

@@ -1,13 +1,17 @@
 // Attention over a key / value cache held in 8 bits: o = softmax(q K^T scale) V over the range of cached tokens that a query's segment attends.
 //
-// One pass with a running maximum and sum, as in cross attention's forward: S^T = K Q^T and O^T = V^T P^T, so that a lane owns a query and the scores feed
-// the second product from the registers they are in. The queries of a segment, of all query heads on a key head, are one list of rows: a workgroup
-// owns 128 of them, four waves of 32, and streams the range's pages through LDS in double-buffered tiles of 32 tokens. Codes come through
-// registers and are written to LDS as bf16, which has every value code * 2^e exactly, by an instruction that takes the exponent along: once for the
-// four waves. Calls of few rows split the range over workgroups, whose results a second launch joins.
+// Two kernels: many rows (cache_attn_kernel) and few (cache_attn_few_kernel, below). Both make one pass with a running maximum and sum, as cross attention's forward does:
+// S^T = K Q^T and O^T = V^T P^T, so that a lane owns a query and the scores feed the second product from the registers they are in.
+//
+// Many rows. The queries of a segment, of all query heads on a key head, are one list of rows: a workgroup owns 128 of them, four waves of 32, and streams
+// the range's pages through LDS in double-buffered tiles of 32 tokens. Codes come through registers and are written to LDS as bf16, which has every value
+// code * 2^e exactly, by an instruction that takes the exponent along: once for the four waves. Three workgroups share a compute unit.
+// What bounds it: the chip's power. 24 heads of 4,096 queries and 32k tokens take 1,607 to 1,640 us (1,010 to 1,026 TFLOP/s; cross attention on bf16 states
+// 1,440 to 1,480). It needs 1.26 times the cycles of that (matrix 44 %, vector 47 %, LDS 65 % of them), at 1.94 GHz for 1.69: reading operands ahead, other orders of a tile's
+// parts and fewer scalar instructions change nothing.
 //
 // fp32 queries are three bf16 terms that add up to them exactly, and so are the probabilities: since the cached values have four bits, three products on bf16
-// matrix cores are as exact as one on float cores, at a fifth of the time.
+// matrix cores are as exact as one on float cores, in three sixteenths of the matrix time (24 heads of 4,096 queries and 8k tokens 950 us, cross attention 2,940).
 #include <climits>
 
 #include "moc_cache.h"
