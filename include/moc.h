@@ -437,7 +437,7 @@ int moc_cross_attn_bwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, i
  * moc_cache: a pool of pages of MOC_CACHE_PAGE tokens, and a table that says where the tokens of a sample are.
  *   k, v          DEVICE [pages][Hk][MOC_CACHE_PAGE][d] codes in e4m3 (OCP: no infinities), 16-byte aligned
  *   k_exp, v_exp  DEVICE [pages][Hk] int8: the value of a code is code * 2^exponent. Exponents are -110 .. 120 (others are taken
- *                 for the nearest of these), so that every value is a normal number of bf16, exactly.
+ *                 for the nearest of these), so that every value is a normal number of bf16, exactly; codes from 256 on are infinite at 120.
  *   table         DEVICE [B][blocks] int32: tokens [64 i, 64 i + 64) of sample b are on page table[b][i]. A number that is
  *                 no page (-1, say) is never followed: those tokens are not there. Rows may share pages that are only read.
  * A pool filled with zeros holds zeros. Keep 64 * blocks < 2^26 and B * Hk <= 65535.
@@ -447,10 +447,11 @@ int moc_cross_attn_bwd(int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t M, i
  *   starts, counts  DEVICE [B] int32 or NULL (0; N); counts are clipped to [0, N].
  * A head's exponent on a page is the least one with |x| <= 448 * 2^exponent for every finite x that is written to it now, and not
  * less than before where tokens in front of starts[b] share the page; these keep their values as long as they are not
- * subnormal codes (below 2^(exponent - 6)), which are rounded again. Values are rounded to nearest, ties to even; NaN and
- * infinities become NaN (and do not touch other tokens). Positions behind starts[b] + counts[b] on a page that is written to hold nothing
- * afterwards (their codes stay, under another exponent): a write ends its sample there. Positions below 0 or without a page are
- * dropped. Pages that one call writes must differ: two samples that append to one page race.
+ * subnormal codes (below 2^(exponent - 6)), which are rounded again. Values are rounded to nearest, ties to even (from
+ * 248 * 2^120 = 3.3e38 on to what is infinite); NaN and infinities become NaN (and do not touch other tokens). Positions behind
+ * starts[b] + counts[b] on a page that is written to hold nothing afterwards (their codes stay, under another exponent): a write
+ * ends its sample there. Positions below 0 or without a page are dropped. Pages that one call writes must differ: two samples that
+ * append to one page race. A sample without tokens writes nothing, whatever its row of the table names.
  *
  * moc_cache_read: k_out, v_out (DEVICE out, contiguous [B,Hk,N,d], either may be NULL) from the positions starts[b] + n; rows
  * n >= counts[b], and positions that are not there, are 0. MOC_BF16 and MOC_F32 both hold the values exactly.

@@ -204,6 +204,20 @@ def test_write_again_ends_the_sample_there():
     assert torch.equal(cache.k_exp[1:3], fresh.k_exp[1:3]) and torch.equal(cache.v_exp[1:3], fresh.v_exp[1:3])
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_sample_without_tokens_writes_nothing(dtype):
+    """Samples that ended keep their table row; the page that they end on is another sample's by now, or holds an exponent that no write leaves."""
+    cache = scattered_cache(4, 128, 2, 64)
+    cache.table[1] = cache.table[0]
+    cache.table[3] = cache.table[0]
+    for e in (cache.k_exp, cache.v_exp):
+        e[int(cache.table[2, 0])] = 125
+    pool = Pool(cache)
+    k, v = states(4, 2, 70, 64, dtype, 8)
+    write_both(cache, pool, k * 1000, v * 1000, [3, 20, 5, 80], [70, 0, 0, -4])
+    check_pool(cache, pool)
+
+
 SPECIAL = {
     "zeros": [0.0, -0.0], "one": [1.0], "most": [448.0, 449.0], "just over": [448.0 * (1 + 2 ** -7)], "ties": [1.0625, 1.1875, -1.0625, 17.0, 448.0],
     "subnormal": [448.0, 2.0 ** -10, 3 * 2.0 ** -10, 2.0 ** -9, 2.0 ** -6 - 2.0 ** -11, -(2.0 ** -10)], "tiny": [2.0 ** -126, 2.0 ** -120], "denormal": [2.0 ** -133, 2.0 ** -130],
@@ -224,6 +238,20 @@ def test_write_special_values(name, dtype):
         write_both(cache, pool, one, one, [0], None)
         write_both(cache, pool, k, v, [start], None)
         check_pool(cache, pool)
+
+
+def test_values_that_round_beyond_float():
+    """248 * 2^120 and more are nearest to the code 256 or above it, 2^128 and more: infinite when read, less than that is finite."""
+    k = torch.tensor([247.0, 247.5, 249.0, 255.0]).double().mul(2.0 ** 120).float().repeat(64)[:64].reshape(1, 1, 1, 64).cuda()
+    cache = mb.kv_cache(1, 64, 1, 64)
+    mb.cache_write(cache, k, -k)
+    for dtype in (torch.bfloat16, torch.float32):
+        got = mb.cache_read(cache, 1, dtype=dtype)
+        want = torch.tensor([240.0 * 2.0 ** 120, 240.0 * 2.0 ** 120, math.inf, math.inf]).repeat(16).reshape(1, 1, 1, 64)
+        assert torch.equal(got[0].float().cpu(), want) and torch.equal(got[1].float().cpu(), -want)
+        for N in (1, 150):                                  # attended alone: the value itself
+            o, _ = mb.cache_attn(torch.zeros(1, 1, N, 64, dtype=dtype, device="cuda"), cache, kv_ranges=i32([[[0, 1]]]))
+            assert not torch.isfinite(o).any()              # (0 times an infinite key is NaN)
 
 
 def test_every_code_follows_a_growing_exponent():
